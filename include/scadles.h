@@ -354,6 +354,115 @@ scadles_status scadles_stream_simulate(uint32_t K, const uint64_t* rate, const u
                                        uint64_t b_max, int policy, uint64_t T, uint64_t* queued, uint64_t* batch,
                                        uint64_t* dropped);
 
+/* ---- AdamW over many tensors at once ----------------------------------------------------
+ * The optimizer that language models are trained with, in place of Eqn 4c:
+ * the gradients are any tensors, or the parts of the aggregate of Eqn 4b. A
+ * plan lists the tensors once; a step is one launch over all of them. Per
+ * element, with t the step's number from 1 and every operation rounded once to
+ * float in this order:
+ *   g = grad * factor                  (with a clip; see scadles_grad_norm)
+ *   m = beta1 * m + (1 - beta1) * g
+ *   v = beta2 * v + (1 - beta2) * (g * g)
+ *   d = sqrt(v) * (1 / sqrt(1 - beta2^t)) + eps
+ *   param = param * (1 - lr * weight_decay) - (m / d) * (lr / (1 - beta1^t))
+ * (the factors in parentheses are computed in double and rounded to float).
+ *
+ * 8-bit moments. Blocks of SCADLES_MOMENT_BLOCK consecutive elements of a
+ * tensor share one word of `tops`: the largest step of m in its lower half, of
+ * v in its upper half. The step of a value x is (bits(x) + u) >> 20 of the
+ * bits of |x| (the exponent and three bits of the mantissa), at most 2039, u in
+ * [0, 2^20) the dither ((i * A + t * B) mod 2^32) >> 12 of element i of its
+ * tensor at step t: A, B = 0x9E3779B9, 0xBB67AE85 for m and 0x6A09E667,
+ * 0x9E3779B9 for v. With base = max(top, span) - span, a code is step - base,
+ * clamped to [0, span]: span 127 for m, whose sign is the code's bit 7 (0 for
+ * code 0), 255 for v, where values > 0 have at least code 1. A code c > 0
+ * stands for the float of bits (c + base) << 20. The update itself uses the
+ * moments before this rounding. If a value of the block is not finite, all of
+ * the block's codes stand for NaN. All-zero bytes are zero moments.
+ *
+ *   param  (dev, n floats, 4-byte aligned) updated in place.
+ *   grad   (dev, n of the plan's type, aligned to it); not modified.
+ *   m, v   (dev, 4-byte aligned) n floats each, or n bytes each with 8-bit
+ *          moments.
+ *   tops   (dev, ceil(n / SCADLES_MOMENT_BLOCK) words) with 8-bit moments,
+ *          NULL else.
+ *   copy   (dev, n bfloat16) or NULL: receives param rounded to nearest even.
+ *   n      0 <= n <= 2^32 - 1; an empty tensor's pointers are ignored.
+ *   weight_decay  finite; 0 for tensors without decay (biases, norms).
+ * No two arrays of a tensor may overlap, nor those of different tensors (the
+ * latter is not checked).                                                   */
+#define SCADLES_F32 0
+#define SCADLES_BF16 1
+#define SCADLES_MOMENT_BLOCK 256
+typedef struct scadles_adamw_tensor {
+  float* param;
+  const void* grad;
+  void* m;
+  void* v;
+  uint32_t* tops;
+  uint16_t* copy;
+  uint64_t n;
+  float weight_decay;
+} scadles_adamw_tensor;
+
+/* A plan: a small host struct filled by scadles_adamw_plan_build (its fields
+ * are the library's), and a table in device memory of the caller that must
+ * stay in place, unmodified, as long as the plan is used.                   */
+typedef struct scadles_adamw_plan {
+  void* table;
+  uint64_t chunks_at, chunks, n;
+  uint32_t moment_bits, grad_type, magic, reserved;
+} scadles_adamw_plan;
+
+/* Bytes of the table of a plan for these tensors (only their sizes are read);
+ * 0 for arguments the build would reject: count outside [1, 2^20], a tensor
+ * of more than 2^32 - 1 elements, or more than about 2^35 elements in all.  */
+size_t scadles_adamw_plan_bytes(const scadles_adamw_tensor* tensors, uint32_t count);
+
+/* Lists the tensors (host[count], read during the call) in a plan.
+ *   moment_bits 32 or 8; grad_type SCADLES_F32 or SCADLES_BF16 (of all tensors).
+ *   table  (dev, scadles_adamw_plan_bytes(...) bytes, 256-byte aligned).
+ *   plan   (host) receives the handle.
+ * The table is written by launches on `stream`; later calls on other streams
+ * must be ordered after them. Calls with the same plan must not overlap.
+ * Build again when a pointer, a size or a weight decay changes.              */
+scadles_status scadles_adamw_plan_build(const scadles_adamw_tensor* tensors, uint32_t count, int moment_bits,
+                                        int grad_type, void* table, size_t table_bytes, scadles_adamw_plan* plan,
+                                        void* stream);
+
+/* Global norm of the plan's gradients and the clip factor that follows, in one
+ * launch: norm = sqrt(sum of all grad^2), squares and sums in double in a fixed
+ * order; factor = max_norm / norm where norm > max_norm, else 1.
+ *   max_norm  > 0; +INFINITY never clips.
+ *   clip      (dev, 2 floats, 4-byte aligned) receives norm and factor. If the
+ *             norm is not finite (some gradient is not), the factor is NaN,
+ *             and a step given this clip changes nothing.                    */
+scadles_status scadles_grad_norm(const scadles_adamw_plan* plan, double max_norm, float* clip, void* stream);
+
+/* One AdamW step of every tensor of the plan, in one launch.
+ *   options (host) lr finite; beta1, beta2 in [0, 1); eps > 0 as a float;
+ *           step the step's number, from 1 (a step that its clip turned off
+ *           counts as one if the caller counts it).
+ *   clip    (dev, 2 floats) from scadles_grad_norm, or NULL: gradients as
+ *           they are.
+ * Infinities and NaN in gradients without a clip go into the moments and
+ * parameters they belong to (with 8-bit moments: their block's moments).     */
+typedef struct scadles_adamw_options {
+  double lr, beta1, beta2, eps;
+  uint64_t step;
+} scadles_adamw_options;
+scadles_status scadles_adamw_step(const scadles_adamw_plan* plan, const scadles_adamw_options* options,
+                                  const float* clip, void* stream);
+
+/* The moments' values as floats, packed in the tensors' order (dev, as many
+ * floats as all tensors have elements, 4-byte aligned, m and v not
+ * overlapping): out of the plan's moments, or into them. 8-bit moments are
+ * rounded with the dither of `step`; values that came from
+ * scadles_adamw_get_moments are kept exactly.                                */
+scadles_status scadles_adamw_get_moments(const scadles_adamw_plan* plan, float* m, float* v, void* stream);
+scadles_status scadles_adamw_set_moments(const scadles_adamw_plan* plan, const float* m, const float* v,
+                                         uint64_t step, void* stream);
+
 /* Message for the last non-OK status returned on the calling thread.        */
 const char* scadles_last_error(void);
 

@@ -31,6 +31,7 @@ import torch as _torch_for_runtime  # noqa: E402,F401
 _lib = ctypes.CDLL(LIB_PATH)
 
 MAX_DEVICES = 64
+MOMENT_BLOCK = 256                     # SCADLES_MOMENT_BLOCK
 NOALLOC_SCRATCH_BYTES = 128 << 20      # SCADLES_NOALLOC_SCRATCH_BYTES
 PROFILE_STAGES = 5
 STAGE_NAMES = ("bracket", "main_select", "post_select", "aggregate", "total")
@@ -53,6 +54,24 @@ class StepOptions(ctypes.Structure):
 class Stream(ctypes.Structure):
     """scadles_stream: one device's stream buffer."""
     _fields_ = [("rate", _u64), ("elapsed_us", _u64), ("queued", _u64), ("trained", _u64), ("dropped", _u64)]
+
+
+class AdamWTensor(ctypes.Structure):
+    """scadles_adamw_tensor: one tensor of an AdamW plan."""
+    _fields_ = [("param", _vp), ("grad", _vp), ("m", _vp), ("v", _vp), ("tops", _vp), ("copy", _vp), ("n", _u64),
+                ("weight_decay", ctypes.c_float)]
+
+
+class AdamWPlan(ctypes.Structure):
+    """scadles_adamw_plan: the handle of a plan (its fields are the library's)."""
+    _fields_ = [("table", _vp), ("chunks_at", _u64), ("chunks", _u64), ("n", _u64), ("moment_bits", _u32),
+                ("grad_type", _u32), ("magic", _u32), ("reserved", _u32)]
+
+
+class AdamWOptions(ctypes.Structure):
+    """scadles_adamw_options: a step's hyperparameters and its number."""
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("step", _u64)]
 
 
 def _sig(name, restype, *argtypes):
@@ -103,6 +122,14 @@ _stream_iteration = _sig("scadles_stream_iteration", ctypes.c_int, _u32, ctypes.
                          ctypes.POINTER(ctypes.c_float), ctypes.POINTER(ctypes.c_double))
 _stream_simulate = _sig("scadles_stream_simulate", ctypes.c_int, _u32, ctypes.POINTER(_u64), ctypes.POINTER(_u64), _u64,
                         _u64, ctypes.c_int, _u64, ctypes.POINTER(_u64), ctypes.POINTER(_u64), ctypes.POINTER(_u64))
+_adamw_plan_bytes = _sig("scadles_adamw_plan_bytes", ctypes.c_size_t, ctypes.POINTER(AdamWTensor), _u32)
+_adamw_plan_build = _sig("scadles_adamw_plan_build", ctypes.c_int, ctypes.POINTER(AdamWTensor), _u32, ctypes.c_int,
+                         ctypes.c_int, _vp, ctypes.c_size_t, ctypes.POINTER(AdamWPlan), _vp)
+_grad_norm = _sig("scadles_grad_norm", ctypes.c_int, ctypes.POINTER(AdamWPlan), ctypes.c_double, _vp, _vp)
+_adamw_step = _sig("scadles_adamw_step", ctypes.c_int, ctypes.POINTER(AdamWPlan), ctypes.POINTER(AdamWOptions), _vp,
+                   _vp)
+_adamw_get_moments = _sig("scadles_adamw_get_moments", ctypes.c_int, ctypes.POINTER(AdamWPlan), _vp, _vp, _vp)
+_adamw_set_moments = _sig("scadles_adamw_set_moments", ctypes.c_int, ctypes.POINTER(AdamWPlan), _vp, _vp, _u64, _vp)
 _last_error = _sig("scadles_last_error", ctypes.c_char_p)
 _set_option = _sig("scadles_set_option", ctypes.c_int, ctypes.c_char_p, ctypes.c_int64)
 _profile_enable = _sig("scadles_profile_enable", ctypes.c_int, ctypes.c_int)
@@ -559,3 +586,172 @@ def step_fused(grads, ratios, weights, *, delta: float = math.inf, params=None, 
                stream=None) -> StepOutputs:
     """One-shot convenience wrapper around FusedStep."""
     return FusedStep(grads, ratios, delta=delta, params=params).run(weights, lr, stream=stream)
+
+
+# ---- AdamW ----------------------------------------------------------------------------------------
+
+class _Order:
+    """Orders calls on other streams after work that set an object up."""
+
+    def __init__(self):
+        self.event, self.ready = _torch().cuda.Event(), None
+
+    def record(self, stream):
+        self.event.record(stream)
+        self.ready = stream.cuda_stream
+
+    def enter(self, stream):
+        """The stream to run on (the current one for None), after the set-up."""
+        if stream is None:
+            stream = _torch().cuda.current_stream()
+        if stream.cuda_stream != self.ready:
+            stream.wait_event(self.event)
+        return stream
+
+
+class AdamW:
+    """AdamW over many tensors at once, one launch per step, with moments in 32
+    bits or in blocks of 8-bit codes (format: scadles.h).
+
+    ``params``: contiguous float32 tensors, updated in place; ``grads``: as many
+    contiguous tensors of the same sizes, all float32 or all bfloat16, read at
+    every step where they are (a part of a flat gradient will do, at any
+    offset). ``weight_decay``: one value, or one per tensor. ``copies``:
+    bfloat16 tensors that receive the updated parameters, or None.
+
+    The moments start at zero and belong to the object: ``m`` and ``v`` (float32
+    [n], the tensors packed in order; with ``state_bits=8`` uint8 [blocks, 256],
+    every tensor starting a block) and ``tops`` (int32 [blocks] or None), ``t``
+    the number of steps made."""
+
+    def __init__(self, params, grads, *, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay=0.01,
+                 state_bits: int = 32, copies=None, stream=None):
+        torch = _torch()
+        self.params = list(params)
+        if not self.params:
+            raise ValueError("params is empty")
+        if state_bits not in (8, 32):
+            raise ValueError("state_bits must be 32 or 8")
+        for i, p in enumerate(self.params):
+            _dev_f32(p, f"params[{i}]")
+        self.device = self.params[0].device
+        self.sizes = [p.numel() for p in self.params]
+        self.n = sum(self.sizes)
+        self.betas, self.eps, self.state_bits = (float(betas[0]), float(betas[1])), float(eps), int(state_bits)
+        L = len(self.params)
+        decay = [float(weight_decay)] * L if isinstance(weight_decay, (int, float)) else [float(w) for w in weight_decay]
+        self.copies = None if copies is None else list(copies)
+        if len(decay) != L or (self.copies is not None and len(self.copies) != L):
+            raise ValueError("one weight_decay and one copy per tensor")
+        for i, c in enumerate(self.copies or []):
+            if not isinstance(c, torch.Tensor) or c.dtype != torch.bfloat16 or not c.is_contiguous():
+                raise TypeError(f"copies[{i}] must be a contiguous bfloat16 GPU tensor")
+            if c.device != self.device or c.numel() != self.sizes[i]:
+                raise ValueError(f"copies[{i}] must be on the parameters' GPU and of their size")
+        self._order = _Order()
+        self._tensors = (AdamWTensor * L)()
+        self._plan, self._options = AdamWPlan(), AdamWOptions(0.0, self.betas[0], self.betas[1], self.eps, 0)
+        self.t = 0
+        stream = torch.cuda.current_stream() if stream is None else stream
+        with torch.cuda.stream(stream):
+            if self.state_bits == 8:
+                blocks = [-(-x // MOMENT_BLOCK) for x in self.sizes]
+                self.m = torch.zeros((sum(blocks), MOMENT_BLOCK), dtype=torch.uint8, device=self.device)
+                self.v = torch.zeros_like(self.m)
+                self.tops = torch.zeros(sum(blocks), dtype=torch.int32, device=self.device)
+            else:
+                self.m = torch.zeros(self.n, dtype=torch.float32, device=self.device)
+                self.v = torch.zeros_like(self.m)
+                self.tops = None
+            at = 0
+            m, v, tops = self.m.data_ptr(), self.v.data_ptr(), None if self.tops is None else self.tops.data_ptr()
+            for i, p in enumerate(self.params):
+                x = self._tensors[i]
+                x.param, x.n, x.weight_decay = p.data_ptr(), self.sizes[i], decay[i]
+                x.copy = None if self.copies is None else self.copies[i].data_ptr()
+                if self.state_bits == 8:
+                    x.m, x.v, x.tops = m + at * MOMENT_BLOCK, v + at * MOMENT_BLOCK, tops + at * 4
+                    at += blocks[i]
+                else:
+                    x.m, x.v = m + at * 4, v + at * 4
+                    at += self.sizes[i]
+            self._table = _workspace(int(_adamw_plan_bytes(self._tensors, L)), self.device)
+            self.clip = torch.zeros(2, dtype=torch.float32, device=self.device)
+        self.set_grads(grads, stream=stream)
+
+    def set_grads(self, grads, *, stream=None):
+        """Point the optimizer at other gradients of the same sizes (writes the plan anew)."""
+        torch = _torch()
+        grads = list(grads)
+        if len(grads) != len(self.params):
+            raise ValueError("one gradient per parameter")
+        for i, g in enumerate(grads):
+            if not isinstance(g, torch.Tensor) or not g.is_cuda or not g.is_contiguous():
+                raise TypeError(f"grads[{i}] must be a contiguous GPU tensor")
+            if g.dtype not in (torch.float32, torch.bfloat16) or g.dtype != grads[0].dtype:
+                raise TypeError("grads must be all float32 or all bfloat16")
+            if g.device != self.device or g.numel() != self.sizes[i]:
+                raise ValueError(f"grads[{i}] must be on the parameters' GPU and of their size")
+            self._tensors[i].grad = g.data_ptr()
+        stream = self._order.enter(stream) if self._order.ready is not None else stream or torch.cuda.current_stream()
+        _check(_adamw_plan_build(self._tensors, len(grads), self.state_bits, 1 if grads[0].dtype == torch.bfloat16 else 0,
+                                 self._table.data_ptr(), self._table.numel(), ctypes.byref(self._plan),
+                                 stream.cuda_stream))
+        self.grads = grads
+        self._order.record(stream)
+
+    def grad_norm(self, max_norm: float = math.inf, *, stream=None):
+        """float32[2] = (global norm of the gradients, factor that clips it to
+        ``max_norm``), for ``step``; the factor is NaN when the norm is not
+        finite. The tensor is the object's own and overwritten by the next call."""
+        stream = self._order.enter(stream)
+        _check(_grad_norm(ctypes.byref(self._plan), float(max_norm), self.clip.data_ptr(), stream.cuda_stream))
+        return self.clip
+
+    def step(self, lr: float, *, clip=None, stream=None):
+        """One step, with the gradients times clip[1] when given (as from
+        ``grad_norm``; a NaN there leaves everything but ``t`` as it is)."""
+        stream = self._order.enter(stream)
+        o = self._options
+        o.lr, o.step = float(lr), self.t + 1
+        if clip is not None and clip.numel() != 2:
+            raise ValueError("clip must have two entries")
+        _check(_adamw_step(ctypes.byref(self._plan), ctypes.byref(o), None if clip is None else _dev_f32(clip, "clip"),
+                           stream.cuda_stream))
+        self.t += 1
+
+    def moments(self, *, stream=None):
+        """(m, v) as float32 [n], the tensors packed in order: the 32-bit moments
+        themselves, or what the 8-bit codes stand for."""
+        if self.state_bits == 32:
+            return self.m, self.v
+        torch = _torch()
+        stream = self._order.enter(stream)
+        with torch.cuda.stream(stream):
+            m, v = (torch.empty(self.n, dtype=torch.float32, device=self.device) for _ in range(2))
+        _check(_adamw_get_moments(ctypes.byref(self._plan), m.data_ptr(), v.data_ptr(), stream.cuda_stream))
+        return m, v
+
+    def load(self, t: int, m, v, *, tops=None, stream=None):
+        """Continue from step ``t`` with these moments: the values as ``moments``
+        gives them, or the codes ``m``, ``v`` with ``tops``."""
+        torch = _torch()
+        if t < 0:
+            raise ValueError("t must not be negative")
+        stream = self._order.enter(stream)
+        if tops is not None:
+            if self.state_bits != 8:
+                raise ValueError("tops belongs to 8-bit moments")
+            for x, mine, name in ((m, self.m, "m"), (v, self.v, "v"), (tops, self.tops, "tops")):
+                if x.dtype != mine.dtype or x.shape != mine.shape:
+                    raise ValueError(f"{name} must be {mine.dtype} of shape {tuple(mine.shape)}")
+            with torch.cuda.stream(stream):
+                for x, mine in ((m, self.m), (v, self.v), (tops, self.tops)):
+                    mine.copy_(x)
+        else:
+            if m.numel() != self.n or v.numel() != self.n:
+                raise ValueError("m and v must hold every element")
+            _check(_adamw_set_moments(ctypes.byref(self._plan), _dev_f32(m, "m"), _dev_f32(v, "v"), int(t),
+                                      stream.cuda_stream))
+        self.t = int(t)
+        self._order.record(stream)
