@@ -463,6 +463,92 @@ scadles_status scadles_adamw_get_moments(const scadles_adamw_plan* plan, float* 
 scadles_status scadles_adamw_set_moments(const scadles_adamw_plan* plan, const float* m, const float* v,
                                          uint64_t step, void* stream);
 
+/* ---- the router of a mixture of experts ----------------------------------------------------
+ * The tokens of K devices (of streams of different rates, so of batches of
+ * different sizes) are routed to E experts, k per token, and the losses that
+ * keep the experts evenly used are taken over all devices with the Eqn 4a
+ * weights, not device by device: a slow stream's few tokens say little about
+ * the load. For row t of device d, x its logits and n_d the device's counted
+ * rows:
+ *   p = softmax(x), lse = log sum exp(x)
+ *   idx  = the k experts of the largest x, in descending order, ties to the
+ *          lower index (as scadles_topk_select breaks them)
+ *   gate = p of those, divided by their sum if renormalise is set
+ *   counts[d][e] = choices of e by d's rows
+ *   load_e = sum_d weights[d] * counts[d][e] / (k * n_d)
+ *   prob_e = sum_d weights[d] / n_d * sum_t p_e
+ *   loss[0] = E * sum_e load_e * prob_e           (balance; 1 when even)
+ *   loss[1] = sum_d weights[d] / n_d * sum_t lse^2    (z)
+ * Softmax statistics are kept in float, sums over rows in double in a fixed
+ * order. An expert at -infinity is never chosen: missing choices have index -1
+ * and gate 0. A row with `valid` 0, or with every logit at -infinity, routes
+ * nowhere: indices -1, gates, lse and gradient 0, not counted. A device without
+ * counted rows adds nothing. A NaN or +infinity makes its row's gates, lse and
+ * gradient and the losses NaN; indices stay within [-1, E).                  */
+#define SCADLES_ROUTER_MAX_EXPERTS 1024
+#define SCADLES_ROUTER_MAX_K 16
+
+/* Shape of a call.
+ *   tokens       rows of logits, 0 <= tokens <= 2^31 - 1.
+ *   experts, k   1 <= experts <= SCADLES_ROUTER_MAX_EXPERTS; 1 <= k <=
+ *                min(experts, SCADLES_ROUTER_MAX_K).
+ *   devices      1 <= devices <= SCADLES_MAX_DEVICES.
+ *   tok_off      (host[devices + 1]) rows [tok_off[d], tok_off[d + 1]) are
+ *                device d's; from 0 to tokens, not decreasing.
+ *   weights      (host[devices]) finite and >= 0.
+ *   ld           elements between the starts of two rows, >= experts.
+ *   logits_type  SCADLES_F32 or SCADLES_BF16.                                */
+typedef struct scadles_router {
+  uint64_t tokens;
+  uint64_t ld;
+  const uint64_t* tok_off;
+  const float* weights;
+  uint32_t experts, k, devices;
+  int32_t logits_type;
+  int32_t renormalise;
+} scadles_router;
+
+/* What the forward pass writes and the backward pass reads (dev, 4-byte
+ * aligned, not overlapping): idx and gate tokens x k, lse tokens, counts
+ * devices x experts, load experts, share devices (1 / n_d, 0 without rows),
+ * loss 2.                                                                    */
+typedef struct scadles_router_out {
+  int32_t* idx;
+  float* gate;
+  float* lse;
+  int32_t* counts;
+  float* load;
+  float* share;
+  float* loss;
+} scadles_router_out;
+
+/* Workspace bytes of scadles_router_forward for up to `tokens` rows, however
+ * they are spread over the devices; 0 for arguments the call would reject.  */
+size_t scadles_router_workspace_bytes(uint64_t tokens, uint32_t experts, uint32_t devices);
+
+/* Forward pass.
+ *   logits  (dev, tokens rows of experts elements, aligned to its type).
+ *   valid   (dev, tokens bytes) or NULL: 0 marks rows that are padding.
+ *   router->weights must sum to 1 within devices * 2^-23.                    */
+scadles_status scadles_router_forward(const scadles_router* router, const void* logits, const uint8_t* valid,
+                                      const scadles_router_out* out, void* ws, size_t ws_bytes, void* stream);
+
+/* Gradient of the logits, with load held constant:
+ *   dlogits = weights[d] / n_d * p * (dloss[0] * E * (load - sum_j load_j p_j)
+ *             + 2 * dloss[1] * lse) + the gradient of the gates under dgate.
+ *   router   as in the forward pass, except for the weights, which need not
+ *            sum to 1: the forward's give the gradient of its losses; ones
+ *            give each device's own share, for scadles_weighted_aggregate
+ *            to weight.
+ *   out      the forward pass's; counts and loss are not read.
+ *   dgate    (dev, tokens x k floats) or NULL (zero).
+ *   dloss    (dev, 2 floats) or NULL (zero).
+ *   dlogits  (dev, tokens rows of experts elements of the logits' type, ld_out
+ *            elements between rows) overwritten; may not overlap an input.    */
+scadles_status scadles_router_backward(const scadles_router* router, const void* logits, const scadles_router_out* out,
+                                       const float* dgate, const float* dloss, void* dlogits, uint64_t ld_out,
+                                       void* stream);
+
 /* Message for the last non-OK status returned on the calling thread.        */
 const char* scadles_last_error(void);
 

@@ -32,6 +32,7 @@ _lib = ctypes.CDLL(LIB_PATH)
 
 MAX_DEVICES = 64
 MOMENT_BLOCK = 256                     # SCADLES_MOMENT_BLOCK
+ROUTER_MAX_EXPERTS, ROUTER_MAX_K = 1024, 16
 NOALLOC_SCRATCH_BYTES = 128 << 20      # SCADLES_NOALLOC_SCRATCH_BYTES
 PROFILE_STAGES = 5
 STAGE_NAMES = ("bracket", "main_select", "post_select", "aggregate", "total")
@@ -72,6 +73,19 @@ class AdamWOptions(ctypes.Structure):
     """scadles_adamw_options: a step's hyperparameters and its number."""
     _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
                 ("eps", ctypes.c_double), ("step", _u64)]
+
+
+class RouterShape(ctypes.Structure):
+    """scadles_router: the shape of a router call."""
+    _fields_ = [("tokens", _u64), ("ld", _u64), ("tok_off", ctypes.POINTER(_u64)),
+                ("weights", ctypes.POINTER(ctypes.c_float)), ("experts", _u32), ("k", _u32), ("devices", _u32),
+                ("logits_type", ctypes.c_int32), ("renormalise", ctypes.c_int32)]
+
+
+class RouterOut(ctypes.Structure):
+    """scadles_router_out: what the router's forward pass writes."""
+    _fields_ = [("idx", _vp), ("gate", _vp), ("lse", _vp), ("counts", _vp), ("load", _vp), ("share", _vp),
+                ("loss", _vp)]
 
 
 def _sig(name, restype, *argtypes):
@@ -130,6 +144,11 @@ _adamw_step = _sig("scadles_adamw_step", ctypes.c_int, ctypes.POINTER(AdamWPlan)
                    _vp)
 _adamw_get_moments = _sig("scadles_adamw_get_moments", ctypes.c_int, ctypes.POINTER(AdamWPlan), _vp, _vp, _vp)
 _adamw_set_moments = _sig("scadles_adamw_set_moments", ctypes.c_int, ctypes.POINTER(AdamWPlan), _vp, _vp, _u64, _vp)
+_router_ws_bytes = _sig("scadles_router_workspace_bytes", ctypes.c_size_t, _u64, _u32, _u32)
+_router_forward = _sig("scadles_router_forward", ctypes.c_int, ctypes.POINTER(RouterShape), _vp, _vp,
+                       ctypes.POINTER(RouterOut), _vp, ctypes.c_size_t, _vp)
+_router_backward = _sig("scadles_router_backward", ctypes.c_int, ctypes.POINTER(RouterShape), _vp,
+                        ctypes.POINTER(RouterOut), _vp, _vp, _vp, _u64, _vp)
 _last_error = _sig("scadles_last_error", ctypes.c_char_p)
 _set_option = _sig("scadles_set_option", ctypes.c_int, ctypes.c_char_p, ctypes.c_int64)
 _profile_enable = _sig("scadles_profile_enable", ctypes.c_int, ctypes.c_int)
@@ -755,3 +774,119 @@ class AdamW:
                                       stream.cuda_stream))
         self.t = int(t)
         self._order.record(stream)
+
+
+# ---- the router of a mixture of experts ---------------------------------------------------------------
+
+@dataclass
+class RouterOutputs:
+    """What ``Router.forward`` returns (the router's own buffers, overwritten by
+    its next forward pass); ``shape`` is the call's, for the backward pass."""
+    idx: object          # int32 [T, k], -1 where there is no choice
+    gate: object         # float32 [T, k]
+    lse: object          # float32 [T]
+    counts: object       # int32 [devices, experts]
+    load: object         # float32 [experts]
+    share: object        # float32 [devices]: 1 / counted rows
+    loss: object         # float32 [2]: balance, z
+    shape: object
+
+
+class Router:
+    """Routes the tokens of K devices to ``experts`` experts, ``k`` each, with the
+    balance loss and the z loss over all devices (scadles_router_forward), and
+    gives the logits' gradient. Outputs and workspace are allocated once, for up
+    to ``max_tokens`` rows."""
+
+    def __init__(self, max_tokens: int, experts: int, k: int, *, devices: int = 1, renormalise: bool = False,
+                 device=None):
+        torch = _torch()
+        self.max_tokens, self.experts, self.k, self.devices = int(max_tokens), int(experts), int(k), int(devices)
+        self.renormalise = bool(renormalise)
+        need = int(_router_ws_bytes(self.max_tokens, self.experts, self.devices)) if self.max_tokens >= 0 else 0
+        if need == 0 or not 1 <= self.k <= min(self.experts, ROUTER_MAX_K):
+            raise ScadlesError(1, f"invalid max_tokens={max_tokens}, experts={experts}, k={k} or devices={devices}")
+        dev = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
+        f32 = dict(dtype=torch.float32, device=dev)
+        T, E, K = self.max_tokens, self.experts, self.devices
+        self.idx = torch.empty((T, self.k), dtype=torch.int32, device=dev)
+        self.gate, self.lse = torch.empty((T, self.k), **f32), torch.empty(T, **f32)
+        self.counts = torch.empty((K, E), dtype=torch.int32, device=dev)
+        self.load, self.share, self.loss = torch.empty(E, **f32), torch.empty(K, **f32), torch.empty(2, **f32)
+        self.ws = _workspace(need, dev)
+        self._out = RouterOut(*[x.data_ptr() for x in (self.idx, self.gate, self.lse, self.counts, self.load, self.share,
+                                                       self.loss)])
+
+    def _logits(self, x, name):
+        torch = _torch()
+        if not isinstance(x, torch.Tensor) or not x.is_cuda or x.dtype not in (torch.float32, torch.bfloat16):
+            raise TypeError(f"{name} must be a float32 or bfloat16 GPU tensor")
+        if x.dim() != 2 or x.shape[1] != self.experts or (x.shape[1] > 1 and x.stride(1) != 1):
+            raise ValueError(f"{name} must be [tokens, {self.experts}] with adjacent experts")
+        if x.shape[0] > 1 and x.stride(0) < self.experts:
+            raise ValueError(f"{name}: rows overlap")
+        return x.data_ptr(), x.stride(0) if x.shape[0] > 1 else self.experts
+
+    def _weights(self, weights):
+        w = np.ascontiguousarray(weights, dtype=np.float32)
+        if w.shape != (self.devices,):
+            raise ValueError("one weight per device")
+        return (ctypes.c_float * self.devices).from_buffer_copy(w)
+
+    def forward(self, logits, *, tok_off=None, weights=None, valid=None, stream=None) -> RouterOutputs:
+        """``logits`` [T, experts] float32 or bfloat16, rows ``tok_off[d]`` to
+        ``tok_off[d + 1]`` those of device d (None: one device). ``weights``: Eqn
+        4a, by default the devices' shares of the rows. ``valid``: bool [T] or
+        None; False marks padding."""
+        torch = _torch()
+        p, ld = self._logits(logits, "logits")
+        T = logits.shape[0]
+        if T > self.max_tokens:
+            raise ValueError(f"more than max_tokens = {self.max_tokens} rows")
+        off = [0, T] if tok_off is None else tok_off
+        if len(off) != self.devices + 1:
+            raise ValueError("tok_off must have devices + 1 entries")
+        off = (_u64 * len(off))(*off)
+        if weights is None:
+            weights = [(off[d + 1] - off[d]) / T if T else 1.0 / self.devices for d in range(self.devices)]
+        if valid is not None:
+            if valid.dtype not in (torch.bool, torch.uint8) or not valid.is_cuda or not valid.is_contiguous():
+                raise TypeError("valid must be a contiguous bool GPU tensor")
+            if valid.numel() != T:
+                raise ValueError("valid must have one entry per row")
+        w = self._weights(weights)
+        shape = RouterShape(T, ld, off, w, self.experts, self.k, self.devices, logits.dtype == torch.bfloat16,
+                            self.renormalise)
+        _check(_router_forward(ctypes.byref(shape), p, None if valid is None else valid.data_ptr(),
+                               ctypes.byref(self._out), self.ws.data_ptr(), self.ws.numel(), _stream_ptr(stream)))
+        return RouterOutputs(self.idx[:T], self.gate[:T], self.lse[:T], self.counts, self.load, self.share, self.loss,
+                             shape)
+
+    def backward(self, logits, out: RouterOutputs, d_gate=None, d_loss=None, *, weights=None, d_logits=None, stream=None):
+        """Gradient of ``logits`` under ``d_gate`` [T, k] (or None) of the gates and
+        ``d_loss`` [2] (or None) of the losses, both float32. ``weights``: as in the
+        forward pass by default; ones give each device's own share, before the
+        aggregation weights it. Returned in ``d_logits`` if given."""
+        torch = _torch()
+        p, ld = self._logits(logits, "logits")
+        f, T = out.shape, logits.shape[0]
+        if out.load is not self.load:
+            raise ValueError("out is another router's")
+        if T != f.tokens or f.logits_type != (logits.dtype == torch.bfloat16):
+            raise ValueError("logits are not those of the forward pass")
+        for x, n, name in ((d_gate, T * self.k, "d_gate"), (d_loss, 2, "d_loss")):
+            if x is not None and x.numel() != n:
+                raise ValueError(f"{name} must have {n} entries")
+        if d_logits is None:
+            stream = torch.cuda.current_stream() if stream is None else stream
+            with torch.cuda.stream(stream):
+                d_logits = torch.empty((T, self.experts), dtype=logits.dtype, device=logits.device)
+        q, ld_out = self._logits(d_logits, "d_logits")
+        if d_logits.dtype != logits.dtype or d_logits.shape[0] != T:
+            raise ValueError("d_logits must be like logits")
+        shape = RouterShape(f.tokens, ld, f.tok_off, f.weights if weights is None else self._weights(weights), f.experts,
+                            f.k, f.devices, f.logits_type, f.renormalise)
+        _check(_router_backward(ctypes.byref(shape), p, ctypes.byref(self._out),
+                                None if d_gate is None else _dev_f32(d_gate, "d_gate"),
+                                None if d_loss is None else _dev_f32(d_loss, "d_loss"), q, ld_out, _stream_ptr(stream)))
+        return d_logits

@@ -32,8 +32,8 @@
 #include <cstring>
 
 #include "abi.h"
-#include "frame.h"
 #include "radix.h"
+#include "vec4.h"
 
 using namespace scadles;
 
@@ -139,64 +139,6 @@ __global__ __launch_bounds__(kBlock) void k_adamw_chunks(const Tensor* t, uint32
   r.i0 = (uint32_t)e;
   r.wd = x.wd;
   out[c] = r;
-}
-
-// ---- four consecutive elements of a tensor at any alignment of its type ---------------------
-// Tensors may start anywhere in a flat buffer; the memory system takes wide
-// accesses at the element's own alignment.
-typedef f4 f4any __attribute__((aligned(4)));
-typedef uint16_t h4any __attribute__((ext_vector_type(4), aligned(2)));
-
-__device__ inline f4 load_f4(const float* p, uint32_t k)
-{
-  if (k >= 4) return *(const GLOBAL f4any*)gptr(p);
-  f4 x = {};
-  for (uint32_t q = 0; q < 3; ++q)
-    if (q < k) x[q] = gptr(p)[q];
-  return x;
-}
-
-__device__ inline f4 load_once_f4(const float* p, uint32_t k)
-{
-  return k >= 4 ? (f4)__builtin_nontemporal_load((const GLOBAL f4any*)gptr(p)) : load_f4(p, k);
-}
-
-__device__ inline f4 load_once_f4(const uint16_t* p, uint32_t k)
-{
-  h4any h = {};
-  if (k >= 4) {
-    h = __builtin_nontemporal_load((const GLOBAL h4any*)gptr(p));
-  } else {
-    for (uint32_t q = 0; q < 3; ++q)
-      if (q < k) h[q] = gptr(p)[q];
-  }
-  f4 x;
-#pragma unroll
-  for (int q = 0; q < 4; ++q) x[q] = __uint_as_float((uint32_t)h[q] << 16);
-  return x;
-}
-
-__device__ inline void store_f4(float* p, f4 x, uint32_t k)
-{
-  if (k >= 4) {
-    *(GLOBAL f4any*)gptr(p) = x;
-    return;
-  }
-  for (uint32_t q = 0; q < 3; ++q)
-    if (q < k) gptr(p)[q] = x[q];
-}
-
-__device__ inline void store_bf16(uint16_t* p, f4 x, uint32_t k)
-{
-  h4any h;
-#pragma unroll
-  for (int q = 0; q < 4; ++q) h[q] = __builtin_bit_cast(uint16_t, (__bf16)x[q]);   // to nearest, ties to even
-  if (k >= 4) {
-    *(GLOBAL h4any*)gptr(p) = h;
-    return;
-  }
-  for (uint32_t q = 0; q < 3; ++q)
-    if (q < k) gptr(p)[q] = h[q];
 }
 
 __device__ inline uint32_t load_codes(const uint8_t* p, uint32_t k)
@@ -340,7 +282,7 @@ __global__ __launch_bounds__(kBlock) void k_adamw(const Chunk* chunks, StepArgs 
       v[q] = vq;
     }
     store_f4(c.p + e, p, k);
-    if (c.copy) store_bf16(c.copy + e, p, k);
+    if (c.copy) store_f4(c.copy + e, p, k);
     if (kBits8) {
 #pragma unroll
       for (uint32_t q = 0; q < 4; ++q)

@@ -1,0 +1,677 @@
+// router.hip -- the router of a mixture of experts whose tokens lie on K devices:
+// softmax, Top-k choice, gates, expert counts, the balance loss and the z loss
+// over all devices, and the gradient of the logits.
+//
+// Row t of device d (weight w_d, n_d counted rows), E experts, k choices:
+//   p = softmax(x), lse = log sum exp(x), S = the k largest x (ties: the lower index)
+//   gate = p over S, or p over S divided by its sum
+//   load_e = sum_d w_d / (k n_d) * c_de,   prob_e = sum_d w_d / n_d * sum_t p_te
+//   balance = E sum_e load_e prob_e,       z = sum_d w_d / n_d * sum_t lse^2
+// Backward (load is a constant), a and b the losses' incoming gradients:
+//   dx = w_d / n_d * p (a E (load - sum_j load_j p_j) + 2 b lse) + the gates' part,
+//   which is gate (dgate - sum gate dgate) over S, or p (dgate over S - sum gate dgate).
+//
+// Both directions read the logits once. A row lies in the registers of a group
+// of G lanes, V elements each, so that its maximum, sums and choices are a few
+// lane exchanges; a workgroup takes several rounds of 256 / G rows of one
+// device and keeps the experts' probability sums in registers meanwhile.
+#include <cmath>
+#include <cstring>
+
+#include "abi.h"
+#include "radix.h"
+#include "vec4.h"
+
+using namespace scadles;
+
+namespace {
+
+constexpr uint32_t kMaxChoices = SCADLES_ROUTER_MAX_K;
+constexpr uint32_t kMaxExperts = SCADLES_ROUTER_MAX_EXPERTS;
+constexpr uint32_t kFinishExperts = 32;    // experts of one workgroup of k_route_finish
+constexpr int kFinishBlock = 1024;
+constexpr uint32_t kRouteBlocks = 1024;    // workgroups aimed at when rounds are chosen,
+constexpr uint32_t kMaxRounds = 256;       // and the most rounds of one: it sums probabilities in float
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+
+// Where the rows lie and what workgroup takes which.
+struct Rows {
+  uint64_t off[kMaxK + 1];     // device d's rows are [off[d], off[d + 1])
+  uint32_t first[kMaxK + 1];   // and its workgroups [first[d], first[d + 1])
+  float w[kMaxK];
+  uint64_t ld;                 // elements between rows of logits
+  uint32_t E, k, K, per;       // per: rows of one workgroup
+  uint32_t renormalise;
+};
+
+// What the workgroups leave for the sums over all rows.
+struct Parts {
+  float* prob;                 // [W][E] sums of probabilities
+  uint32_t* count;             // [W][E] choices
+  double* z;                   // [W] sums of lse^2
+  uint32_t* rows;              // [W] counted rows
+  double* balance;             // [finishing workgroups]
+  uint32_t* ticket;
+  uint32_t W;
+};
+
+struct RouteOut {
+  int32_t* idx;
+  float* gate;
+  float* lse;
+  int32_t* counts;
+  float* load;
+  float* share;
+  float* loss;
+};
+
+// ---- exchanges within a group of G lanes ------------------------------------------------------
+template <int kCtrl>
+__device__ inline uint32_t dpp(uint32_t x)
+{
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kCtrl, 0xF, 0xF, true);
+}
+
+// Combines x over the group; every lane ends with the same value, in the same
+// pattern of operations whatever the data.
+template <int G, class Op>
+__device__ inline float group_reduce(float x, Op op)
+{
+  auto f = [](uint32_t u) { return __uint_as_float(u); };
+  if constexpr (G >= 2) x = op(x, f(dpp<0xB1>(__float_as_uint(x))));    // lanes 1 apart
+  if constexpr (G >= 4) x = op(x, f(dpp<0x4E>(__float_as_uint(x))));    // 2 apart
+  if constexpr (G >= 8) x = op(x, f(dpp<0x141>(__float_as_uint(x))));   // the halves of 8
+  if constexpr (G >= 16) x = op(x, f(dpp<0x140>(__float_as_uint(x))));  // of 16
+  if constexpr (G >= 32) x = op(x, __shfl_xor(x, 16, 64));
+  if constexpr (G >= 64) x = op(x, __shfl_xor(x, 32, 64));
+  return x;
+}
+
+template <int G>
+__device__ inline float group_max(float x)
+{
+  return group_reduce<G>(x, [](float a, float b) { return __builtin_fmaxf(a, b); });
+}
+
+template <int G>
+__device__ inline float group_sum(float x)
+{
+  return group_reduce<G>(x, [](float a, float b) { return a + b; });
+}
+
+template <int G>
+__device__ inline uint32_t group_min(uint32_t x)
+{
+  auto f = [](float a, float b) {
+    const uint32_t u = __float_as_uint(a), v = __float_as_uint(b);
+    return __uint_as_float(u < v ? u : v);
+  };
+  return __float_as_uint(group_reduce<G>(__uint_as_float(x), f));
+}
+
+__device__ inline float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+
+// Orders LDS accesses of the lanes of a wave, which run in step: only the
+// compiler has to keep their order.
+__device__ inline void wave_sync()
+{
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// The device whose workgroups include w.
+__device__ inline uint32_t device_of(const Rows& r, uint32_t w)
+{
+  uint32_t lo = 0, hi = r.K;
+  while (hi - lo > 1) {
+    const uint32_t mid = (lo + hi) / 2;
+    if (r.first[mid] <= w) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+// Element i of a lane's V is expert 4 (G (i / 4) + lane) + i % 4: 16 bytes of
+// every lane side by side.
+template <int G>
+__device__ constexpr uint32_t expert_at(int i) { return (uint32_t)(4 * G * (i / 4) + i % 4); }
+
+template <class X, int G, int V>
+__device__ inline void load_row(float (&x)[V], const X* row, uint32_t l4, uint32_t E, bool on)
+{
+#pragma unroll
+  for (int j = 0; j < V / 4; ++j) {
+    const uint32_t e = expert_at<G>(4 * j) + l4;
+    const uint32_t k = on && e < E ? E - e : 0u;
+    const f4 v = load_once_f4(row + e, k, -__builtin_inff());
+#pragma unroll
+    for (int q = 0; q < 4; ++q) x[4 * j + q] = v[q];
+  }
+}
+
+// ---- the sums over all rows ---------------------------------------------------------------------
+// Experts [32 b, 32 b + 32): every slice of the threads adds a run of the
+// workgroups' results in order, then the slices are added in order.
+template <int NT>
+struct FinishLds {
+  static constexpr int kSlices = NT / (int)kFinishExperts;
+  uint32_t rows[kMaxK];
+  double scale[kMaxK];
+  uint32_t count[kMaxK][kFinishExperts];
+  double load[kSlices][kFinishExperts], prob[kSlices][kFinishExperts];
+  double z[NT / 64];
+};
+
+template <int NT>
+__device__ inline double finish_experts(const Rows& r, const Parts& s, const RouteOut& o, uint32_t b, FinishLds<NT>& m)
+{
+  constexpr uint32_t kSlices = FinishLds<NT>::kSlices;
+  const uint32_t tid = threadIdx.x;
+  for (uint32_t i = tid; i < kMaxK; i += NT) m.rows[i] = 0u;
+  for (uint32_t i = tid; i < kMaxK * kFinishExperts; i += NT) (&m.count[0][0])[i] = 0u;
+  __syncthreads();
+  for (uint32_t w = tid; w < s.W; w += NT) {
+    const uint32_t n = s.rows[w];
+    if (n) atomicAdd(&m.rows[device_of(r, w)], n);
+  }
+  __syncthreads();
+  if (tid < r.K) {
+    const uint32_t n = m.rows[tid];
+    m.scale[tid] = n ? (double)r.w[tid] / (double)n : 0.0;
+    if (b == 0) o.share[tid] = n ? 1.0f / (float)n : 0.0f;
+  }
+  __syncthreads();
+  const uint32_t le = tid % kFinishExperts, slice = tid / kFinishExperts, e = b * kFinishExperts + le;
+  double load = 0.0, prob = 0.0;
+  if (e < r.E) {
+    const uint32_t w0 = (uint32_t)((uint64_t)s.W * slice / kSlices), w1 = (uint32_t)((uint64_t)s.W * (slice + 1) / kSlices);
+    if (w0 < w1) {
+      uint32_t d = device_of(r, w0), run = 0;
+      for (uint32_t w = w0; w < w1; ++w) {
+        if (w >= r.first[d + 1]) {
+          if (run) atomicAdd(&m.count[d][le], run);
+          run = 0;
+          while (w >= r.first[d + 1]) ++d;
+        }
+        const uint32_t c = s.count[(uint64_t)w * r.E + e];
+        run += c;
+        load += m.scale[d] * (double)c;
+        prob += m.scale[d] * (double)s.prob[(uint64_t)w * r.E + e];
+      }
+      if (run) atomicAdd(&m.count[d][le], run);
+    }
+  }
+  m.load[slice][le] = load;
+  m.prob[slice][le] = prob;
+  double z = 0.0;
+  if (b == 0)
+    for (uint32_t w = tid; w < s.W; w += NT) z += m.scale[device_of(r, w)] * s.z[w];
+  z = wave_sum_f64(z);
+  if (lane_id() == 0) m.z[tid >> 6] = z;
+  __syncthreads();
+  for (uint32_t i = tid; i < r.K * kFinishExperts; i += NT) {
+    const uint32_t d = i / kFinishExperts, x = b * kFinishExperts + i % kFinishExperts;
+    if (x < r.E) o.counts[(uint64_t)d * r.E + x] = (int32_t)m.count[d][i % kFinishExperts];
+  }
+  double balance = 0.0;
+  if (tid < 64) {
+    load = prob = 0.0;
+    if (tid < kFinishExperts && e < r.E) {
+      for (uint32_t q = 0; q < kSlices; ++q) {
+        load += m.load[q][tid];
+        prob += m.prob[q][tid];
+      }
+      load /= (double)r.k;
+      o.load[e] = (float)load;
+    }
+    balance = wave_sum_f64(load * prob * (double)r.E);
+  }
+  if (b == 0 && tid == 0) {
+    z = 0.0;
+    for (int q = 0; q < NT / 64; ++q) z += m.z[q];
+    o.loss[1] = (float)z;
+  }
+  __syncthreads();
+  return balance;        // in the first wave
+}
+
+__global__ __launch_bounds__(kFinishBlock) void k_route_finish(Rows r, Parts s, RouteOut o)
+{
+  __shared__ FinishLds<kFinishBlock> m;
+  const double balance = finish_experts<kFinishBlock>(r, s, o, blockIdx.x, m);
+  if (threadIdx.x == 0) put(&s.balance[blockIdx.x], balance);
+  if (!block_is_last(s.ticket, 1u, gridDim.x)) return;
+  if (threadIdx.x) return;
+  double sum = 0.0;
+  for (uint32_t b = 0; b < gridDim.x; ++b) sum += get(&s.balance[b]);
+  o.loss[0] = (float)sum;
+}
+
+// ---- forward ------------------------------------------------------------------------------------
+template <int G, int V>
+struct RouteLds {
+  static constexpr int kGroups = kBlock / G;
+  uint32_t count[G * V];
+  float prob[kGroups * G * V];
+  uint32_t idx[kGroups][kMaxChoices];
+  float ex[kGroups][kMaxChoices];
+  double z[kGroups];
+  uint32_t rows[kGroups];
+};
+
+template <class X, int G, int V, bool kOne>
+__global__ __launch_bounds__(kBlock) void k_route(Rows r, const X* logits, const uint8_t* valid, RouteOut o, Parts s)
+{
+  constexpr int kGroups = kBlock / G;
+  __shared__ RouteLds<G, V> m;
+  const uint32_t tid = threadIdx.x, l = tid % G, l4 = 4 * l, group = tid / G;
+  const uint32_t d = device_of(r, blockIdx.x);
+  const uint64_t row0 = r.off[d] + (uint64_t)(blockIdx.x - r.first[d]) * r.per;
+  const uint64_t row1 = row0 + r.per < r.off[d + 1] ? row0 + r.per : r.off[d + 1];
+  for (uint32_t e = tid; e < G * V; e += kBlock) m.count[e] = 0u;
+  if (blockIdx.x == 0 && tid == 0) *s.ticket = 0u;
+  __syncthreads();
+  float acc[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) acc[i] = 0.0f;
+  double z = 0.0;
+  uint32_t rows = 0;
+  for (uint64_t base = row0; base < row1; base += kGroups) {
+    const uint64_t row = base + group;
+    const bool on = row < row1 && (!valid || gptr(valid)[row]);
+    float x[V];
+    load_row<X, G, V>(x, logits + row * r.ld, l4, r.E, on);
+    float mx = x[0];
+#pragma unroll
+    for (int i = 1; i < V; ++i) mx = __builtin_fmaxf(mx, x[i]);
+    mx = group_max<G>(mx);
+    // a row without a value above -inf sums to zero: it routes nowhere and is not counted
+    const float mid = mx == -__builtin_inff() ? 0.0f : mx;
+    float p[V], sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      p[i] = exp_of(x[i] - mid);
+      sum += p[i];
+    }
+    sum = group_sum<G>(sum);
+    const bool counted = !(sum == 0.0f);
+    const float inv = counted ? 1.0f / sum : 0.0f;
+    const float lse = counted ? mid + __builtin_amdgcn_logf(sum) * kLn2 : 0.0f;
+#pragma unroll
+    for (int i = 0; i < V; ++i) acc[i] += p[i] * inv;
+    z += (double)lse * (double)lse;
+    rows += counted ? 1u : 0u;
+    float chosen = 0.0f;
+    for (uint32_t c = 0; c < r.k; ++c) {
+      float top = mx;
+      if (c) {
+        top = x[0];
+#pragma unroll
+        for (int i = 1; i < V; ++i) top = __builtin_fmaxf(top, x[i]);
+        top = group_max<G>(top);
+      }
+      uint32_t at = ~0u;
+#pragma unroll
+      for (int i = V - 1; i >= 0; --i) at = x[i] == top ? expert_at<G>(i) + l4 : at;
+      at = group_min<G>(at);
+      const bool some = top > -__builtin_inff() && at != ~0u;
+#pragma unroll
+      for (int i = 0; i < V; ++i) x[i] = expert_at<G>(i) + l4 == at ? -__builtin_inff() : x[i];
+      const float ex = some ? exp_of(top - mid) : 0.0f;
+      chosen += ex;
+      if (l == 0) {
+        m.idx[group][c] = some ? at : ~0u;
+        m.ex[group][c] = ex;
+        if (some) atomicAdd(&m.count[at], 1u);
+      }
+    }
+    float to_gate = inv;
+    if (r.renormalise && sum < __builtin_inff()) to_gate = chosen > 0.0f ? 1.0f / chosen : 0.0f;   // else NaN, as inv is
+    wave_sync();
+    if (row < row1) {
+      for (uint32_t c = l; c < r.k; c += G) {
+        o.idx[row * r.k + c] = (int32_t)m.idx[group][c];
+        o.gate[row * r.k + c] = m.ex[group][c] * to_gate;
+      }
+      if (l == 0) o.lse[row] = lse;
+    }
+    wave_sync();
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i) m.prob[group * (G * V) + expert_at<G>(i) + l4] = acc[i];
+  if (l == 0) {
+    m.z[group] = z;
+    m.rows[group] = rows;
+  }
+  __syncthreads();
+  for (uint32_t e = tid; e < r.E; e += kBlock) {
+    float sum = 0.0f;
+    for (int g = 0; g < kGroups; ++g) sum += m.prob[g * (G * V) + e];
+    s.prob[(uint64_t)blockIdx.x * r.E + e] = sum;
+    s.count[(uint64_t)blockIdx.x * r.E + e] = m.count[e];
+  }
+  if (tid == 0) {
+    double sum = 0.0;
+    uint32_t n = 0;
+    for (int g = 0; g < kGroups; ++g) {
+      sum += m.z[g];
+      n += m.rows[g];
+    }
+    s.z[blockIdx.x] = sum;
+    s.rows[blockIdx.x] = n;
+  }
+  if constexpr (kOne) {        // the only workgroup: no second launch
+    __shared__ FinishLds<kBlock> f;
+    __syncthreads();
+    double balance = 0.0;
+    for (uint32_t b = 0; b * kFinishExperts < r.E; ++b) balance += finish_experts<kBlock>(r, s, o, b, f);
+    if (tid == 0) o.loss[0] = (float)balance;
+  }
+}
+
+// ---- backward -----------------------------------------------------------------------------------
+template <class X, int G, int V>
+__global__ __launch_bounds__(kBlock) void k_route_back(Rows r, const X* logits, RouteOut o, const float* dgate,
+                                                       const float* dloss, X* dlogits, uint64_t ld_out)
+{
+  constexpr int kGroups = kBlock / G;
+  __shared__ float s_part[kGroups][G * V];      // the gates' part of the group's row, zero elsewhere
+  const uint32_t tid = threadIdx.x, l = tid % G, l4 = 4 * l, group = tid / G;
+  const uint32_t d = device_of(r, blockIdx.x);
+  const uint64_t row0 = r.off[d] + (uint64_t)(blockIdx.x - r.first[d]) * r.per;
+  const uint64_t row1 = row0 + r.per < r.off[d + 1] ? row0 + r.per : r.off[d + 1];
+  const float scale = r.w[d] * o.share[d];
+  const float a = dloss ? dloss[0] * scale * (float)r.E : 0.0f, b2 = dloss ? 2.0f * dloss[1] * scale : 0.0f;
+  float load[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const uint32_t e = expert_at<G>(i) + l4;
+    load[i] = e < r.E ? o.load[e] : 0.0f;
+    s_part[group][e] = 0.0f;
+  }
+  wave_sync();
+  for (uint64_t base = row0; base < row1; base += kGroups) {
+    const uint64_t row = base + group;
+    const bool in = row < row1;
+    const float lse = in ? o.lse[row] : 0.0f;
+    const bool on = in && (o.idx[row * r.k] >= 0 || lse != lse);   // routed, or NaN
+    float x[V];
+    load_row<X, G, V>(x, logits + row * r.ld, l4, r.E, on);
+    float sum = 0.0f, mean = 0.0f;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      x[i] = exp_of(x[i] - lse);
+      sum += x[i];
+      mean += x[i] * load[i];
+    }
+    sum = group_sum<G>(sum);
+    mean = group_sum<G>(mean);
+    float part = 0.0f;
+    if (dgate) {
+      for (uint32_t c = l; c < r.k; c += G)
+        if (on) part += o.gate[row * r.k + c] * dgate[row * r.k + c];
+      part = group_sum<G>(part);
+      for (uint32_t c = l; c < r.k; c += G) {
+        const int32_t e = on ? o.idx[row * r.k + c] : -1;
+        if (e >= 0) s_part[group][e] = o.gate[row * r.k + c] * (dgate[row * r.k + c] - (r.renormalise ? part : 0.0f));
+      }
+      if (r.renormalise) part = 0.0f;
+      wave_sync();
+    }
+    const float inv = on ? 1.0f / sum : 0.0f;   // lse is rounded: its error cancels
+    const float all = b2 * lse - part - a * (mean * inv);
+#pragma unroll
+    for (int j = 0; j < V / 4; ++j) {
+      const uint32_t e = expert_at<G>(4 * j) + l4;
+      f4 dx;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) dx[q] = on ? x[4 * j + q] * inv * (a * load[4 * j + q] + all) : 0.0f;
+      if (dgate) {
+        const f4 g = *reinterpret_cast<const f4*>(&s_part[group][e]);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) dx[q] += g[q];
+      }
+      if (in && e < r.E) store_f4(dlogits + row * ld_out + e, dx, r.E - e);
+    }
+    if (dgate) {
+      wave_sync();
+      for (uint32_t c = l; c < r.k; c += G) {
+        const int32_t e = on ? o.idx[row * r.k + c] : -1;
+        if (e >= 0) s_part[group][e] = 0.0f;
+      }
+      wave_sync();
+    }
+  }
+}
+
+// ---- host side ------------------------------------------------------------------------------------
+// Lanes per row and elements per lane for E experts.
+template <class F>
+void with_shape(uint32_t E, F f)
+{
+  if (E <= 16) f(std::integral_constant<int, 4>(), std::integral_constant<int, 4>());
+  else if (E <= 32) f(std::integral_constant<int, 8>(), std::integral_constant<int, 4>());
+  else if (E <= 64) f(std::integral_constant<int, 16>(), std::integral_constant<int, 4>());
+  else if (E <= 128) f(std::integral_constant<int, 16>(), std::integral_constant<int, 8>());
+  else if (E <= 256) f(std::integral_constant<int, 16>(), std::integral_constant<int, 16>());
+  else if (E <= 512) f(std::integral_constant<int, 32>(), std::integral_constant<int, 16>());
+  else f(std::integral_constant<int, 64>(), std::integral_constant<int, 16>());
+}
+
+uint32_t rows_per_round(uint32_t E)
+{
+  uint32_t n = 0;
+  with_shape(E, [&](auto g, auto) { n = kBlock / g; });
+  return n;
+}
+
+// Rows of one workgroup, so that about kRouteBlocks workgroups share T rows.
+uint32_t rows_per_block(uint64_t T, uint32_t E)
+{
+  const uint32_t round = rows_per_round(E);
+  uint64_t rounds = div_up(T, (uint64_t)round * kRouteBlocks);
+  if (rounds < 1) rounds = 1;
+  if (rounds > kMaxRounds) rounds = kMaxRounds;
+  return round * (uint32_t)rounds;
+}
+
+scadles_status check_router(const scadles_router* q)
+{
+  if (!q) return fail(SCADLES_EINVAL, "router is NULL");
+  if (q->tokens > 0x7FFFFFFFull) return fail(SCADLES_EINVAL, "more than 2^31 - 1 tokens");
+  if (!q->experts || q->experts > kMaxExperts) return fail(SCADLES_EINVAL, "experts = %u is outside [1, %u]", q->experts, kMaxExperts);
+  if (!q->k || q->k > q->experts || q->k > kMaxChoices)
+    return fail(SCADLES_EINVAL, "k = %u is outside [1, min(experts, %u)]", q->k, kMaxChoices);
+  if (!q->devices || q->devices > kMaxK) return fail(SCADLES_EINVAL, "devices = %u is outside [1, %d]", q->devices, kMaxK);
+  if (q->logits_type != SCADLES_F32 && q->logits_type != SCADLES_BF16)
+    return fail(SCADLES_EINVAL, "unknown logits_type %d", q->logits_type);
+  if (q->ld < q->experts) return fail(SCADLES_EINVAL, "ld is smaller than experts");
+  if (!q->tok_off) return fail(SCADLES_EINVAL, "tok_off is NULL");
+  if (q->tok_off[0] != 0 || q->tok_off[q->devices] != q->tokens) return fail(SCADLES_EINVAL, "tok_off must run from 0 to tokens");
+  for (uint32_t d = 0; d < q->devices; ++d)
+    if (q->tok_off[d + 1] < q->tok_off[d]) return fail(SCADLES_EINVAL, "tok_off must not decrease");
+  if (!q->weights) return fail(SCADLES_EINVAL, "weights is NULL");
+  for (uint32_t d = 0; d < q->devices; ++d)
+    if (!std::isfinite(q->weights[d]) || q->weights[d] < 0.0f) return fail(SCADLES_EINVAL, "weight %u is negative or not finite", d);
+  return SCADLES_OK;
+}
+
+// What the kernels need to know of the rows; returns the workgroups.
+uint32_t make_rows(const scadles_router* q, Rows& r)
+{
+  std::memset(&r, 0, sizeof(r));
+  r.per = rows_per_block(q->tokens, q->experts);
+  r.E = q->experts;
+  r.k = q->k;
+  r.K = q->devices;
+  r.ld = q->ld;
+  r.renormalise = q->renormalise ? 1u : 0u;
+  uint64_t w = 0;
+  for (uint32_t d = 0; d < r.K; ++d) {
+    r.off[d] = q->tok_off[d];
+    r.first[d] = (uint32_t)w;
+    r.w[d] = q->weights[d];
+    w += div_up(q->tok_off[d + 1] - q->tok_off[d], r.per);
+  }
+  r.off[r.K] = q->tokens;
+  r.first[r.K] = (uint32_t)w;
+  return (uint32_t)w;
+}
+
+uint64_t take(uint64_t& at, uint64_t bytes)
+{
+  const uint64_t here = at;
+  at = div_up(at + bytes, 256) * 256;
+  return here;
+}
+
+// The workspace's pieces for W workgroups; returns its size.
+uint64_t lay_out(uint32_t W, uint32_t E, char* ws, Parts& s)
+{
+  uint64_t at = 0;
+  const uint64_t cells = (uint64_t)W * E * 4;
+  s.ticket = reinterpret_cast<uint32_t*>(ws + take(at, 256));
+  s.balance = reinterpret_cast<double*>(ws + take(at, kMaxExperts / kFinishExperts * 8));
+  s.z = reinterpret_cast<double*>(ws + take(at, (uint64_t)W * 8));
+  s.rows = reinterpret_cast<uint32_t*>(ws + take(at, (uint64_t)W * 4));
+  s.prob = reinterpret_cast<float*>(ws + take(at, cells));
+  s.count = reinterpret_cast<uint32_t*>(ws + take(at, cells));
+  s.W = W;
+  return at;
+}
+
+// A call without rows: nothing is counted.
+__global__ void k_route_empty(Rows r, RouteOut o)
+{
+  for (uint32_t i = threadIdx.x; i < r.K * r.E; i += blockDim.x) o.counts[i] = 0;
+  for (uint32_t i = threadIdx.x; i < r.E; i += blockDim.x) o.load[i] = 0.0f;
+  for (uint32_t i = threadIdx.x; i < r.K; i += blockDim.x) o.share[i] = 0.0f;
+  if (threadIdx.x < 2) o.loss[threadIdx.x] = 0.0f;
+}
+
+scadles_status check_out(const scadles_router* q, const scadles_router_out* o)
+{
+  if (!o) return fail(SCADLES_EINVAL, "out is NULL");
+  if (q->tokens && (!o->idx || !o->gate || !o->lse)) return fail(SCADLES_EINVAL, "idx, gate and lse must not be NULL");
+  if (!o->counts || !o->load || !o->share || !o->loss) return fail(SCADLES_EINVAL, "counts, load, share and loss must not be NULL");
+  for (const void* p : {(const void*)o->idx, (const void*)o->gate, (const void*)o->lse, (const void*)o->counts, (const void*)o->load,
+                        (const void*)o->share, (const void*)o->loss})
+    if (!is_aligned(p, 4)) return fail(SCADLES_EINVAL, "an output is not 4-byte aligned");
+  return SCADLES_OK;
+}
+
+// Elements from the first to the last of T rows.
+uint64_t span_bytes(const scadles_router* q, uint64_t ld)
+{
+  return q->tokens ? ((q->tokens - 1) * ld + q->experts) * (q->logits_type == SCADLES_BF16 ? 2 : 4) : 0;
+}
+
+template <class X>
+hipError_t launch_route(const Rows& r, const void* logits, const uint8_t* valid, const RouteOut& o, const Parts& s, hipStream_t st)
+{
+  with_shape(r.E, [&](auto g, auto v) {
+    if (s.W == 1) k_route<X, g, v, true><<<1, kBlock, 0, st>>>(r, (const X*)logits, valid, o, s);
+    else k_route<X, g, v, false><<<s.W, kBlock, 0, st>>>(r, (const X*)logits, valid, o, s);
+  });
+  if (s.W > 1) k_route_finish<<<(uint32_t)div_up(r.E, kFinishExperts), kFinishBlock, 0, st>>>(r, s, o);
+  return hipGetLastError();
+}
+
+template <class X>
+hipError_t launch_back(const Rows& r, uint32_t W, const void* logits, const RouteOut& o, const float* dgate, const float* dloss,
+                       void* dlogits, uint64_t ld_out, hipStream_t st)
+{
+  with_shape(r.E, [&](auto g, auto v) {
+    k_route_back<X, g, v><<<W, kBlock, 0, st>>>(r, (const X*)logits, o, dgate, dloss, (X*)dlogits, ld_out);
+  });
+  return hipGetLastError();
+}
+
+RouteOut outputs(const scadles_router_out* o)
+{
+  return {o->idx, o->gate, o->lse, o->counts, o->load, o->share, o->loss};
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t scadles_router_workspace_bytes(uint64_t tokens, uint32_t experts, uint32_t devices)
+{
+  if (tokens > 0x7FFFFFFFull || !experts || experts > kMaxExperts || !devices || devices > kMaxK) return 0;
+  // the most workgroups of any call of so many rows or fewer; every device's last one may be partly filled
+  const uint64_t round = rows_per_round(experts);
+  uint64_t W = tokens / round < kRouteBlocks ? tokens / round : kRouteBlocks;
+  if (tokens / (round * kMaxRounds) > W) W = tokens / (round * kMaxRounds);
+  W += devices;
+  Parts s;
+  return (size_t)lay_out((uint32_t)W, experts, nullptr, s);
+}
+
+scadles_status scadles_router_forward(const scadles_router* router, const void* logits, const uint8_t* valid,
+                                      const scadles_router_out* out, void* ws, size_t ws_bytes, void* stream)
+{
+  if (scadles_status st = check_router(router)) return st;
+  double total = 0.0;
+  for (uint32_t d = 0; d < router->devices; ++d) total += (double)router->weights[d];
+  if (std::fabs(total - 1.0) > (double)router->devices * std::ldexp(1.0, -23))
+    return fail(SCADLES_EINVAL, "weights sum to %.17g, not 1 (Eqn 4a)", total);
+  if (scadles_status st = check_out(router, out)) return st;
+  const uint64_t esize = router->logits_type == SCADLES_BF16 ? 2 : 4, T = router->tokens;
+  if (T && !logits) return fail(SCADLES_EINVAL, "logits is NULL");
+  if (!is_aligned(logits, esize)) return fail(SCADLES_EINVAL, "logits is not aligned to its elements");
+  Rows r;
+  Parts s;
+  const uint32_t W = make_rows(router, r);
+  const uint64_t need = lay_out(W, router->experts, static_cast<char*>(ws), s);
+  if (!ws || !is_aligned(ws, 256)) return fail(SCADLES_EWORKSPACE, "workspace must be 256-byte aligned and not NULL");
+  if (ws_bytes < need) return fail(SCADLES_EWORKSPACE, "workspace has %zu bytes, needs %zu", ws_bytes, (size_t)need);
+  const void* outs[7] = {out->idx, out->gate, out->lse, out->counts, out->load, out->share, out->loss};
+  const uint64_t sizes[7] = {T * router->k * 4, T * router->k * 4, T * 4, (uint64_t)router->devices * router->experts * 4,
+                             (uint64_t)router->experts * 4, (uint64_t)router->devices * 4, 8};
+  for (int x = 0; x < 7; ++x) {
+    if (bytes_overlap(outs[x], sizes[x], logits, span_bytes(router, router->ld)) || bytes_overlap(outs[x], sizes[x], valid, T) ||
+        bytes_overlap(outs[x], sizes[x], ws, need))
+      return fail(SCADLES_EINVAL, "an output overlaps an input or the workspace");
+    for (int y = 0; y < x; ++y)
+      if (bytes_overlap(outs[x], sizes[x], outs[y], sizes[y])) return fail(SCADLES_EINVAL, "two outputs overlap");
+  }
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const RouteOut o = outputs(out);
+  if (W == 0) {
+    k_route_empty<<<1, kBlock, 0, st>>>(r, o);
+    return launch_status(hipGetLastError(), "router forward");
+  }
+  return launch_status(esize == 2 ? launch_route<uint16_t>(r, logits, valid, o, s, st) : launch_route<float>(r, logits, valid, o, s, st),
+                       "router forward");
+}
+
+scadles_status scadles_router_backward(const scadles_router* router, const void* logits, const scadles_router_out* out,
+                                       const float* dgate, const float* dloss, void* dlogits, uint64_t ld_out, void* stream)
+{
+  if (scadles_status st = check_router(router)) return st;
+  if (scadles_status st = check_out(router, out)) return st;
+  const uint64_t esize = router->logits_type == SCADLES_BF16 ? 2 : 4, T = router->tokens;
+  if (T && (!logits || !dlogits)) return fail(SCADLES_EINVAL, "logits and dlogits must not be NULL");
+  if (!is_aligned(logits, esize) || !is_aligned(dlogits, esize))
+    return fail(SCADLES_EINVAL, "logits or dlogits is not aligned to its elements");
+  if (!is_aligned(dgate, 4) || !is_aligned(dloss, 4)) return fail(SCADLES_EINVAL, "dgate or dloss is not 4-byte aligned");
+  if (ld_out < router->experts) return fail(SCADLES_EINVAL, "ld_out is smaller than experts");
+  const uint64_t bytes = span_bytes(router, ld_out);
+  const void* ins[8] = {logits, out->idx, out->gate, out->lse, out->load, out->share, dgate, dloss};
+  const uint64_t sizes[8] = {span_bytes(router, router->ld), T * router->k * 4, T * router->k * 4, T * 4,
+                             (uint64_t)router->experts * 4, (uint64_t)router->devices * 4, T * router->k * 4, 8};
+  for (int x = 0; x < 8; ++x)
+    if (bytes_overlap(dlogits, bytes, ins[x], sizes[x])) return fail(SCADLES_EINVAL, "dlogits overlaps an input");
+  Rows r;
+  const uint32_t W = make_rows(router, r);
+  if (W == 0) return SCADLES_OK;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const RouteOut o = outputs(out);
+  return launch_status(esize == 2 ? launch_back<uint16_t>(r, W, logits, o, dgate, dloss, dlogits, ld_out, st)
+                                  : launch_back<float>(r, W, logits, o, dgate, dloss, dlogits, ld_out, st),
+                       "router backward");
+}
+
+}  // extern "C"
