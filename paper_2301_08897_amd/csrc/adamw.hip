@@ -41,7 +41,9 @@ namespace {
 
 constexpr uint32_t kMoment = SCADLES_MOMENT_BLOCK;
 constexpr uint32_t kChunk = 2048;          // elements of one workgroup
-constexpr uint32_t kNormBlocks = 2048;     // workgroups of the norm (at most)
+// The norm's workgroups, at most: one per compute unit. Every workgroup counts
+// itself in at one address when it is done, which takes 10 ns each.
+constexpr uint32_t kNormBlocks = 256, kNormBlock = 1024, kNormWaves = kNormBlock / 64;
 constexpr uint32_t kPutTensors = 40;       // tensors of one launch's arguments
 constexpr uint32_t kMagic = 0x5C4D0001u;
 constexpr uint32_t kSpanM = 127, kSpanV = 255;
@@ -344,26 +346,45 @@ __global__ __launch_bounds__(kBlock) void k_adamw_moments(const Chunk* chunks, f
 // Squares and sums in double. Workgroups sum their chunks in order, the last
 // one to finish sums the workgroups' results in order, so the norm does not
 // depend on the order in which they run.
-template <class G>
-__global__ __launch_bounds__(kBlock) void k_grad_norm(const Chunk* chunks, uint32_t count, Head* head, double max_norm,
-                                                      float* out)
+__device__ inline double norm_block_sum(double v, double* lds)
 {
-  __shared__ double s_sum[kWaves];
+  v = wave_sum_f64(v);
+  if (lane_id() == 0) lds[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = lane_id() < kNormWaves ? lds[lane_id()] : 0.0;
+  return wave_sum_f64(v);
+}
+
+template <class G>
+__global__ __launch_bounds__(kNormBlock) void k_grad_norm(const Chunk* chunks, uint32_t count, Head* head, double max_norm,
+                                                          float* out)
+{
+  __shared__ double s_sum[2][kNormWaves];
+  constexpr int kLoads = kChunk / 256;       // a wave takes a chunk, all of its loads at once
   double sum = 0.0;
-  for (uint32_t i = blockIdx.x; i < count; i += gridDim.x) {
-    const Chunk c = chunks[i];
-    for (uint32_t e = threadIdx.x * 4; e < c.n; e += kBlock * 4) {
-      const f4 g = load_once_f4((const G*)c.g + e, c.n - e);
+  for (uint32_t i = blockIdx.x * kNormWaves + wave_id(); i < count; i += gridDim.x * kNormWaves) {
+    const G* g = (const G*)chunks[i].g + lane_id() * 4;
+    const uint32_t n = chunks[i].n;
+    f4 x[kLoads];
+    if (n == kChunk) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) sum = __builtin_fma((double)g[q], (double)g[q], sum);
+      for (int j = 0; j < kLoads; ++j) x[j] = load_once_f4(g + j * 256, 4);
+    } else {
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) {
+        const uint32_t e = j * 256 + lane_id() * 4;
+        x[j] = load_once_f4(g + j * 256, e < n ? n - e : 0u);
+      }
     }
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) sum = __builtin_fma((double)x[j][q], (double)x[j][q], sum);
   }
-  sum = block_sum_f64(sum, s_sum);
+  sum = norm_block_sum(sum, s_sum[0]);
   if (threadIdx.x == 0) put(&head->part[blockIdx.x], sum);
   if (!block_is_last(&head->ticket, 1u, gridDim.x)) return;
-  sum = 0.0;
-  for (uint32_t i = threadIdx.x; i < gridDim.x; i += kBlock) sum += get(&head->part[i]);
-  sum = block_sum_f64(sum, s_sum);
+  sum = norm_block_sum(threadIdx.x < gridDim.x ? get(&head->part[threadIdx.x]) : 0.0, s_sum[1]);
   if (threadIdx.x) return;
   put(&head->ticket, 0u);
   const double norm = sqrt(sum);
@@ -489,10 +510,11 @@ scadles_status scadles_grad_norm(const scadles_adamw_plan* plan, double max_norm
   if (!clip || !is_aligned(clip, 4)) return fail(SCADLES_EINVAL, "clip must be 4-byte aligned and not NULL");
   hipStream_t s = static_cast<hipStream_t>(stream);
   const uint32_t count = (uint32_t)plan->chunks;
-  const uint32_t grid = count < 1 ? 1 : count < kNormBlocks ? count : kNormBlocks;
+  const uint64_t blocks = div_up(count, kNormWaves);
+  const uint32_t grid = blocks < 1 ? 1 : blocks < kNormBlocks ? (uint32_t)blocks : kNormBlocks;
   Head* head = static_cast<Head*>(plan->table);
-  if (plan->grad_type == SCADLES_BF16) k_grad_norm<uint16_t><<<grid, kBlock, 0, s>>>(chunks_of(plan), count, head, max_norm, clip);
-  else k_grad_norm<float><<<grid, kBlock, 0, s>>>(chunks_of(plan), count, head, max_norm, clip);
+  if (plan->grad_type == SCADLES_BF16) k_grad_norm<uint16_t><<<grid, kNormBlock, 0, s>>>(chunks_of(plan), count, head, max_norm, clip);
+  else k_grad_norm<float><<<grid, kNormBlock, 0, s>>>(chunks_of(plan), count, head, max_norm, clip);
   return launch_status(hipGetLastError(), "gradient norm");
 }
 

@@ -28,10 +28,11 @@ namespace {
 
 constexpr uint32_t kMaxChoices = SCADLES_ROUTER_MAX_K;
 constexpr uint32_t kMaxExperts = SCADLES_ROUTER_MAX_EXPERTS;
-constexpr uint32_t kFinishExperts = 32;    // experts of one workgroup of k_route_finish
-constexpr int kFinishBlock = 1024;
-constexpr uint32_t kRouteBlocks = 1024;    // workgroups aimed at when rounds are chosen,
-constexpr uint32_t kMaxRounds = 256;       // and the most rounds of one: it sums probabilities in float
+constexpr uint32_t kFinishExperts = 8;     // experts of one workgroup of k_route_finish
+constexpr int kFinishBlock = 512;
+constexpr uint32_t kFewFrom = 3;           // choices from which they are made by a threshold
+constexpr uint32_t kRouteBlocks = 1024;    // workgroups, at most, unless they would take
+constexpr uint32_t kMaxRounds = 256;       // more rounds each than this: they sum probabilities in float
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 // Where the rows lie and what workgroup takes which.
@@ -45,9 +46,13 @@ struct Rows {
 };
 
 // What the workgroups leave for the sums over all rows.
+struct Cell {
+  uint32_t count;              // choices of an expert
+  float prob;                  // and the sum of its probabilities
+};
+
 struct Parts {
-  float* prob;                 // [W][E] sums of probabilities
-  uint32_t* count;             // [W][E] choices
+  Cell* cell;                  // [W][E]
   double* z;                   // [W] sums of lse^2
   uint32_t* rows;              // [W] counted rows
   double* balance;             // [finishing workgroups]
@@ -120,22 +125,37 @@ __device__ inline void wave_sync()
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// The device whose workgroups include w.
-__device__ inline uint32_t device_of(const Rows& r, uint32_t w)
+// The device whose workgroups include w, and the rows of that workgroup. Every
+// lane loads a device's bounds, so that the arguments are waited for once.
+struct Share {
+  uint32_t d;
+  uint64_t row0, row1;
+};
+
+__device__ inline uint64_t lane_value(uint64_t x, uint32_t l)
 {
-  uint32_t lo = 0, hi = r.K;
-  while (hi - lo > 1) {
-    const uint32_t mid = (lo + hi) / 2;
-    if (r.first[mid] <= w) lo = mid;
-    else hi = mid;
-  }
-  return lo;
+  return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), l) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)x, l);
+}
+
+__device__ inline Share share_of(const Rows& r, uint32_t w)
+{
+  const uint32_t l = lane_id(), dl = l < r.K ? l : r.K - 1;
+  const uint32_t first = r.first[dl], next = r.first[dl + 1];
+  const uint64_t begin = r.off[dl], end = r.off[dl + 1];
+  Share s;
+  s.d = (uint32_t)__builtin_popcountll(__ballot(l < r.K && next <= w));    // devices that end before w
+  s.row0 = lane_value(begin, s.d) + (uint64_t)(w - (uint32_t)__builtin_amdgcn_readlane((int)first, s.d)) * r.per;
+  const uint64_t stop = lane_value(end, s.d);
+  s.row1 = s.row0 + r.per < stop ? s.row0 + r.per : stop;
+  return s;
 }
 
 // Element i of a lane's V is expert 4 (G (i / 4) + lane) + i % 4: 16 bytes of
 // every lane side by side.
 template <int G>
 __device__ constexpr uint32_t expert_at(int i) { return (uint32_t)(4 * G * (i / 4) + i % 4); }
+template <int G>
+__device__ inline uint32_t expert_of(uint32_t i, uint32_t l4) { return (i >> 2) * (4 * G) + (i & 3u) + l4; }
 
 template <class X, int G, int V>
 __device__ inline void load_row(float (&x)[V], const X* row, uint32_t l4, uint32_t E, bool on)
@@ -151,101 +171,155 @@ __device__ inline void load_row(float (&x)[V], const X* row, uint32_t l4, uint32
 }
 
 // ---- the sums over all rows ---------------------------------------------------------------------
-// Experts [32 b, 32 b + 32): every slice of the threads adds a run of the
-// workgroups' results in order, then the slices are added in order.
-template <int NT>
+// Experts [8 b, 8 b + 8): every slice of 8 threads adds a run of the
+// workgroups' results in order, kAhead loaded at once; then the slices are added
+// in a fixed pattern.
 struct FinishLds {
-  static constexpr int kSlices = NT / (int)kFinishExperts;
+  static constexpr int NT = kFinishBlock;
+  uint32_t first[kMaxK + 1];
   uint32_t rows[kMaxK];
   double scale[kMaxK];
   uint32_t count[kMaxK][kFinishExperts];
-  double load[kSlices][kFinishExperts], prob[kSlices][kFinishExperts];
+  double load[NT / 64][kFinishExperts], prob[NT / 64][kFinishExperts];
   double z[NT / 64];
 };
 
-template <int NT>
-__device__ inline double finish_experts(const Rows& r, const Parts& s, const RouteOut& o, uint32_t b, FinishLds<NT>& m)
+// The device whose workgroups include w, from the table in LDS.
+__device__ inline uint32_t device_in(const uint32_t* first, uint32_t K, uint32_t w)
 {
-  constexpr uint32_t kSlices = FinishLds<NT>::kSlices;
-  const uint32_t tid = threadIdx.x;
-  for (uint32_t i = tid; i < kMaxK; i += NT) m.rows[i] = 0u;
-  for (uint32_t i = tid; i < kMaxK * kFinishExperts; i += NT) (&m.count[0][0])[i] = 0u;
-  __syncthreads();
-  for (uint32_t w = tid; w < s.W; w += NT) {
-    const uint32_t n = s.rows[w];
-    if (n) atomicAdd(&m.rows[device_of(r, w)], n);
+  uint32_t lo = 0, hi = K;
+  while (hi - lo > 1) {
+    const uint32_t mid = (lo + hi) / 2;
+    if (first[mid] <= w) lo = mid;
+    else hi = mid;
   }
-  __syncthreads();
-  if (tid < r.K) {
-    const uint32_t n = m.rows[tid];
-    m.scale[tid] = n ? (double)r.w[tid] / (double)n : 0.0;
-    if (b == 0) o.share[tid] = n ? 1.0f / (float)n : 0.0f;
-  }
-  __syncthreads();
-  const uint32_t le = tid % kFinishExperts, slice = tid / kFinishExperts, e = b * kFinishExperts + le;
-  double load = 0.0, prob = 0.0;
-  if (e < r.E) {
-    const uint32_t w0 = (uint32_t)((uint64_t)s.W * slice / kSlices), w1 = (uint32_t)((uint64_t)s.W * (slice + 1) / kSlices);
-    if (w0 < w1) {
-      uint32_t d = device_of(r, w0), run = 0;
-      for (uint32_t w = w0; w < w1; ++w) {
-        if (w >= r.first[d + 1]) {
-          if (run) atomicAdd(&m.count[d][le], run);
-          run = 0;
-          while (w >= r.first[d + 1]) ++d;
-        }
-        const uint32_t c = s.count[(uint64_t)w * r.E + e];
-        run += c;
-        load += m.scale[d] * (double)c;
-        prob += m.scale[d] * (double)s.prob[(uint64_t)w * r.E + e];
-      }
-      if (run) atomicAdd(&m.count[d][le], run);
-    }
-  }
-  m.load[slice][le] = load;
-  m.prob[slice][le] = prob;
-  double z = 0.0;
-  if (b == 0)
-    for (uint32_t w = tid; w < s.W; w += NT) z += m.scale[device_of(r, w)] * s.z[w];
-  z = wave_sum_f64(z);
-  if (lane_id() == 0) m.z[tid >> 6] = z;
-  __syncthreads();
-  for (uint32_t i = tid; i < r.K * kFinishExperts; i += NT) {
-    const uint32_t d = i / kFinishExperts, x = b * kFinishExperts + i % kFinishExperts;
-    if (x < r.E) o.counts[(uint64_t)d * r.E + x] = (int32_t)m.count[d][i % kFinishExperts];
-  }
-  double balance = 0.0;
-  if (tid < 64) {
-    load = prob = 0.0;
-    if (tid < kFinishExperts && e < r.E) {
-      for (uint32_t q = 0; q < kSlices; ++q) {
-        load += m.load[q][tid];
-        prob += m.prob[q][tid];
-      }
-      load /= (double)r.k;
-      o.load[e] = (float)load;
-    }
-    balance = wave_sum_f64(load * prob * (double)r.E);
-  }
-  if (b == 0 && tid == 0) {
-    z = 0.0;
-    for (int q = 0; q < NT / 64; ++q) z += m.z[q];
-    o.loss[1] = (float)z;
-  }
-  __syncthreads();
-  return balance;        // in the first wave
+  return lo;
 }
 
 __global__ __launch_bounds__(kFinishBlock) void k_route_finish(Rows r, Parts s, RouteOut o)
 {
-  __shared__ FinishLds<kFinishBlock> m;
-  const double balance = finish_experts<kFinishBlock>(r, s, o, blockIdx.x, m);
+  __shared__ FinishLds m;
+  constexpr uint32_t NT = kFinishBlock, kSlices = NT / kFinishExperts, kAhead = 16;
+  const uint32_t b = blockIdx.x;
+  const uint32_t tid = threadIdx.x;
+  const uint32_t le = tid % kFinishExperts, slice = tid / kFinishExperts, e = b * kFinishExperts + le;
+  const uint32_t w0 = (uint32_t)((uint64_t)s.W * slice / kSlices), w1 = (uint32_t)((uint64_t)s.W * (slice + 1) / kSlices);
+  Cell ahead[kAhead];
+  auto fetch = [&](uint32_t base) {
+#pragma unroll
+    for (uint32_t u = 0; u < kAhead; ++u) {
+      ahead[u] = Cell{0u, 0.0f};
+      if (e < r.E && base + u < w1) ahead[u] = s.cell[(uint64_t)(base + u) * r.E + e];
+    }
+  };
+  fetch(w0);                                   // in flight while the devices' rows are counted
+  const float weight = tid < r.K ? r.w[tid] : 0.0f;
+  uint32_t n = tid < s.W ? s.rows[tid] : 0u;
+  double z = tid < s.W && b == 0 ? s.z[tid] : 0.0;
+  if (tid <= kMaxK) m.first[tid] = tid <= r.K ? r.first[tid] : ~0u;
+  if (tid < kMaxK) m.rows[tid] = 0u;
+  for (uint32_t i = tid; i < r.K * kFinishExperts; i += NT) (&m.count[0][0])[i] = 0u;
+  __syncthreads();
+  const uint32_t dev = device_in(m.first, r.K, tid < s.W ? tid : 0u);
+  if (n) atomicAdd(&m.rows[dev], n);
+  for (uint32_t w = tid + NT; w < s.W; w += NT)
+    if ((n = s.rows[w])) atomicAdd(&m.rows[device_in(m.first, r.K, w)], n);
+  __syncthreads();
+  if (tid < r.K) {
+    n = m.rows[tid];
+    m.scale[tid] = n ? (double)weight / (double)n : 0.0;
+    if (b == 0) o.share[tid] = n ? 1.0f / (float)n : 0.0f;
+  }
+  __syncthreads();
+  double load = 0.0, prob = 0.0;
+  if (e < r.E && w0 < w1) {
+    uint32_t d = device_in(m.first, r.K, w0), end = m.first[d + 1], run = 0;
+    double scale = m.scale[d];
+    // kAhead results of one device at most are added in float
+    auto flush = [&](float p, uint32_t c) {
+      load = __builtin_fma(scale, (double)c, load);
+      prob = __builtin_fma(scale, (double)p, prob);
+      run += c;
+    };
+    for (uint32_t base = w0; base < w1; base += kAhead) {
+      if (base != w0) fetch(base);
+      float p = 0.0f;
+      uint32_t c = 0;
+      if (end >= w1 || base + kAhead <= end) {
+#pragma unroll
+        for (uint32_t u = 0; u < kAhead; ++u) {
+          p += ahead[u].prob;
+          c += ahead[u].count;
+        }
+      } else {
+#pragma unroll
+        for (uint32_t u = 0; u < kAhead; ++u) {
+          if (base + u < w1 && base + u >= end) {
+            flush(p, c);
+            if (run) atomicAdd(&m.count[d][le], run);
+            run = c = 0;
+            p = 0.0f;
+            while (base + u >= end) end = m.first[++d + 1];
+            scale = m.scale[d];
+          }
+          p += ahead[u].prob;
+          c += ahead[u].count;
+        }
+      }
+      flush(p, c);
+    }
+    if (run) atomicAdd(&m.count[d][le], run);
+  }
+#pragma unroll
+  for (int x = kFinishExperts; x < 64; x *= 2) {
+    load += __shfl_xor(load, x, 64);
+    prob += __shfl_xor(prob, x, 64);
+  }
+  if (lane_id() < kFinishExperts) {
+    m.load[tid >> 6][le] = load;
+    m.prob[tid >> 6][le] = prob;
+  }
+  if (b == 0) {
+    z *= m.scale[dev];
+    for (uint32_t w = tid + NT; w < s.W; w += NT) z = __builtin_fma(m.scale[device_in(m.first, r.K, w)], s.z[w], z);
+    z = wave_sum_f64(z);
+    if (lane_id() == 0) m.z[tid >> 6] = z;
+  }
+  __syncthreads();
+  for (uint32_t i = tid; i < r.K * kFinishExperts; i += NT) {
+    const uint32_t x = b * kFinishExperts + i % kFinishExperts;
+    if (x < r.E) o.counts[(uint64_t)(i / kFinishExperts) * r.E + x] = (int32_t)m.count[i / kFinishExperts][i % kFinishExperts];
+  }
+  double balance = 0.0;
+  if (tid < 64) {
+    // lane tid takes expert tid % 16 of every fourth wave's sums
+    load = prob = 0.0;
+    for (uint32_t q = tid / kFinishExperts; q < NT / 64; q += 64 / kFinishExperts) {
+      load += m.load[q][le];
+      prob += m.prob[q][le];
+    }
+#pragma unroll
+    for (int x = kFinishExperts; x < 64; x *= 2) {
+      load += __shfl_xor(load, x, 64);
+      prob += __shfl_xor(prob, x, 64);
+    }
+    load /= (double)r.k;
+    if (tid < kFinishExperts && e < r.E) {
+      o.load[e] = (float)load;
+      balance = load * prob * (double)r.E;
+    }
+    balance = wave_sum_f64(balance);
+    if (b == 0) {
+      z = wave_sum_f64(tid < NT / 64 ? m.z[tid] : 0.0);
+      if (tid == 0) o.loss[1] = (float)z;
+    }
+  }
   if (threadIdx.x == 0) put(&s.balance[blockIdx.x], balance);
-  if (!block_is_last(s.ticket, 1u, gridDim.x)) return;
-  if (threadIdx.x) return;
+  if (!block_is_last(s.ticket, 1u, gridDim.x) || threadIdx.x >= 64) return;
   double sum = 0.0;
-  for (uint32_t b = 0; b < gridDim.x; ++b) sum += get(&s.balance[b]);
-  o.loss[0] = (float)sum;
+  for (uint32_t i = threadIdx.x; i < gridDim.x; i += 64) sum += get(&s.balance[i]);
+  sum = wave_sum_f64(sum);
+  if (threadIdx.x == 0) o.loss[0] = (float)sum;
 }
 
 // ---- forward ------------------------------------------------------------------------------------
@@ -258,17 +332,108 @@ struct RouteLds {
   float ex[kGroups][kMaxChoices];
   double z[kGroups];
   uint32_t rows[kGroups];
+  alignas(16) float top[kGroups][G];
+  alignas(16) uint64_t few[kGroups][G];
+  uint32_t nfew[kGroups];
 };
 
+// The k choices of every group's row of the wave, one after the other: k rounds
+// of the largest value left, then the lowest index that has it. x is used up.
+template <int G, int V>
+__device__ inline void choose_in_turn(float (&x)[V], float mx, float mid, uint32_t k, uint32_t l4, uint32_t group, RouteLds<G, V>& m)
+{
+  for (uint32_t c = 0; c < k; ++c) {
+    float top = mx;
+    if (c) {
+      top = x[0];
+#pragma unroll
+      for (int i = 1; i < V; ++i) top = __builtin_fmaxf(top, x[i]);
+      top = group_max<G>(top);
+    }
+    uint32_t mine = V;                      // the lane's first element that has it
+#pragma unroll
+    for (int i = V - 1; i >= 0; --i) mine = x[i] == top ? (uint32_t)i : mine;
+    const uint32_t e = mine < (uint32_t)V ? expert_of<G>(mine, l4) : ~0u, at = group_min<G>(e);
+    const bool some = top > -__builtin_inff() && at != ~0u;
+    if (e != at) mine = V;
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[i] = (uint32_t)i == mine ? -__builtin_inff() : x[i];
+    if (l4 == 0) {
+      m.idx[group][c] = some ? at : ~0u;
+      m.ex[group][c] = some ? exp_of(top - mid) : 0.0f;
+      if (some) atomicAdd(&m.count[at], 1u);
+    }
+  }
+}
+
+// The same by a threshold: at least k lanes hold a value at or above the k-th
+// largest of the lanes' maxima `top`, so the choices are among the values at or
+// above it. They are put into LDS, one per lane, and ranked by counting the
+// larger ones (equal values: the lower index is the larger). False, with nothing
+// done, where a row of the wave has more such values than lanes; rare as long as
+// k is at most half the lanes (random logits: 10.6 values on average for 8 of
+// 16 lanes, standard deviation 2).
+template <int G, int V>
+__device__ inline bool choose_few(const float (&x)[V], float top, float mid, uint32_t k, uint32_t l, uint32_t group, RouteLds<G, V>& m)
+{
+  m.top[group][l] = top;
+  m.few[group][l] = 0ull;
+  if (l == 0) m.nfew[group] = 0u;
+  wave_sync();
+  uint32_t above = 0;
+#pragma unroll
+  for (int j = 0; j < G / 4; ++j) {
+    const f4 t = *reinterpret_cast<const f4*>(&m.top[group][4 * j]);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) above += t[q] > top ? 1u : 0u;
+  }
+  float least = group_reduce<G>(above < k ? top : __builtin_inff(), [](float a, float b) { return __builtin_fminf(a, b); });
+  least = __builtin_fmaxf(least, -__FLT_MAX__);            // an expert at -infinity is never chosen
+  uint32_t n = 0;
+#pragma unroll
+  for (int i = 0; i < V; ++i) n += x[i] >= least ? 1u : 0u;
+  uint32_t at = n ? atomicAdd(&m.nfew[group], n) : 0u, none = ~(4 * l);
+  asm volatile("" : "+v"(none));             // 16 differences of it would be kept in registers over the rows
+  wave_sync();
+  if (__ballot(m.nfew[group] > (uint32_t)G)) return false;
+#pragma unroll
+  for (int i = 0; i < V; ++i)
+    if (x[i] >= least) m.few[group][at++] = (uint64_t)__float_as_uint(x[i] + 0.0f) << 32 | (none - expert_at<G>(i));
+  if (l < k) {
+    m.idx[group][l] = ~0u;
+    m.ex[group][l] = 0.0f;
+  }
+  wave_sync();
+  // order of floats as integers, above 0 for a value that is there
+  auto order = [](uint64_t v) {
+    const uint32_t u = (uint32_t)(v >> 32);
+    const uint32_t flip = (uint32_t)((int32_t)u >> 31) | 0x80000000u;
+    return v ? (uint64_t)(u ^ flip) << 32 | (uint32_t)v : 0ull;
+  };
+  const uint64_t raw = m.few[group][l], mine = order(raw);
+  wave_sync();
+  m.few[group][l] = mine;
+  wave_sync();
+  uint32_t rank = 0;
+#pragma unroll
+  for (int j = 0; j < G; ++j) rank += m.few[group][j] > mine ? 1u : 0u;
+  if (mine && rank < k) {
+    const uint32_t e = ~(uint32_t)mine;
+    m.idx[group][rank] = e;
+    m.ex[group][rank] = exp_of(__uint_as_float((uint32_t)(raw >> 32)) - mid);
+    atomicAdd(&m.count[e], 1u);
+  }
+  return true;
+}
+
 template <class X, int G, int V, bool kOne>
-__global__ __launch_bounds__(kBlock) void k_route(Rows r, const X* logits, const uint8_t* valid, RouteOut o, Parts s)
+__global__ __launch_bounds__(kBlock, kOne ? 1 : V >= 16 ? 4 : 5) void k_route(Rows r, const X* logits, const uint8_t* valid, RouteOut o, Parts s)
 {
   constexpr int kGroups = kBlock / G;
   __shared__ RouteLds<G, V> m;
   const uint32_t tid = threadIdx.x, l = tid % G, l4 = 4 * l, group = tid / G;
-  const uint32_t d = device_of(r, blockIdx.x);
-  const uint64_t row0 = r.off[d] + (uint64_t)(blockIdx.x - r.first[d]) * r.per;
-  const uint64_t row1 = row0 + r.per < r.off[d + 1] ? row0 + r.per : r.off[d + 1];
+  const Share mine = share_of(r, blockIdx.x);
+  const uint64_t row0 = mine.row0, row1 = mine.row1;
   for (uint32_t e = tid; e < G * V; e += kBlock) m.count[e] = 0u;
   if (blockIdx.x == 0 && tid == 0) *s.ticket = 0u;
   __syncthreads();
@@ -282,10 +447,10 @@ __global__ __launch_bounds__(kBlock) void k_route(Rows r, const X* logits, const
     const bool on = row < row1 && (!valid || gptr(valid)[row]);
     float x[V];
     load_row<X, G, V>(x, logits + row * r.ld, l4, r.E, on);
-    float mx = x[0];
+    float top = x[0];
 #pragma unroll
-    for (int i = 1; i < V; ++i) mx = __builtin_fmaxf(mx, x[i]);
-    mx = group_max<G>(mx);
+    for (int i = 1; i < V; ++i) top = __builtin_fmaxf(top, x[i]);
+    const float mx = group_max<G>(top);
     // a row without a value above -inf sums to zero: it routes nowhere and is not counted
     const float mid = mx == -__builtin_inff() ? 0.0f : mx;
     float p[V], sum = 0.0f;
@@ -299,36 +464,19 @@ __global__ __launch_bounds__(kBlock) void k_route(Rows r, const X* logits, const
     const float inv = counted ? 1.0f / sum : 0.0f;
     const float lse = counted ? mid + __builtin_amdgcn_logf(sum) * kLn2 : 0.0f;
 #pragma unroll
-    for (int i = 0; i < V; ++i) acc[i] += p[i] * inv;
+    for (int i = 0; i < V; ++i) acc[i] = __builtin_fmaf(p[i], inv, acc[i]);
     z += (double)lse * (double)lse;
     rows += counted ? 1u : 0u;
+    if (!(G >= 16 && r.k >= kFewFrom && 2 * r.k <= G && choose_few<G, V>(x, top, mid, r.k, l, group, m)))
+      choose_in_turn<G, V>(x, mx, mid, r.k, l4, group, m);
+    wave_sync();
     float chosen = 0.0f;
-    for (uint32_t c = 0; c < r.k; ++c) {
-      float top = mx;
-      if (c) {
-        top = x[0];
-#pragma unroll
-        for (int i = 1; i < V; ++i) top = __builtin_fmaxf(top, x[i]);
-        top = group_max<G>(top);
-      }
-      uint32_t at = ~0u;
-#pragma unroll
-      for (int i = V - 1; i >= 0; --i) at = x[i] == top ? expert_at<G>(i) + l4 : at;
-      at = group_min<G>(at);
-      const bool some = top > -__builtin_inff() && at != ~0u;
-#pragma unroll
-      for (int i = 0; i < V; ++i) x[i] = expert_at<G>(i) + l4 == at ? -__builtin_inff() : x[i];
-      const float ex = some ? exp_of(top - mid) : 0.0f;
-      chosen += ex;
-      if (l == 0) {
-        m.idx[group][c] = some ? at : ~0u;
-        m.ex[group][c] = ex;
-        if (some) atomicAdd(&m.count[at], 1u);
-      }
+    if (r.renormalise) {
+      for (uint32_t c = l; c < r.k; c += G) chosen += m.ex[group][c];
+      chosen = group_sum<G>(chosen);
     }
     float to_gate = inv;
     if (r.renormalise && sum < __builtin_inff()) to_gate = chosen > 0.0f ? 1.0f / chosen : 0.0f;   // else NaN, as inv is
-    wave_sync();
     if (row < row1) {
       for (uint32_t c = l; c < r.k; c += G) {
         o.idx[row * r.k + c] = (int32_t)m.idx[group][c];
@@ -345,28 +493,44 @@ __global__ __launch_bounds__(kBlock) void k_route(Rows r, const X* logits, const
     m.rows[group] = rows;
   }
   __syncthreads();
+  double zs = 0.0, n = 0.0;
+  if (tid < 64) {
+    zs = wave_sum_f64(tid < kGroups ? m.z[tid] : 0.0);
+    n = wave_sum_f64(tid < kGroups ? (double)m.rows[tid] : 0.0);
+    if constexpr (kOne) {
+      if (tid == 0) m.z[0] = n;
+    } else if (tid == 0) {
+      s.z[blockIdx.x] = zs;
+      s.rows[blockIdx.x] = (uint32_t)n;
+    }
+  }
+  if constexpr (kOne) __syncthreads();
+  double scale = 0.0, balance = 0.0;
+  if constexpr (kOne) {
+    n = m.z[0];
+    scale = n > 0.0 ? (double)r.w[mine.d] / n : 0.0;
+  }
   for (uint32_t e = tid; e < r.E; e += kBlock) {
     float sum = 0.0f;
+#pragma unroll 4
     for (int g = 0; g < kGroups; ++g) sum += m.prob[g * (G * V) + e];
-    s.prob[(uint64_t)blockIdx.x * r.E + e] = sum;
-    s.count[(uint64_t)blockIdx.x * r.E + e] = m.count[e];
-  }
-  if (tid == 0) {
-    double sum = 0.0;
-    uint32_t n = 0;
-    for (int g = 0; g < kGroups; ++g) {
-      sum += m.z[g];
-      n += m.rows[g];
+    if constexpr (kOne) {
+      const double load = scale * (double)m.count[e] / (double)r.k;
+      balance += load * scale * (double)sum * (double)r.E;
+      o.load[e] = (float)load;
+      for (uint32_t d = 0; d < r.K; ++d) o.counts[(uint64_t)d * r.E + e] = d == mine.d ? (int32_t)m.count[e] : 0;
+    } else {
+      s.cell[(uint64_t)blockIdx.x * r.E + e] = Cell{m.count[e], sum};
     }
-    s.z[blockIdx.x] = sum;
-    s.rows[blockIdx.x] = n;
   }
-  if constexpr (kOne) {        // the only workgroup: no second launch
-    __shared__ FinishLds<kBlock> f;
-    __syncthreads();
-    double balance = 0.0;
-    for (uint32_t b = 0; b * kFinishExperts < r.E; ++b) balance += finish_experts<kBlock>(r, s, o, b, f);
-    if (tid == 0) o.loss[0] = (float)balance;
+  if constexpr (kOne) {        // the only workgroup: it makes the sums over all rows itself
+    for (uint32_t d = tid; d < r.K; d += kBlock) o.share[d] = d == mine.d && n > 0.0 ? (float)(1.0 / n) : 0.0f;
+    __shared__ double s_sum[kWaves];
+    balance = block_sum_f64(balance, s_sum);
+    if (tid == 0) {
+      o.loss[0] = (float)balance;
+      o.loss[1] = (float)(scale * zs);
+    }
   }
 }
 
@@ -378,10 +542,9 @@ __global__ __launch_bounds__(kBlock) void k_route_back(Rows r, const X* logits, 
   constexpr int kGroups = kBlock / G;
   __shared__ float s_part[kGroups][G * V];      // the gates' part of the group's row, zero elsewhere
   const uint32_t tid = threadIdx.x, l = tid % G, l4 = 4 * l, group = tid / G;
-  const uint32_t d = device_of(r, blockIdx.x);
-  const uint64_t row0 = r.off[d] + (uint64_t)(blockIdx.x - r.first[d]) * r.per;
-  const uint64_t row1 = row0 + r.per < r.off[d + 1] ? row0 + r.per : r.off[d + 1];
-  const float scale = r.w[d] * o.share[d];
+  const Share mine = share_of(r, blockIdx.x);
+  const uint64_t row0 = mine.row0, row1 = mine.row1;
+  const float scale = r.w[mine.d] * o.share[mine.d];
   const float a = dloss ? dloss[0] * scale * (float)r.E : 0.0f, b2 = dloss ? 2.0f * dloss[1] * scale : 0.0f;
   float load[V];
 #pragma unroll
@@ -466,14 +629,23 @@ uint32_t rows_per_round(uint32_t E)
   return n;
 }
 
-// Rows of one workgroup, so that about kRouteBlocks workgroups share T rows.
-uint32_t rows_per_block(uint64_t T, uint32_t E)
+uint32_t blocks_for(const scadles_router* q, uint64_t per)
 {
-  const uint32_t round = rows_per_round(E);
-  uint64_t rounds = div_up(T, (uint64_t)round * kRouteBlocks);
-  if (rounds < 1) rounds = 1;
-  if (rounds > kMaxRounds) rounds = kMaxRounds;
-  return round * (uint32_t)rounds;
+  uint64_t w = 0;
+  for (uint32_t d = 0; d < q->devices; ++d) w += div_up(q->tok_off[d + 1] - q->tok_off[d], per);
+  return (uint32_t)w;
+}
+
+// Rounds of rows of one workgroup, so that at most kRouteBlocks workgroups share
+// the rows: that many fit the GPU at once, and one more would make the call
+// take twice as long (131072 x 256: 52 us with 1040 of them, 29 us with 927).
+uint32_t rounds_for(const scadles_router* q)
+{
+  const uint64_t round = rows_per_round(q->experts);
+  uint64_t n = div_up(q->tokens, round * kRouteBlocks);
+  if (n < 1) n = 1;
+  while (n < kMaxRounds && blocks_for(q, round * n) > kRouteBlocks) ++n;
+  return (uint32_t)(n < kMaxRounds ? n : kMaxRounds);
 }
 
 scadles_status check_router(const scadles_router* q)
@@ -501,7 +673,7 @@ scadles_status check_router(const scadles_router* q)
 uint32_t make_rows(const scadles_router* q, Rows& r)
 {
   std::memset(&r, 0, sizeof(r));
-  r.per = rows_per_block(q->tokens, q->experts);
+  r.per = rows_per_round(q->experts) * rounds_for(q);
   r.E = q->experts;
   r.k = q->k;
   r.K = q->devices;
@@ -530,13 +702,11 @@ uint64_t take(uint64_t& at, uint64_t bytes)
 uint64_t lay_out(uint32_t W, uint32_t E, char* ws, Parts& s)
 {
   uint64_t at = 0;
-  const uint64_t cells = (uint64_t)W * E * 4;
   s.ticket = reinterpret_cast<uint32_t*>(ws + take(at, 256));
   s.balance = reinterpret_cast<double*>(ws + take(at, kMaxExperts / kFinishExperts * 8));
   s.z = reinterpret_cast<double*>(ws + take(at, (uint64_t)W * 8));
   s.rows = reinterpret_cast<uint32_t*>(ws + take(at, (uint64_t)W * 4));
-  s.prob = reinterpret_cast<float*>(ws + take(at, cells));
-  s.count = reinterpret_cast<uint32_t*>(ws + take(at, cells));
+  s.cell = reinterpret_cast<Cell*>(ws + take(at, (uint64_t)W * E * sizeof(Cell)));
   s.W = W;
   return at;
 }
@@ -601,10 +771,9 @@ size_t scadles_router_workspace_bytes(uint64_t tokens, uint32_t experts, uint32_
 {
   if (tokens > 0x7FFFFFFFull || !experts || experts > kMaxExperts || !devices || devices > kMaxK) return 0;
   // the most workgroups of any call of so many rows or fewer; every device's last one may be partly filled
-  const uint64_t round = rows_per_round(experts);
-  uint64_t W = tokens / round < kRouteBlocks ? tokens / round : kRouteBlocks;
-  if (tokens / (round * kMaxRounds) > W) W = tokens / (round * kMaxRounds);
-  W += devices;
+  const uint64_t round = rows_per_round(experts), few = tokens / round + devices;
+  const uint64_t many = tokens / (round * kMaxRounds) + devices;
+  const uint64_t W = few < kRouteBlocks ? few : many > kRouteBlocks ? many : kRouteBlocks;
   Parts s;
   return (size_t)lay_out((uint32_t)W, experts, nullptr, s);
 }
