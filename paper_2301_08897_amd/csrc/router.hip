@@ -17,6 +17,7 @@
 // device and keeps the experts' probability sums in registers meanwhile.
 #include <cmath>
 #include <cstring>
+#include <type_traits>
 
 #include "abi.h"
 #include "radix.h"
@@ -78,43 +79,75 @@ __device__ inline uint32_t dpp(uint32_t x)
 }
 
 // Combines x over the group; every lane ends with the same value, in the same
-// pattern of operations whatever the data.
-template <int G, class Op>
-__device__ inline float group_reduce(float x, Op op)
+// pattern of operations whatever the data. `step` combines with the lane that
+// the given exchange names.
+template <int G, class Step, class Far>
+__device__ inline float group_reduce(float x, Step step, Far far)
 {
-  auto f = [](uint32_t u) { return __uint_as_float(u); };
-  if constexpr (G >= 2) x = op(x, f(dpp<0xB1>(__float_as_uint(x))));    // lanes 1 apart
-  if constexpr (G >= 4) x = op(x, f(dpp<0x4E>(__float_as_uint(x))));    // 2 apart
-  if constexpr (G >= 8) x = op(x, f(dpp<0x141>(__float_as_uint(x))));   // the halves of 8
-  if constexpr (G >= 16) x = op(x, f(dpp<0x140>(__float_as_uint(x))));  // of 16
-  if constexpr (G >= 32) x = op(x, __shfl_xor(x, 16, 64));
-  if constexpr (G >= 64) x = op(x, __shfl_xor(x, 32, 64));
+  if constexpr (G >= 2) x = step(x, std::integral_constant<int, 0xB1>());    // lanes 1 apart
+  if constexpr (G >= 4) x = step(x, std::integral_constant<int, 0x4E>());    // 2 apart
+  if constexpr (G >= 8) x = step(x, std::integral_constant<int, 0x141>());   // the halves of 8
+  if constexpr (G >= 16) x = step(x, std::integral_constant<int, 0x140>());  // of 16
+  if constexpr (G >= 32) x = far(x, __shfl_xor(x, 16, 64));
+  if constexpr (G >= 64) x = far(x, __shfl_xor(x, 32, 64));
   return x;
 }
+
+// One instruction with the exchange in it; the compiler would put a move and a
+// second maximum (against signalling NaN) before it. It waits for x itself.
+#define SCADLES_DPP_STEP(op, how) asm volatile("s_nop 1\n\t" op " %0, %1, %1 " how " row_mask:0xf bank_mask:0xf" : "=v"(y) : "v"(x))
+#define SCADLES_DPP_OP(op)                                            \
+  [](float x, auto ctrl) {                                            \
+    float y;                                                          \
+    if constexpr (ctrl == 0xB1) SCADLES_DPP_STEP(op, "quad_perm:[1,0,3,2]"); \
+    else if constexpr (ctrl == 0x4E) SCADLES_DPP_STEP(op, "quad_perm:[2,3,0,1]"); \
+    else if constexpr (ctrl == 0x141) SCADLES_DPP_STEP(op, "row_half_mirror"); \
+    else SCADLES_DPP_STEP(op, "row_mirror");                          \
+    return y;                                                         \
+  }
 
 template <int G>
 __device__ inline float group_max(float x)
 {
-  return group_reduce<G>(x, [](float a, float b) { return __builtin_fmaxf(a, b); });
+  return group_reduce<G>(x, SCADLES_DPP_OP("v_max_f32_dpp"), [](float a, float b) { return __builtin_fmaxf(a, b); });
+}
+
+template <int G>
+__device__ inline float group_least(float x)
+{
+  return group_reduce<G>(x, SCADLES_DPP_OP("v_min_f32_dpp"), [](float a, float b) { return __builtin_fminf(a, b); });
 }
 
 template <int G>
 __device__ inline float group_sum(float x)
 {
-  return group_reduce<G>(x, [](float a, float b) { return a + b; });
+  return group_reduce<G>(x, [](float a, auto ctrl) { return a + __uint_as_float(dpp<ctrl>(__float_as_uint(a))); },
+                         [](float a, float b) { return a + b; });
 }
 
 template <int G>
 __device__ inline uint32_t group_min(uint32_t x)
 {
-  auto f = [](float a, float b) {
-    const uint32_t u = __float_as_uint(a), v = __float_as_uint(b);
-    return __uint_as_float(u < v ? u : v);
-  };
-  return __float_as_uint(group_reduce<G>(__uint_as_float(x), f));
+  auto least = [](uint32_t u, uint32_t v) { return __uint_as_float(u < v ? u : v); };
+  return __float_as_uint(group_reduce<G>(__uint_as_float(x),
+                                         [&](float a, auto ctrl) { return least(__float_as_uint(a), dpp<ctrl>(__float_as_uint(a))); },
+                                         [&](float a, float b) { return least(__float_as_uint(a), __float_as_uint(b)); }));
 }
 
 __device__ inline float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+
+// exp(x - mid) of a row, as 2^(x log2 e - mid log2 e) with one rounding for the
+// product and the difference; the rounding of mid log2 e is a factor of the
+// whole row and cancels in its probabilities. In a row whose products could
+// overflow (`far`), of the difference.
+struct Exp {
+  float mid, c;
+  bool far;
+  __device__ inline float operator()(float x) const
+  {
+    return far ? exp_of(x - mid) : __builtin_amdgcn_exp2f(__builtin_fmaf(x, kLog2e, -c));
+  }
+};
 
 // Orders LDS accesses of the lanes of a wave, which run in step: only the
 // compiler has to keep their order.
@@ -160,11 +193,20 @@ __device__ inline uint32_t expert_of(uint32_t i, uint32_t l4) { return (i >> 2) 
 template <class X, int G, int V>
 __device__ inline void load_row(float (&x)[V], const X* row, uint32_t l4, uint32_t E, bool on)
 {
+  if (!on) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[i] = -__builtin_inff();
+    return;
+  }
+  const X* p = row + l4;
 #pragma unroll
   for (int j = 0; j < V / 4; ++j) {
-    const uint32_t e = expert_at<G>(4 * j) + l4;
-    const uint32_t k = on && e < E ? E - e : 0u;
-    const f4 v = load_once_f4(row + e, k, -__builtin_inff());
+    uint32_t k = 4;
+    if (expert_at<G>(4 * j + 4) > E) {         // not all lanes have four elements here
+      const uint32_t e = expert_at<G>(4 * j) + l4;
+      k = e < E ? E - e : 0u;
+    }
+    const f4 v = load_once_f4(p + expert_at<G>(4 * j), k, -__builtin_inff());
 #pragma unroll
     for (int q = 0; q < 4; ++q) x[4 * j + q] = v[q];
   }
@@ -327,20 +369,21 @@ template <int G, int V>
 struct RouteLds {
   static constexpr int kGroups = kBlock / G;
   uint32_t count[G * V];
-  float prob[kGroups * G * V];
+  alignas(16) float row[kGroups][G * V];     // the groups' rows, at the end the groups' probability sums
   uint32_t idx[kGroups][kMaxChoices];
   float ex[kGroups][kMaxChoices];
   double z[kGroups];
   uint32_t rows[kGroups];
   alignas(16) float top[kGroups][G];
   alignas(16) uint64_t few[kGroups][G];
+  uint32_t at[kGroups][G];
   uint32_t nfew[kGroups];
 };
 
 // The k choices of every group's row of the wave, one after the other: k rounds
 // of the largest value left, then the lowest index that has it. x is used up.
 template <int G, int V>
-__device__ inline void choose_in_turn(float (&x)[V], float mx, float mid, uint32_t k, uint32_t l4, uint32_t group, RouteLds<G, V>& m)
+__device__ inline void choose_in_turn(float (&x)[V], float mx, const Exp& ex, uint32_t k, uint32_t l4, uint32_t group, RouteLds<G, V>& m)
 {
   for (uint32_t c = 0; c < k; ++c) {
     float top = mx;
@@ -360,7 +403,7 @@ __device__ inline void choose_in_turn(float (&x)[V], float mx, float mid, uint32
     for (int i = 0; i < V; ++i) x[i] = (uint32_t)i == mine ? -__builtin_inff() : x[i];
     if (l4 == 0) {
       m.idx[group][c] = some ? at : ~0u;
-      m.ex[group][c] = some ? exp_of(top - mid) : 0.0f;
+      m.ex[group][c] = some ? ex(top) : 0.0f;
       if (some) atomicAdd(&m.count[at], 1u);
     }
   }
@@ -368,59 +411,69 @@ __device__ inline void choose_in_turn(float (&x)[V], float mx, float mid, uint32
 
 // The same by a threshold: at least k lanes hold a value at or above the k-th
 // largest of the lanes' maxima `top`, so the choices are among the values at or
-// above it. They are put into LDS, one per lane, and ranked by counting the
-// larger ones (equal values: the lower index is the larger). False, with nothing
-// done, where a row of the wave has more such values than lanes; rare as long as
-// k is at most half the lanes (random logits: 10.6 values on average for 8 of
-// 16 lanes, standard deviation 2).
+// above it. Their experts are listed in LDS, one per lane, and ranked by
+// counting the larger ones (of equal values, the lower index is the larger).
+// False, with nothing chosen, where a row of the wave has more such values than
+// lanes; rare as long as k is at most half the lanes (random logits: 10.6 values
+// on average for 8 of 16 lanes, standard deviation 2). Comparisons are taken
+// from the sign of a difference and gathered bit by bit: a compare's result
+// would have to be waited for.
 template <int G, int V>
-__device__ inline bool choose_few(const float (&x)[V], float top, float mid, uint32_t k, uint32_t l, uint32_t group, RouteLds<G, V>& m)
+__device__ inline bool choose_few(const float (&x)[V], float top, const Exp& ex, uint32_t k, uint32_t l, uint32_t group, RouteLds<G, V>& m)
 {
+  auto append = [](uint32_t bits, float x) { return __builtin_amdgcn_alignbit(bits, __float_as_uint(x), 31); };
+  top = __builtin_fmaxf(top, -__FLT_MAX__);                // an expert at -infinity is never chosen
   m.top[group][l] = top;
+#pragma unroll
+  for (int j = 0; j < V / 4; ++j)
+    *reinterpret_cast<f4*>(&m.row[group][expert_at<G>(4 * j) + 4 * l]) = f4{x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]};
   m.few[group][l] = 0ull;
   if (l == 0) m.nfew[group] = 0u;
   wave_sync();
   uint32_t above = 0;
 #pragma unroll
-  for (int j = 0; j < G / 4; ++j) {
-    const f4 t = *reinterpret_cast<const f4*>(&m.top[group][4 * j]);
+  for (int h = 0; h < G; h += 32) {
+    uint32_t bits = 0;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) above += t[q] > top ? 1u : 0u;
+    for (int j = h; j < h + 32 && j < G; j += 4) {
+      const f4 t = *reinterpret_cast<const f4*>(&m.top[group][j]);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) bits = append(bits, top - t[q]);
+    }
+    above += __builtin_popcount(bits);
   }
-  float least = group_reduce<G>(above < k ? top : __builtin_inff(), [](float a, float b) { return __builtin_fminf(a, b); });
-  least = __builtin_fmaxf(least, -__FLT_MAX__);            // an expert at -infinity is never chosen
-  uint32_t n = 0;
+  const float least = group_least<G>(above < k ? top : __builtin_inff());
+  uint32_t below = 0;
 #pragma unroll
-  for (int i = 0; i < V; ++i) n += x[i] >= least ? 1u : 0u;
-  uint32_t at = n ? atomicAdd(&m.nfew[group], n) : 0u, none = ~(4 * l);
-  asm volatile("" : "+v"(none));             // 16 differences of it would be kept in registers over the rows
+  for (int i = V - 1; i >= 0; --i) below = append(below, x[i] - least);      // bit i: element i
+  uint32_t mine = ~below & ((1u << V) - 1);
+  const uint32_t n = __builtin_popcount(mine);
+  uint32_t at = n ? atomicAdd(&m.nfew[group], n) : 0u;
   wave_sync();
-  if (__ballot(m.nfew[group] > (uint32_t)G)) return false;
-#pragma unroll
-  for (int i = 0; i < V; ++i)
-    if (x[i] >= least) m.few[group][at++] = (uint64_t)__float_as_uint(x[i] + 0.0f) << 32 | (none - expert_at<G>(i));
+  const uint32_t all = m.nfew[group];
+  if (__ballot(all > (uint32_t)G)) return false;
+  while (mine) {
+    m.at[group][at++] = expert_of<G>((uint32_t)__builtin_ctz(mine), 4 * l);
+    mine &= mine - 1;
+  }
   if (l < k) {
     m.idx[group][l] = ~0u;
     m.ex[group][l] = 0.0f;
   }
   wave_sync();
-  // order of floats as integers, above 0 for a value that is there
-  auto order = [](uint64_t v) {
-    const uint32_t u = (uint32_t)(v >> 32);
-    const uint32_t flip = (uint32_t)((int32_t)u >> 31) | 0x80000000u;
-    return v ? (uint64_t)(u ^ flip) << 32 | (uint32_t)v : 0ull;
-  };
-  const uint64_t raw = m.few[group][l], mine = order(raw);
-  wave_sync();
-  m.few[group][l] = mine;
+  const bool some = l < all;
+  const uint32_t e = some ? m.at[group][l] : 0u;
+  const float value = m.row[group][e];
+  const uint32_t u = __float_as_uint(value + 0.0f);        // -0 counts as 0; order of floats as integers
+  const uint64_t key = some ? (uint64_t)(u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u)) << 32 | ~e : 0ull;
+  if (some) m.few[group][l] = key;
   wave_sync();
   uint32_t rank = 0;
-#pragma unroll
-  for (int j = 0; j < G; ++j) rank += m.few[group][j] > mine ? 1u : 0u;
-  if (mine && rank < k) {
-    const uint32_t e = ~(uint32_t)mine;
+#pragma unroll 4
+  for (int j = 0; j < G; ++j) rank += m.few[group][j] > key ? 1u : 0u;
+  if (some && rank < k) {
     m.idx[group][rank] = e;
-    m.ex[group][rank] = exp_of(__uint_as_float((uint32_t)(raw >> 32)) - mid);
+    m.ex[group][rank] = ex(value);
     atomicAdd(&m.count[e], 1u);
   }
   return true;
@@ -442,8 +495,8 @@ __global__ __launch_bounds__(kBlock, kOne ? 1 : V >= 16 ? 4 : 5) void k_route(Ro
   for (int i = 0; i < V; ++i) acc[i] = 0.0f;
   double z = 0.0;
   uint32_t rows = 0;
-  for (uint64_t base = row0; base < row1; base += kGroups) {
-    const uint64_t row = base + group;
+  for (uint64_t base = row0 + wave_id() * (64 / G); base < row1; base += kGroups) {     // the wave's rows
+    const uint64_t row = base + lane_id() / G;
     const bool on = row < row1 && (!valid || gptr(valid)[row]);
     float x[V];
     load_row<X, G, V>(x, logits + row * r.ld, l4, r.E, on);
@@ -454,21 +507,27 @@ __global__ __launch_bounds__(kBlock, kOne ? 1 : V >= 16 ? 4 : 5) void k_route(Ro
     // a row without a value above -inf sums to zero: it routes nowhere and is not counted
     const float mid = mx == -__builtin_inff() ? 0.0f : mx;
     float p[V], sum = 0.0f;
+    const Exp ex = {mid, mid * kLog2e, !(__builtin_fabsf(mid) < 1e30f)};
+    if (__ballot(ex.far)) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      p[i] = exp_of(x[i] - mid);
-      sum += p[i];
+      for (int i = 0; i < V; ++i) p[i] = ex(x[i]);
+    } else {
+      const Exp near = {mid, ex.c, false};
+#pragma unroll
+      for (int i = 0; i < V; ++i) p[i] = near(x[i]);
     }
+#pragma unroll
+    for (int i = 0; i < V; ++i) sum += p[i];
     sum = group_sum<G>(sum);
     const bool counted = !(sum == 0.0f);
-    const float inv = counted ? 1.0f / sum : 0.0f;
+    const float inv = counted ? __builtin_amdgcn_rcpf(sum) : 0.0f;       // 1 <= sum <= E
     const float lse = counted ? mid + __builtin_amdgcn_logf(sum) * kLn2 : 0.0f;
 #pragma unroll
     for (int i = 0; i < V; ++i) acc[i] = __builtin_fmaf(p[i], inv, acc[i]);
     z += (double)lse * (double)lse;
     rows += counted ? 1u : 0u;
-    if (!(G >= 16 && r.k >= kFewFrom && 2 * r.k <= G && choose_few<G, V>(x, top, mid, r.k, l, group, m)))
-      choose_in_turn<G, V>(x, mx, mid, r.k, l4, group, m);
+    if (!(G >= 16 && r.k >= kFewFrom && 2 * r.k <= G && choose_few<G, V>(x, top, ex, r.k, l, group, m)))
+      choose_in_turn<G, V>(x, mx, ex, r.k, l4, group, m);
     wave_sync();
     float chosen = 0.0f;
     if (r.renormalise) {
@@ -476,7 +535,7 @@ __global__ __launch_bounds__(kBlock, kOne ? 1 : V >= 16 ? 4 : 5) void k_route(Ro
       chosen = group_sum<G>(chosen);
     }
     float to_gate = inv;
-    if (r.renormalise && sum < __builtin_inff()) to_gate = chosen > 0.0f ? 1.0f / chosen : 0.0f;   // else NaN, as inv is
+    if (r.renormalise && sum < __builtin_inff()) to_gate = chosen > 0.0f ? __builtin_amdgcn_rcpf(chosen) : 0.0f;   // else NaN, as inv is
     if (row < row1) {
       for (uint32_t c = l; c < r.k; c += G) {
         o.idx[row * r.k + c] = (int32_t)m.idx[group][c];
@@ -487,7 +546,7 @@ __global__ __launch_bounds__(kBlock, kOne ? 1 : V >= 16 ? 4 : 5) void k_route(Ro
     wave_sync();
   }
 #pragma unroll
-  for (int i = 0; i < V; ++i) m.prob[group * (G * V) + expert_at<G>(i) + l4] = acc[i];
+  for (int i = 0; i < V; ++i) m.row[group][expert_at<G>(i) + l4] = acc[i];
   if (l == 0) {
     m.z[group] = z;
     m.rows[group] = rows;
@@ -513,7 +572,7 @@ __global__ __launch_bounds__(kBlock, kOne ? 1 : V >= 16 ? 4 : 5) void k_route(Ro
   for (uint32_t e = tid; e < r.E; e += kBlock) {
     float sum = 0.0f;
 #pragma unroll 4
-    for (int g = 0; g < kGroups; ++g) sum += m.prob[g * (G * V) + e];
+    for (int g = 0; g < kGroups; ++g) sum += m.row[g][e];
     if constexpr (kOne) {
       const double load = scale * (double)m.count[e] / (double)r.k;
       balance += load * scale * (double)sum * (double)r.E;
@@ -554,8 +613,8 @@ __global__ __launch_bounds__(kBlock) void k_route_back(Rows r, const X* logits, 
     s_part[group][e] = 0.0f;
   }
   wave_sync();
-  for (uint64_t base = row0; base < row1; base += kGroups) {
-    const uint64_t row = base + group;
+  for (uint64_t base = row0 + wave_id() * (64 / G); base < row1; base += kGroups) {     // the wave's rows
+    const uint64_t row = base + lane_id() / G;
     const bool in = row < row1;
     const float lse = in ? o.lse[row] : 0.0f;
     const bool on = in && (o.idx[row * r.k] >= 0 || lse != lse);   // routed, or NaN
@@ -636,16 +695,16 @@ uint32_t blocks_for(const scadles_router* q, uint64_t per)
   return (uint32_t)w;
 }
 
-// Rounds of rows of one workgroup, so that at most kRouteBlocks workgroups share
-// the rows: that many fit the GPU at once, and one more would make the call
-// take twice as long (131072 x 256: 52 us with 1040 of them, 29 us with 927).
-uint32_t rounds_for(const scadles_router* q)
+// Rows of one workgroup, so that at most kRouteBlocks workgroups share them: that
+// many fit the GPU at once, and a few more make the call take nearly twice as
+// long. At least a round, then as many rows more as a wave takes at once.
+uint64_t rows_for(const scadles_router* q)
 {
-  const uint64_t round = rows_per_round(q->experts);
-  uint64_t n = div_up(q->tokens, round * kRouteBlocks);
-  if (n < 1) n = 1;
-  while (n < kMaxRounds && blocks_for(q, round * n) > kRouteBlocks) ++n;
-  return (uint32_t)(n < kMaxRounds ? n : kMaxRounds);
+  const uint64_t round = rows_per_round(q->experts), unit = round / kWaves, most = round * kMaxRounds;
+  uint64_t n = div_up(div_up(q->tokens, kRouteBlocks), unit) * unit;
+  if (n < round) n = round;
+  while (n < most && blocks_for(q, n) > kRouteBlocks) n += unit;
+  return n < most ? n : most;
 }
 
 scadles_status check_router(const scadles_router* q)
@@ -673,7 +732,7 @@ scadles_status check_router(const scadles_router* q)
 uint32_t make_rows(const scadles_router* q, Rows& r)
 {
   std::memset(&r, 0, sizeof(r));
-  r.per = rows_per_round(q->experts) * rounds_for(q);
+  r.per = (uint32_t)rows_for(q);
   r.E = q->experts;
   r.k = q->k;
   r.K = q->devices;
