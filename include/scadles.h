@@ -416,7 +416,7 @@ typedef struct scadles_adamw_plan {
 
 /* Bytes of the table of a plan for these tensors (only their sizes are read);
  * 0 for arguments the build would reject: count outside [1, 2^20], a tensor
- * of more than 2^32 - 1 elements, or more than about 2^35 elements in all.  */
+ * of more than 2^32 - 1 elements, or more than about 2^34 elements in all.  */
 size_t scadles_adamw_plan_bytes(const scadles_adamw_tensor* tensors, uint32_t count);
 
 /* Lists the tensors (host[count], read during the call) in a plan.

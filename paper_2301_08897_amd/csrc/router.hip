@@ -33,6 +33,7 @@ constexpr uint32_t kFinishExperts = 8;     // experts of one workgroup of k_rout
 constexpr int kFinishBlock = 512;
 constexpr uint32_t kFewFrom = 3;           // choices from which they are made by a threshold
 constexpr uint32_t kRouteBlocks = 1024;    // workgroups, at most, unless they would take
+constexpr uint32_t kBackBlocks = 1280;     // the same for the backward pass, which has no sums
 constexpr uint32_t kMaxRounds = 256;       // more rounds each than this: they sum probabilities in float
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
@@ -698,12 +699,13 @@ uint32_t blocks_for(const scadles_router* q, uint64_t per)
 // Rows of one workgroup, so that at most kRouteBlocks workgroups share them: that
 // many fit the GPU at once, and a few more make the call take nearly twice as
 // long. At least a round, then as many rows more as a wave takes at once.
-uint64_t rows_for(const scadles_router* q)
+uint64_t rows_for(const scadles_router* q, uint32_t blocks)
 {
   const uint64_t round = rows_per_round(q->experts), unit = round / kWaves, most = round * kMaxRounds;
-  uint64_t n = div_up(div_up(q->tokens, kRouteBlocks), unit) * unit;
+  uint64_t n = div_up(div_up(q->tokens, blocks), round) * round;
+  if (n >= 4 * round) n = div_up(div_up(q->tokens, blocks), unit) * unit;
   if (n < round) n = round;
-  while (n < most && blocks_for(q, n) > kRouteBlocks) n += unit;
+  while (n < most && blocks_for(q, n) > blocks) n += n < 4 * round ? round : unit;
   return n < most ? n : most;
 }
 
@@ -729,10 +731,10 @@ scadles_status check_router(const scadles_router* q)
 }
 
 // What the kernels need to know of the rows; returns the workgroups.
-uint32_t make_rows(const scadles_router* q, Rows& r)
+uint32_t make_rows(const scadles_router* q, uint32_t blocks, Rows& r)
 {
   std::memset(&r, 0, sizeof(r));
-  r.per = (uint32_t)rows_for(q);
+  r.per = (uint32_t)rows_for(q, blocks);
   r.E = q->experts;
   r.k = q->k;
   r.K = q->devices;
@@ -851,7 +853,7 @@ scadles_status scadles_router_forward(const scadles_router* router, const void* 
   if (!is_aligned(logits, esize)) return fail(SCADLES_EINVAL, "logits is not aligned to its elements");
   Rows r;
   Parts s;
-  const uint32_t W = make_rows(router, r);
+  const uint32_t W = make_rows(router, kRouteBlocks, r);
   const uint64_t need = lay_out(W, router->experts, static_cast<char*>(ws), s);
   if (!ws || !is_aligned(ws, 256)) return fail(SCADLES_EWORKSPACE, "workspace must be 256-byte aligned and not NULL");
   if (ws_bytes < need) return fail(SCADLES_EWORKSPACE, "workspace has %zu bytes, needs %zu", ws_bytes, (size_t)need);
@@ -893,7 +895,7 @@ scadles_status scadles_router_backward(const scadles_router* router, const void*
   for (int x = 0; x < 8; ++x)
     if (bytes_overlap(dlogits, bytes, ins[x], sizes[x])) return fail(SCADLES_EINVAL, "dlogits overlaps an input");
   Rows r;
-  const uint32_t W = make_rows(router, r);
+  const uint32_t W = make_rows(router, kBackBlocks, r);
   if (W == 0) return SCADLES_OK;
   hipStream_t st = static_cast<hipStream_t>(stream);
   const RouteOut o = outputs(out);

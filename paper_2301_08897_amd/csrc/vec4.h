@@ -80,4 +80,11 @@ __device__ inline void store_f4(uint16_t* p, f4 x, uint32_t k)
     if (q < k) gptr(p)[q] = h[q];
 }
 
+// The same for data that is not read again soon.
+__device__ inline void store_once_f4(float* p, f4 x, uint32_t k)
+{
+  if (k >= 4) __builtin_nontemporal_store(x, (GLOBAL f4any*)gptr(p));
+  else store_f4(p, x, k);
+}
+
 }  // namespace scadles
