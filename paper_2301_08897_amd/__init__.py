@@ -724,7 +724,7 @@ class AdamW:
         ``max_norm``), for ``step``; the factor is NaN when the norm is not
         finite. The tensor is the object's own and overwritten by the next call."""
         stream = self._order.enter(stream)
-        _check(_grad_norm(ctypes.byref(self._plan), float(max_norm), self.clip.data_ptr(), stream.cuda_stream))
+        _check(_grad_norm(self._plan, float(max_norm), self.clip.data_ptr(), stream.cuda_stream))
         return self.clip
 
     def step(self, lr: float, *, clip=None, stream=None):
@@ -735,7 +735,7 @@ class AdamW:
         o.lr, o.step = float(lr), self.t + 1
         if clip is not None and clip.numel() != 2:
             raise ValueError("clip must have two entries")
-        _check(_adamw_step(ctypes.byref(self._plan), ctypes.byref(o), None if clip is None else _dev_f32(clip, "clip"),
+        _check(_adamw_step(self._plan, o, None if clip is None else _dev_f32(clip, "clip"),
                            stream.cuda_stream))
         self.t += 1
 
@@ -780,8 +780,8 @@ class AdamW:
 
 @dataclass
 class RouterOutputs:
-    """What ``Router.forward`` returns (the router's own buffers, overwritten by
-    its next forward pass); ``shape`` is the call's, for the backward pass."""
+    """What ``Router.forward`` returns: the router's own buffers, overwritten by
+    its next forward pass."""
     idx: object          # int32 [T, k], -1 where there is no choice
     gate: object         # float32 [T, k]
     lse: object          # float32 [T]
@@ -789,7 +789,6 @@ class RouterOutputs:
     load: object         # float32 [experts]
     share: object        # float32 [devices]: 1 / counted rows
     loss: object         # float32 [2]: balance, z
-    shape: object
 
 
 class Router:
@@ -816,22 +815,33 @@ class Router:
         self.ws = _workspace(need, dev)
         self._out = RouterOut(*[x.data_ptr() for x in (self.idx, self.gate, self.lse, self.counts, self.load, self.share,
                                                        self.loss)])
+        self._off, self._w, self._w_back = (_u64 * (K + 1))(), (ctypes.c_float * K)(), (ctypes.c_float * K)()
+        self._off_view = np.frombuffer(self._off, dtype=np.uint64)
+        self._w_view, self._w_back_view = (np.frombuffer(w, dtype=np.float32) for w in (self._w, self._w_back))
+        self._shape, self._back_shape = (
+            RouterShape(0, E, self._off, w, E, self.k, K, 0, self.renormalise) for w in (self._w, self._w_back))
 
     def _logits(self, x, name):
+        """(address, elements between rows) of a [tokens, experts] tensor."""
         torch = _torch()
         if not isinstance(x, torch.Tensor) or not x.is_cuda or x.dtype not in (torch.float32, torch.bfloat16):
             raise TypeError(f"{name} must be a float32 or bfloat16 GPU tensor")
-        if x.dim() != 2 or x.shape[1] != self.experts or (x.shape[1] > 1 and x.stride(1) != 1):
-            raise ValueError(f"{name} must be [tokens, {self.experts}] with adjacent experts")
-        if x.shape[0] > 1 and x.stride(0) < self.experts:
+        if x.dim() != 2 or x.shape[1] != self.experts:
+            raise ValueError(f"{name} must be [tokens, {self.experts}]")
+        row, step = x.stride()
+        if self.experts > 1 and step != 1:
+            raise ValueError(f"{name}: a row's experts must be adjacent")
+        if x.shape[0] < 2:
+            row = self.experts
+        elif row < self.experts:
             raise ValueError(f"{name}: rows overlap")
-        return x.data_ptr(), x.stride(0) if x.shape[0] > 1 else self.experts
+        return x.data_ptr(), row
 
-    def _weights(self, weights):
-        w = np.ascontiguousarray(weights, dtype=np.float32)
-        if w.shape != (self.devices,):
-            raise ValueError("one weight per device")
-        return (ctypes.c_float * self.devices).from_buffer_copy(w)
+    @staticmethod
+    def _fill(view, values, name):
+        if len(values) != len(view):
+            raise ValueError(f"{name} must have {len(view)} entries")
+        view[:] = values
 
     def forward(self, logits, *, tok_off=None, weights=None, valid=None, stream=None) -> RouterOutputs:
         """``logits`` [T, experts] float32 or bfloat16, rows ``tok_off[d]`` to
@@ -843,50 +853,54 @@ class Router:
         T = logits.shape[0]
         if T > self.max_tokens:
             raise ValueError(f"more than max_tokens = {self.max_tokens} rows")
-        off = [0, T] if tok_off is None else tok_off
-        if len(off) != self.devices + 1:
-            raise ValueError("tok_off must have devices + 1 entries")
-        off = (_u64 * len(off))(*off)
+        self._fill(self._off_view, (0, T) if tok_off is None else tok_off, "tok_off")
         if weights is None:
-            weights = [(off[d + 1] - off[d]) / T if T else 1.0 / self.devices for d in range(self.devices)]
+            weights = np.diff(self._off_view.astype(np.int64)) / T if T else [1.0 / self.devices] * self.devices
+        self._fill(self._w_view, weights, "weights")
         if valid is not None:
             if valid.dtype not in (torch.bool, torch.uint8) or not valid.is_cuda or not valid.is_contiguous():
                 raise TypeError("valid must be a contiguous bool GPU tensor")
             if valid.numel() != T:
                 raise ValueError("valid must have one entry per row")
-        w = self._weights(weights)
-        shape = RouterShape(T, ld, off, w, self.experts, self.k, self.devices, logits.dtype == torch.bfloat16,
-                            self.renormalise)
-        _check(_router_forward(ctypes.byref(shape), p, None if valid is None else valid.data_ptr(),
-                               ctypes.byref(self._out), self.ws.data_ptr(), self.ws.numel(), _stream_ptr(stream)))
-        return RouterOutputs(self.idx[:T], self.gate[:T], self.lse[:T], self.counts, self.load, self.share, self.loss,
-                             shape)
+        f = self._shape
+        f.tokens, f.ld, f.logits_type = T, ld, logits.dtype == torch.bfloat16
+        _check(_router_forward(f, p, None if valid is None else valid.data_ptr(), self._out, self.ws.data_ptr(),
+                               self.ws.numel(), _stream_ptr(stream)))
+        if T == self.max_tokens:
+            return RouterOutputs(self.idx, self.gate, self.lse, self.counts, self.load, self.share, self.loss)
+        return RouterOutputs(self.idx[:T], self.gate[:T], self.lse[:T], self.counts, self.load, self.share, self.loss)
 
     def backward(self, logits, out: RouterOutputs, d_gate=None, d_loss=None, *, weights=None, d_logits=None, stream=None):
         """Gradient of ``logits`` under ``d_gate`` [T, k] (or None) of the gates and
-        ``d_loss`` [2] (or None) of the losses, both float32. ``weights``: as in the
-        forward pass by default; ones give each device's own share, before the
-        aggregation weights it. Returned in ``d_logits`` if given."""
+        ``d_loss`` [2] (or None) of the losses, both float32; ``out`` is the last
+        forward pass's. ``weights``: as in the forward pass by default; ones give
+        each device's own share, before the aggregation weights it. Returned in
+        ``d_logits`` if given."""
         torch = _torch()
         p, ld = self._logits(logits, "logits")
-        f, T = out.shape, logits.shape[0]
-        if out.load is not self.load:
-            raise ValueError("out is another router's")
+        f, T = self._shape, logits.shape[0]
+        if out.load is not self.load or out.lse.shape[0] != f.tokens:
+            raise ValueError("out is not this router's last forward pass")
         if T != f.tokens or f.logits_type != (logits.dtype == torch.bfloat16):
             raise ValueError("logits are not those of the forward pass")
-        for x, n, name in ((d_gate, T * self.k, "d_gate"), (d_loss, 2, "d_loss")):
-            if x is not None and x.numel() != n:
-                raise ValueError(f"{name} must have {n} entries")
+        if d_gate is not None and d_gate.numel() != T * self.k:
+            raise ValueError(f"d_gate must have {T * self.k} entries")
+        if d_loss is not None and d_loss.numel() != 2:
+            raise ValueError("d_loss must have 2 entries")
         if d_logits is None:
-            stream = torch.cuda.current_stream() if stream is None else stream
-            with torch.cuda.stream(stream):
+            if stream is None:
                 d_logits = torch.empty((T, self.experts), dtype=logits.dtype, device=logits.device)
+            else:
+                with torch.cuda.stream(stream):
+                    d_logits = torch.empty((T, self.experts), dtype=logits.dtype, device=logits.device)
         q, ld_out = self._logits(d_logits, "d_logits")
         if d_logits.dtype != logits.dtype or d_logits.shape[0] != T:
             raise ValueError("d_logits must be like logits")
-        shape = RouterShape(f.tokens, ld, f.tok_off, f.weights if weights is None else self._weights(weights), f.experts,
-                            f.k, f.devices, f.logits_type, f.renormalise)
-        _check(_router_backward(ctypes.byref(shape), p, ctypes.byref(self._out),
-                                None if d_gate is None else _dev_f32(d_gate, "d_gate"),
+        if weights is not None:
+            self._fill(self._w_back_view, weights, "weights")
+            f = self._back_shape
+            f.tokens, f.logits_type = T, self._shape.logits_type
+        f.ld = ld
+        _check(_router_backward(f, p, self._out, None if d_gate is None else _dev_f32(d_gate, "d_gate"),
                                 None if d_loss is None else _dev_f32(d_loss, "d_loss"), q, ld_out, _stream_ptr(stream)))
         return d_logits

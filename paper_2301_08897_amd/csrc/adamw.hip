@@ -42,9 +42,12 @@ namespace {
 constexpr uint32_t kMoment = SCADLES_MOMENT_BLOCK;
 constexpr uint32_t kPart = 4 * kBlock;     // elements of one workgroup's step: four per thread
 constexpr uint32_t kChunk = 2 * kPart;     // elements of one record of the plan
-// The norm's workgroups, at most: one per compute unit. Every workgroup counts
-// itself in at one address when it is done, which takes 10 ns each.
-constexpr uint32_t kNormBlocks = 256, kNormBlock = 1024, kNormWaves = kNormBlock / 64;
+// The norm's workgroups, at most: one per compute unit, of 1024 threads. Every
+// workgroup counts itself in at one address when it is done, which takes 10 ns
+// each (60 M floats: 47 us with 2048 workgroups of 256 threads, 40 us so). Where
+// 256 workgroups of 256 threads take one chunk per wave, they are quicker to
+// start (147 K floats: 4.4 us against 5.4).
+constexpr uint32_t kNormBlocks = 256, kNormBlock = 1024, kNormSmall = 256;
 constexpr uint32_t kPutTensors = 40;       // tensors of one launch's arguments
 constexpr uint32_t kMagic = 0x5C4D0001u;
 constexpr uint32_t kSpanM = 127, kSpanV = 255;
@@ -367,23 +370,24 @@ __global__ __launch_bounds__(kBlock) void k_adamw_moments(const Chunk* chunks, u
 // Squares and sums in double. Workgroups sum their chunks in order, the last
 // one to finish sums the workgroups' results in order, so the norm does not
 // depend on the order in which they run.
+template <int NT>
 __device__ inline double norm_block_sum(double v, double* lds)
 {
   v = wave_sum_f64(v);
   if (lane_id() == 0) lds[threadIdx.x >> 6] = v;
   __syncthreads();
-  v = lane_id() < kNormWaves ? lds[lane_id()] : 0.0;
+  v = lane_id() < NT / 64 ? lds[lane_id()] : 0.0;
   return wave_sum_f64(v);
 }
 
-template <class G>
-__global__ __launch_bounds__(kNormBlock) void k_grad_norm(const Chunk* chunks, uint32_t count, Head* head, double max_norm,
+template <class G, int NT>
+__global__ __launch_bounds__(NT) void k_grad_norm(const Chunk* chunks, uint32_t count, Head* head, double max_norm,
                                                           float* out)
 {
-  __shared__ double s_sum[2][kNormWaves];
+  __shared__ double s_sum[2][NT / 64];
   constexpr int kLoads = kChunk / 256;       // a wave takes a chunk, all of its loads at once
   double sum = 0.0;
-  for (uint32_t i = blockIdx.x * kNormWaves + wave_id(); i < count; i += gridDim.x * kNormWaves) {
+  for (uint32_t i = blockIdx.x * (NT / 64) + wave_id(); i < count; i += gridDim.x * (NT / 64)) {
     const G* g = (const G*)chunks[i].g + lane_id() * 4;
     const uint32_t n = chunks[i].n;
     f4 x[kLoads];
@@ -402,10 +406,12 @@ __global__ __launch_bounds__(kNormBlock) void k_grad_norm(const Chunk* chunks, u
 #pragma unroll
       for (int q = 0; q < 4; ++q) sum = __builtin_fma((double)x[j][q], (double)x[j][q], sum);
   }
-  sum = norm_block_sum(sum, s_sum[0]);
+  sum = norm_block_sum<NT>(sum, s_sum[0]);
   if (threadIdx.x == 0) put(&head->part[blockIdx.x], sum);
   if (!block_is_last(&head->ticket, 1u, gridDim.x)) return;
-  sum = norm_block_sum(threadIdx.x < gridDim.x ? get(&head->part[threadIdx.x]) : 0.0, s_sum[1]);
+  sum = 0.0;
+  for (uint32_t i = threadIdx.x; i < gridDim.x; i += NT) sum += get(&head->part[i]);
+  sum = norm_block_sum<NT>(sum, s_sum[1]);
   if (threadIdx.x) return;
   put(&head->ticket, 0u);
   const double norm = sqrt(sum);
@@ -446,6 +452,17 @@ void dithers(uint64_t step, uint32_t& um, uint32_t& uv)
 {
   um = (uint32_t)step * kWeylB;
   uv = (uint32_t)step * kWeylA;
+}
+
+template <class G>
+void launch_norm(const Chunk* chunks, uint32_t count, Head* head, double max_norm, float* clip, hipStream_t s)
+{
+  const uint64_t small = div_up(count, kNormSmall / 64), blocks = div_up(count, kNormBlock / 64);
+  if (small <= kNormBlocks)
+    k_grad_norm<G, kNormSmall><<<small < 1 ? 1 : (uint32_t)small, kNormSmall, 0, s>>>(chunks, count, head, max_norm, clip);
+  else
+    k_grad_norm<G, kNormBlock><<<blocks < kNormBlocks ? (uint32_t)blocks : kNormBlocks, kNormBlock, 0, s>>>(chunks, count, head,
+                                                                                                      max_norm, clip);
 }
 
 template <class G, bool kBits8>
@@ -531,11 +548,9 @@ scadles_status scadles_grad_norm(const scadles_adamw_plan* plan, double max_norm
   if (!clip || !is_aligned(clip, 4)) return fail(SCADLES_EINVAL, "clip must be 4-byte aligned and not NULL");
   hipStream_t s = static_cast<hipStream_t>(stream);
   const uint32_t count = (uint32_t)plan->chunks;
-  const uint64_t blocks = div_up(count, kNormWaves);
-  const uint32_t grid = blocks < 1 ? 1 : blocks < kNormBlocks ? (uint32_t)blocks : kNormBlocks;
   Head* head = static_cast<Head*>(plan->table);
-  if (plan->grad_type == SCADLES_BF16) k_grad_norm<uint16_t><<<grid, kNormBlock, 0, s>>>(chunks_of(plan), count, head, max_norm, clip);
-  else k_grad_norm<float><<<grid, kNormBlock, 0, s>>>(chunks_of(plan), count, head, max_norm, clip);
+  if (plan->grad_type == SCADLES_BF16) launch_norm<uint16_t>(chunks_of(plan), count, head, max_norm, clip, s);
+  else launch_norm<float>(chunks_of(plan), count, head, max_norm, clip, s);
   return launch_status(hipGetLastError(), "gradient norm");
 }
 
