@@ -609,23 +609,41 @@ def step_fused(grads, ratios, weights, *, delta: float = math.inf, params=None, 
 
 # ---- AdamW ----------------------------------------------------------------------------------------
 
+def _empty(shape, dtype, device, stream):
+    """Uninitialised memory that belongs to the stream (the current one for None)."""
+    torch = _torch()
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 class _Order:
-    """Orders calls on other streams after work that set an object up."""
+    """Orders an object's calls on other streams after the work that set its
+    buffers up, and tells the allocator that those streams use them."""
 
     def __init__(self):
-        self.event, self.ready = _torch().cuda.Event(), None
+        self.event, self.ready, self.seen, self.buffers = _torch().cuda.Event(), None, set(), ()
 
-    def record(self, stream):
+    def record(self, stream, buffers=None):
+        """The buffers are ready once the stream's work so far is done."""
         self.event.record(stream)
         self.ready = stream.cuda_stream
+        self.seen = {self.ready}
+        if buffers is not None:
+            self.buffers = buffers
 
     def enter(self, stream):
-        """The stream to run on (the current one for None), after the set-up."""
+        """The address of the stream to run on (the current one for None)."""
         if stream is None:
             stream = _torch().cuda.current_stream()
-        if stream.cuda_stream != self.ready:
+        p = stream.cuda_stream
+        if p not in self.seen:
             stream.wait_event(self.event)
-        return stream
+            for x in self.buffers:
+                x.record_stream(stream)
+            self.seen.add(p)
+        return p
 
 
 class AdamW:
@@ -712,31 +730,30 @@ class AdamW:
             if g.device != self.device or g.numel() != self.sizes[i]:
                 raise ValueError(f"grads[{i}] must be on the parameters' GPU and of their size")
             self._tensors[i].grad = g.data_ptr()
-        stream = self._order.enter(stream) if self._order.ready is not None else stream or torch.cuda.current_stream()
+        stream = torch.cuda.current_stream() if stream is None else stream
+        if self._order.ready is not None:
+            self._order.enter(stream)
         _check(_adamw_plan_build(self._tensors, len(grads), self.state_bits, 1 if grads[0].dtype == torch.bfloat16 else 0,
-                                 self._table.data_ptr(), self._table.numel(), ctypes.byref(self._plan),
-                                 stream.cuda_stream))
+                                 self._table.data_ptr(), self._table.numel(), self._plan, stream.cuda_stream))
         self.grads = grads
-        self._order.record(stream)
+        self._order.record(stream, [x for x in (self.m, self.v, self.tops, self._table, self.clip) if x is not None])
 
     def grad_norm(self, max_norm: float = math.inf, *, stream=None):
         """float32[2] = (global norm of the gradients, factor that clips it to
         ``max_norm``), for ``step``; the factor is NaN when the norm is not
         finite. The tensor is the object's own and overwritten by the next call."""
-        stream = self._order.enter(stream)
-        _check(_grad_norm(self._plan, float(max_norm), self.clip.data_ptr(), stream.cuda_stream))
+        _check(_grad_norm(self._plan, float(max_norm), self.clip.data_ptr(), self._order.enter(stream)))
         return self.clip
 
     def step(self, lr: float, *, clip=None, stream=None):
         """One step, with the gradients times clip[1] when given (as from
         ``grad_norm``; a NaN there leaves everything but ``t`` as it is)."""
-        stream = self._order.enter(stream)
         o = self._options
         o.lr, o.step = float(lr), self.t + 1
         if clip is not None and clip.numel() != 2:
             raise ValueError("clip must have two entries")
         _check(_adamw_step(self._plan, o, None if clip is None else _dev_f32(clip, "clip"),
-                           stream.cuda_stream))
+                           self._order.enter(stream)))
         self.t += 1
 
     def moments(self, *, stream=None):
@@ -744,11 +761,8 @@ class AdamW:
         themselves, or what the 8-bit codes stand for."""
         if self.state_bits == 32:
             return self.m, self.v
-        torch = _torch()
-        stream = self._order.enter(stream)
-        with torch.cuda.stream(stream):
-            m, v = (torch.empty(self.n, dtype=torch.float32, device=self.device) for _ in range(2))
-        _check(_adamw_get_moments(ctypes.byref(self._plan), m.data_ptr(), v.data_ptr(), stream.cuda_stream))
+        m, v = (_empty(self.n, _torch().float32, self.device, stream) for _ in range(2))
+        _check(_adamw_get_moments(self._plan, m.data_ptr(), v.data_ptr(), self._order.enter(stream)))
         return m, v
 
     def load(self, t: int, m, v, *, tops=None, stream=None):
@@ -757,7 +771,8 @@ class AdamW:
         torch = _torch()
         if t < 0:
             raise ValueError("t must not be negative")
-        stream = self._order.enter(stream)
+        stream = torch.cuda.current_stream() if stream is None else stream
+        self._order.enter(stream)
         if tops is not None:
             if self.state_bits != 8:
                 raise ValueError("tops belongs to 8-bit moments")
@@ -770,7 +785,7 @@ class AdamW:
         else:
             if m.numel() != self.n or v.numel() != self.n:
                 raise ValueError("m and v must hold every element")
-            _check(_adamw_set_moments(ctypes.byref(self._plan), _dev_f32(m, "m"), _dev_f32(v, "v"), int(t),
+            _check(_adamw_set_moments(self._plan, _dev_f32(m, "m"), _dev_f32(v, "v"), int(t),
                                       stream.cuda_stream))
         self.t = int(t)
         self._order.record(stream)
@@ -815,6 +830,9 @@ class Router:
         self.ws = _workspace(need, dev)
         self._out = RouterOut(*[x.data_ptr() for x in (self.idx, self.gate, self.lse, self.counts, self.load, self.share,
                                                        self.loss)])
+        self._order = _Order()
+        self._order.record(torch.cuda.current_stream(dev), [self.idx, self.gate, self.lse, self.counts, self.load,
+                                                            self.share, self.loss, self.ws])
         self._off, self._w, self._w_back = (_u64 * (K + 1))(), (ctypes.c_float * K)(), (ctypes.c_float * K)()
         self._off_view = np.frombuffer(self._off, dtype=np.uint64)
         self._w_view, self._w_back_view = (np.frombuffer(w, dtype=np.float32) for w in (self._w, self._w_back))
@@ -865,7 +883,7 @@ class Router:
         f = self._shape
         f.tokens, f.ld, f.logits_type = T, ld, logits.dtype == torch.bfloat16
         _check(_router_forward(f, p, None if valid is None else valid.data_ptr(), self._out, self.ws.data_ptr(),
-                               self.ws.numel(), _stream_ptr(stream)))
+                               self.ws.numel(), self._order.enter(stream)))
         if T == self.max_tokens:
             return RouterOutputs(self.idx, self.gate, self.lse, self.counts, self.load, self.share, self.loss)
         return RouterOutputs(self.idx[:T], self.gate[:T], self.lse[:T], self.counts, self.load, self.share, self.loss)
@@ -888,11 +906,7 @@ class Router:
         if d_loss is not None and d_loss.numel() != 2:
             raise ValueError("d_loss must have 2 entries")
         if d_logits is None:
-            if stream is None:
-                d_logits = torch.empty((T, self.experts), dtype=logits.dtype, device=logits.device)
-            else:
-                with torch.cuda.stream(stream):
-                    d_logits = torch.empty((T, self.experts), dtype=logits.dtype, device=logits.device)
+            d_logits = _empty((T, self.experts), logits.dtype, logits.device, stream)
         q, ld_out = self._logits(d_logits, "d_logits")
         if d_logits.dtype != logits.dtype or d_logits.shape[0] != T:
             raise ValueError("d_logits must be like logits")
@@ -902,5 +916,6 @@ class Router:
             f.tokens, f.logits_type = T, self._shape.logits_type
         f.ld = ld
         _check(_router_backward(f, p, self._out, None if d_gate is None else _dev_f32(d_gate, "d_gate"),
-                                None if d_loss is None else _dev_f32(d_loss, "d_loss"), q, ld_out, _stream_ptr(stream)))
+                                None if d_loss is None else _dev_f32(d_loss, "d_loss"), q, ld_out,
+                                self._order.enter(stream)))
         return d_logits

@@ -632,8 +632,8 @@ __global__ __launch_bounds__(kBlock) void k_route_back(Rows r, const X* logits, 
     mean = group_sum<G>(mean);
     float part = 0.0f;
     if (dgate) {
-      for (uint32_t c = l; c < r.k; c += G)
-        if (on) part += o.gate[row * r.k + c] * dgate[row * r.k + c];
+      for (uint32_t c = l; c < r.k; c += G)    // what is given for a choice that is missing does not count
+        if (on && o.idx[row * r.k + c] >= 0) part += o.gate[row * r.k + c] * dgate[row * r.k + c];
       part = group_sum<G>(part);
       for (uint32_t c = l; c < r.k; c += G) {
         const int32_t e = on ? o.idx[row * r.k + c] : -1;

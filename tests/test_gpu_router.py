@@ -153,6 +153,51 @@ def test_masks_that_leave_nothing(sc):
 
 
 @pytest.mark.parametrize("renormalise", [False, True])
+def test_garbage_in_masked_places(sc, renormalise):
+    """NaN and infinities in the logits of padding, and in the gradients of
+    choices that are missing, change nothing."""
+    torch, dev = torch_dev()
+    T, E, k = 300, 60, 4
+    rng = np.random.default_rng(10)
+    x = torch.from_numpy(logits(T, E, "normal", rng)).to(dev)
+    x[::7, 2:] = -math.inf                            # two experts left for four choices
+    valid = torch.from_numpy(rng.random(T) < 0.7).to(dev)
+    dg, dl = torch.from_numpy(rng.normal(0, 1, (T, k)).astype(np.float32)).to(dev), torch.ones(2, device=dev)
+    r, q = (sc.Router(T, E, k, renormalise=renormalise) for _ in range(2))
+    f = r.forward(x, valid=valid)
+    dx = r.backward(x, f, torch.where(f.idx >= 0, dg, 0.0), dl)
+    y = x.clone()
+    y[~valid] = torch.tensor([math.nan, math.inf, -math.inf], device=dev).repeat(E // 3)
+    g = q.forward(y, valid=valid)
+    for bad in (math.nan, math.inf):
+        dy = q.backward(y, g, torch.where(g.idx >= 0, dg, bad), dl)
+        assert torch.equal(dx, dy) and bool(torch.isfinite(dx).all()) and not bool(dx[~valid].any())
+    for n in ("idx", "gate", "lse", "counts", "load", "share", "loss"):
+        assert torch.equal(getattr(f, n), getattr(g, n)), n
+
+
+def test_rows_do_not_depend_on_their_neighbours(sc):
+    """A row's choices, gates and gradient are the same bits wherever it lies."""
+    torch, dev = torch_dev()
+    for E, k in ((8, 2), (60, 4), (256, 8), (700, 12)):
+        rng = np.random.default_rng(E)
+        row = torch.from_numpy(logits(1, E, "normal", rng)).to(dev)
+        dg = torch.ones(1, k, device=dev)
+        r = sc.Router(100, E, k)
+        f = r.forward(row)
+        want = [x.clone() for x in (f.idx, f.gate, f.lse, r.backward(row, f, dg))]
+        x = torch.from_numpy(logits(100, E, "masked", rng)).to(dev)
+        x[10:20] = float(np.finfo(np.float32).min)
+        x[20:30, 1] = math.inf
+        x[30:40] *= 1e3
+        x[5::9] = row
+        f = r.forward(x)
+        dx = r.backward(x, f, torch.ones(100, k, device=dev))
+        for a, b in zip(want, (f.idx, f.gate, f.lse, dx)):
+            assert torch.equal(a.expand_as(b[5::9]) if b.dim() > 1 else a.expand(b[5::9].shape), b[5::9]), (E, k)
+
+
+@pytest.mark.parametrize("renormalise", [False, True])
 @pytest.mark.parametrize("bad", [math.nan, math.inf])
 def test_not_finite(sc, bad, renormalise):
     """A row with a NaN or +infinity is NaN where it is computed, and nowhere else."""
