@@ -12,7 +12,7 @@
 //   which is gate (dgate - sum gate dgate) over S, or p (dgate over S - sum gate dgate).
 //
 // Both directions read the logits once. A row lies in the registers of a group
-// of G lanes, V elements each, so that its maximum, sums and choices are a few
+// of G lanes, V elements each (see with_shape), so that its maximum, sums and choices are a few
 // lane exchanges; a workgroup takes several rounds of 256 / G rows of one
 // device and keeps the experts' probability sums in registers meanwhile.
 #include <cmath>
@@ -31,7 +31,8 @@ constexpr uint32_t kMaxChoices = SCADLES_ROUTER_MAX_K;
 constexpr uint32_t kMaxExperts = SCADLES_ROUTER_MAX_EXPERTS;
 constexpr uint32_t kFinishExperts = 16;    // experts of one workgroup of k_route_finish
 constexpr int kFinishBlock = 1024;
-constexpr uint32_t kFewFrom = 3;           // choices from which they are made by a threshold
+constexpr int kFewLanes = 16;              // lanes per row from which choices are made by a threshold,
+constexpr uint32_t kFewFrom = 3;           // if there are so many (see choose_few)
 constexpr uint32_t kRouteBlocks = 1024;    // workgroups, at most, unless they would take
 constexpr uint32_t kBackBlocks = 1280;     // the same for the backward pass, which has no sums
 constexpr uint32_t kMaxRounds = 256;       // more rounds each than this: they sum probabilities in float
@@ -133,6 +134,18 @@ __device__ inline uint32_t group_min(uint32_t x)
   return __float_as_uint(group_reduce<G>(__uint_as_float(x),
                                          [&](float a, auto ctrl) { return least(__float_as_uint(a), dpp<ctrl>(__float_as_uint(a))); },
                                          [&](float a, float b) { return least(__float_as_uint(a), __float_as_uint(b)); }));
+}
+
+// The sum of x over the lanes of a row of 16 that have the same place in their group.
+template <int G>
+__device__ inline float sum_over_row(float x)
+{
+  auto add = [](float a, uint32_t b) { return a + __uint_as_float(b); };
+  if constexpr (G <= 8) x = add(x, dpp<0x128>(__float_as_uint(x)));    // turned by 8 lanes, by 4
+  if constexpr (G <= 4) x = add(x, dpp<0x124>(__float_as_uint(x)));
+  if constexpr (G <= 2) x = add(x, dpp<0x4E>(__float_as_uint(x)));
+  if constexpr (G <= 1) x = add(x, dpp<0xB1>(__float_as_uint(x)));
+  return x;
 }
 
 __device__ inline float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
@@ -370,16 +383,18 @@ __global__ __launch_bounds__(kFinishBlock) void k_route_finish(Rows r, Parts s, 
 template <int G, int V>
 struct RouteLds {
   static constexpr int kGroups = kBlock / G;
+  static constexpr int kChoices = G * V < (int)kMaxChoices ? G * V : (int)kMaxChoices;
   uint32_t count[G * V];
   alignas(16) float row[kGroups][G * V];     // the groups' rows, at the end the groups' probability sums
-  uint32_t idx[kGroups][kMaxChoices];
-  float ex[kGroups][kMaxChoices];
-  double z[kGroups];
-  uint32_t rows[kGroups];
-  alignas(16) float top[kGroups][G];
-  alignas(16) uint64_t few[kGroups][G];
-  uint32_t at[kGroups][G];
-  uint32_t nfew[kGroups];
+  uint32_t idx[kGroups][kChoices];
+  float ex[kGroups][kChoices];
+  double z[kWaves];
+  uint32_t rows[kWaves];
+  static constexpr int kFewGroups = G >= kFewLanes ? kGroups : 1;      // of the choice by a threshold
+  alignas(16) float top[kFewGroups][G];
+  alignas(16) uint64_t few[kFewGroups][G];
+  uint32_t at[kFewGroups][G];
+  uint32_t nfew[kFewGroups];
 };
 
 // The k choices of every group's row of the wave, one after the other: k rounds
@@ -420,6 +435,9 @@ __device__ inline void choose_in_turn(float (&x)[V], float mx, const Exp& ex, ui
 // on average for 8 of 16 lanes, standard deviation 2). Comparisons are taken
 // from the sign of a difference and gathered bit by bit: a compare's result
 // would have to be waited for.
+// 2^25 logits by 3, 4 and 8 choices so, and in turn: 49, 49, 55 and 53, 60, 92 us
+// for 128 experts, 38, 38, 44 and 43, 49, 72 for 256, 42, 42, 42 and 45, 51, 75
+// for 512, 52, 51, 52 and 48, 54, 82 for 1024; two choices, 38 to 52 and 38 to 45.
 template <int G, int V>
 __device__ inline bool choose_few(const float (&x)[V], float top, const Exp& ex, uint32_t k, uint32_t l, uint32_t group, RouteLds<G, V>& m)
 {
@@ -527,8 +545,11 @@ __global__ __launch_bounds__(kBlock, kOne ? 1 : V >= 16 ? 4 : 5) void k_route(Ro
 #pragma unroll
     for (int i = 0; i < V; ++i) acc[i] = __builtin_fmaf(p[i], inv, acc[i]);
     z += (double)lse * (double)lse;
-    rows += counted ? 1u : 0u;
-    if (!(G >= 16 && r.k >= kFewFrom && 2 * r.k <= G && choose_few<G, V>(x, top, ex, r.k, l, group, m)))
+    rows += (uint32_t)__builtin_popcountll(__ballot(counted)) / G;          // of the wave
+    bool done = false;
+    if constexpr (G >= kFewLanes)
+      if (r.k >= kFewFrom && 2 * r.k <= G) done = choose_few<G, V>(x, top, ex, r.k, l, group, m);
+    if (!done)
       choose_in_turn<G, V>(x, mx, ex, r.k, l4, group, m);
     wave_sync();
     float chosen = 0.0f;
@@ -547,34 +568,35 @@ __global__ __launch_bounds__(kBlock, kOne ? 1 : V >= 16 ? 4 : 5) void k_route(Ro
     }
     wave_sync();
   }
+  // the experts' sums of every 16 lanes (of a group, where it has more), then of the workgroup
+  constexpr int kLanes = G < 16 ? 16 : G, kSums = kBlock / kLanes;
 #pragma unroll
-  for (int i = 0; i < V; ++i) m.row[group][expert_at<G>(i) + l4] = acc[i];
-  if (l == 0) {
-    m.z[group] = z;
-    m.rows[group] = rows;
+  for (int i = 0; i < V; ++i) {
+    acc[i] = sum_over_row<G>(acc[i]);
+    if (tid % kLanes < G) m.row[tid / kLanes][expert_at<G>(i) + l4] = acc[i];
+  }
+  z = wave_sum_f64(l == 0 ? z : 0.0);
+  if (lane_id() == 0) {
+    m.z[wave_id()] = z;
+    m.rows[wave_id()] = rows;
   }
   __syncthreads();
-  double zs = 0.0, n = 0.0;
-  if (tid < 64) {
-    zs = wave_sum_f64(tid < kGroups ? m.z[tid] : 0.0);
-    n = wave_sum_f64(tid < kGroups ? (double)m.rows[tid] : 0.0);
-    if constexpr (kOne) {
-      if (tid == 0) m.z[0] = n;
-    } else if (tid == 0) {
-      s.z[blockIdx.x] = zs;
-      s.rows[blockIdx.x] = (uint32_t)n;
-    }
+  double zs = 0.0, balance = 0.0;
+  uint32_t n = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    zs += m.z[w];
+    n += m.rows[w];
   }
-  if constexpr (kOne) __syncthreads();
-  double scale = 0.0, balance = 0.0;
-  if constexpr (kOne) {
-    n = m.z[0];
-    scale = n > 0.0 ? (double)r.w[mine.d] / n : 0.0;
+  if (!kOne && tid == 0) {
+    s.z[blockIdx.x] = zs;
+    s.rows[blockIdx.x] = n;
   }
+  const double scale = kOne && n ? (double)r.w[mine.d] / (double)n : 0.0;
   for (uint32_t e = tid; e < r.E; e += kBlock) {
     float sum = 0.0f;
 #pragma unroll 4
-    for (int g = 0; g < kGroups; ++g) sum += m.row[g][e];
+    for (int g = 0; g < kSums; ++g) sum += m.row[g][e];
     if constexpr (kOne) {
       const double load = scale * (double)m.count[e] / (double)r.k;
       balance += load * scale * (double)sum * (double)r.E;
@@ -585,7 +607,7 @@ __global__ __launch_bounds__(kBlock, kOne ? 1 : V >= 16 ? 4 : 5) void k_route(Ro
     }
   }
   if constexpr (kOne) {        // the only workgroup: it makes the sums over all rows itself
-    for (uint32_t d = tid; d < r.K; d += kBlock) o.share[d] = d == mine.d && n > 0.0 ? (float)(1.0 / n) : 0.0f;
+    for (uint32_t d = tid; d < r.K; d += kBlock) o.share[d] = d == mine.d && n ? 1.0f / (float)n : 0.0f;
     __shared__ double s_sum[kWaves];
     balance = block_sum_f64(balance, s_sum);
     if (tid == 0) {
@@ -670,23 +692,61 @@ __global__ __launch_bounds__(kBlock) void k_route_back(Rows r, const X* logits, 
 }
 
 // ---- host side ------------------------------------------------------------------------------------
-// Lanes per row and elements per lane for E experts.
-template <class F>
-void with_shape(uint32_t E, F f)
+// Lanes per row and elements per lane. The more elements a lane has, the fewer
+// exchanges and rounds of choosing per row; the more lanes, the better their
+// loads lie together, and from kFewLanes on choices can be made by a threshold.
+// Forward with 2 choices, 2^25 logits: 8 experts by 1, 2 and 4 lanes 57, 68 and
+// 114 us; 16 by 1, 2 and 4: 64, 50, 63; 32 by 2, 4 and 8: 60, 48, 62; 64 by 4, 8
+// and 16: 41, 45, 63; 128 by 8 and 16: 37, 45; with 8 choices 128 by 8 and 16: 71,
+// 55; 256 by 16 and 32: 38, 47. Backward (8 choices) 8 experts by 1, 2 and 4 lanes
+// 486, 292 and 307 us; 16 by 1, 2 and 4: 280, 168, 173; 32 by 2, 4 and 8: 118, 89,
+// 111; 64 by 4, 8 and 16: 69, 68, 111; 128 by 8 and 16: 54, 68; 256 by 16 and 32:
+// 53, 68.
+template <int G, int V, class F>
+void shape(F f)
 {
-  if (E <= 16) f(std::integral_constant<int, 4>(), std::integral_constant<int, 4>());
-  else if (E <= 32) f(std::integral_constant<int, 8>(), std::integral_constant<int, 4>());
-  else if (E <= 64) f(std::integral_constant<int, 16>(), std::integral_constant<int, 4>());
-  else if (E <= 128) f(std::integral_constant<int, 16>(), std::integral_constant<int, 8>());
-  else if (E <= 256) f(std::integral_constant<int, 16>(), std::integral_constant<int, 16>());
-  else if (E <= 512) f(std::integral_constant<int, 32>(), std::integral_constant<int, 16>());
-  else f(std::integral_constant<int, 64>(), std::integral_constant<int, 16>());
+  f(std::integral_constant<int, G>(), std::integral_constant<int, V>());
 }
 
-uint32_t rows_per_round(uint32_t E)
+template <class F>
+void with_shape(uint32_t E, uint32_t k, F f)
+{
+  if (E <= 8) shape<1, 8>(f);
+  else if (E <= 16) shape<2, 8>(f);
+  else if (E <= 32) shape<4, 8>(f);
+  else if (E <= 64) shape<4, 16>(f);
+  else if (E <= 128 && k <= 4) shape<8, 16>(f);
+  else if (E <= 128) shape<16, 8>(f);
+  else if (E <= 256) shape<16, 16>(f);
+  else if (E <= 512) shape<32, 16>(f);
+  else shape<64, 16>(f);
+}
+
+template <class F>
+void with_back_shape(uint32_t E, F f)
+{
+  if (E <= 8) shape<2, 4>(f);
+  else if (E <= 16) shape<2, 8>(f);
+  else if (E <= 32) shape<4, 8>(f);
+  else if (E <= 64) shape<4, 16>(f);
+  else if (E <= 128) shape<8, 16>(f);
+  else if (E <= 256) shape<16, 16>(f);
+  else if (E <= 512) shape<32, 16>(f);
+  else shape<64, 16>(f);
+}
+
+// Rows that a workgroup takes at once.
+uint32_t round_of(uint32_t E, uint32_t k)
 {
   uint32_t n = 0;
-  with_shape(E, [&](auto g, auto) { n = kBlock / g; });
+  with_shape(E, k, [&](auto g, auto) { n = kBlock / g; });
+  return n;
+}
+
+uint32_t back_round_of(uint32_t E)
+{
+  uint32_t n = 0;
+  with_back_shape(E, [&](auto g, auto) { n = kBlock / g; });
   return n;
 }
 
@@ -700,9 +760,9 @@ uint32_t blocks_for(const scadles_router* q, uint64_t per)
 // Rows of one workgroup, so that at most kRouteBlocks workgroups share them: that
 // many fit the GPU at once, and a few more make the call take nearly twice as
 // long. At least a round, then as many rows more as a wave takes at once.
-uint64_t rows_for(const scadles_router* q, uint32_t blocks)
+uint64_t rows_for(const scadles_router* q, uint64_t round, uint32_t blocks)
 {
-  const uint64_t round = rows_per_round(q->experts), unit = round / kWaves, most = round * kMaxRounds;
+  const uint64_t unit = round / kWaves, most = round * kMaxRounds;
   uint64_t n = div_up(div_up(q->tokens, blocks), round) * round;
   if (n >= 4 * round) n = div_up(div_up(q->tokens, blocks), unit) * unit;
   if (n < round) n = round;
@@ -732,10 +792,10 @@ scadles_status check_router(const scadles_router* q)
 }
 
 // What the kernels need to know of the rows; returns the workgroups.
-uint32_t make_rows(const scadles_router* q, uint32_t blocks, Rows& r)
+uint32_t make_rows(const scadles_router* q, uint32_t round, uint32_t blocks, Rows& r)
 {
   std::memset(&r, 0, sizeof(r));
-  r.per = (uint32_t)rows_for(q, blocks);
+  r.per = (uint32_t)rows_for(q, round, blocks);
   r.E = q->experts;
   r.k = q->k;
   r.K = q->devices;
@@ -802,7 +862,7 @@ uint64_t span_bytes(const scadles_router* q, uint64_t ld)
 template <class X>
 hipError_t launch_route(const Rows& r, const void* logits, const uint8_t* valid, const RouteOut& o, const Parts& s, hipStream_t st)
 {
-  with_shape(r.E, [&](auto g, auto v) {
+  with_shape(r.E, r.k, [&](auto g, auto v) {
     if (s.W == 1) k_route<X, g, v, true><<<1, kBlock, 0, st>>>(r, (const X*)logits, valid, o, s);
     else k_route<X, g, v, false><<<s.W, kBlock, 0, st>>>(r, (const X*)logits, valid, o, s);
   });
@@ -814,7 +874,7 @@ template <class X>
 hipError_t launch_back(const Rows& r, uint32_t W, const void* logits, const RouteOut& o, const float* dgate, const float* dloss,
                        void* dlogits, uint64_t ld_out, hipStream_t st)
 {
-  with_shape(r.E, [&](auto g, auto v) {
+  with_back_shape(r.E, [&](auto g, auto v) {
     k_route_back<X, g, v><<<W, kBlock, 0, st>>>(r, (const X*)logits, o, dgate, dloss, (X*)dlogits, ld_out);
   });
   return hipGetLastError();
@@ -833,7 +893,9 @@ size_t scadles_router_workspace_bytes(uint64_t tokens, uint32_t experts, uint32_
 {
   if (tokens > 0x7FFFFFFFull || !experts || experts > kMaxExperts || !devices || devices > kMaxK) return 0;
   // the most workgroups of any call of so many rows or fewer; every device's last one may be partly filled
-  const uint64_t round = rows_per_round(experts), few = tokens / round + devices;
+  uint64_t round = round_of(experts, 1);       // the fewest rows of any k
+  if (round_of(experts, kMaxChoices) < round) round = round_of(experts, kMaxChoices);
+  const uint64_t few = tokens / round + devices;
   const uint64_t many = tokens / (round * kMaxRounds) + devices;
   const uint64_t W = few < kRouteBlocks ? few : many > kRouteBlocks ? many : kRouteBlocks;
   Parts s;
@@ -854,7 +916,7 @@ scadles_status scadles_router_forward(const scadles_router* router, const void* 
   if (!is_aligned(logits, esize)) return fail(SCADLES_EINVAL, "logits is not aligned to its elements");
   Rows r;
   Parts s;
-  const uint32_t W = make_rows(router, kRouteBlocks, r);
+  const uint32_t W = make_rows(router, round_of(router->experts, router->k), kRouteBlocks, r);
   const uint64_t need = lay_out(W, router->experts, static_cast<char*>(ws), s);
   if (!ws || !is_aligned(ws, 256)) return fail(SCADLES_EWORKSPACE, "workspace must be 256-byte aligned and not NULL");
   if (ws_bytes < need) return fail(SCADLES_EWORKSPACE, "workspace has %zu bytes, needs %zu", ws_bytes, (size_t)need);
@@ -896,7 +958,7 @@ scadles_status scadles_router_backward(const scadles_router* router, const void*
   for (int x = 0; x < 8; ++x)
     if (bytes_overlap(dlogits, bytes, ins[x], sizes[x])) return fail(SCADLES_EINVAL, "dlogits overlaps an input");
   Rows r;
-  const uint32_t W = make_rows(router, kBackBlocks, r);
+  const uint32_t W = make_rows(router, back_round_of(router->experts), kBackBlocks, r);
   if (W == 0) return SCADLES_OK;
   hipStream_t st = static_cast<hipStream_t>(stream);
   const RouteOut o = outputs(out);
