@@ -44,9 +44,9 @@ constexpr uint32_t kPart = 4 * kBlock;     // elements of one workgroup's step: 
 constexpr uint32_t kChunk = 2 * kPart;     // elements of one record of the plan
 // The norm's workgroups, at most: one per compute unit, of 1024 threads. Every
 // workgroup counts itself in at one address when it is done, which takes 10 ns
-// each (60 M floats: 47 us with 2048 workgroups of 256 threads, 40 us so). Where
+// each (60 M floats: 48 us with 2048 workgroups of 256 threads, 40 us so). Where
 // 256 workgroups of 256 threads take one chunk per wave, they are quicker to
-// start (147 K floats: 4.4 us against 5.4).
+// start (147 K floats: 4.6 us against 5.4).
 constexpr uint32_t kNormBlocks = 256, kNormBlock = 1024, kNormSmall = 256;
 constexpr uint32_t kPutTensors = 40;       // tensors of one launch's arguments
 constexpr uint32_t kMagic = 0x5C4D0001u;
