@@ -12,9 +12,10 @@
 //   which is gate (dgate - sum gate dgate) over S, or p (dgate over S - sum gate dgate).
 //
 // Both directions read the logits once. A row lies in the registers of a group
-// of G lanes, V elements each (see with_shape), so that its maximum, sums and choices are a few
-// lane exchanges; a workgroup takes several rounds of 256 / G rows of one
-// device and keeps the experts' probability sums in registers meanwhile.
+// of G lanes, V elements each (see with_shape), so that its maximum, sums and
+// choices are a few lane exchanges; a workgroup takes several rounds of 256 / G
+// rows of one device and keeps the experts' probability sums in registers
+// meanwhile.
 #include <cmath>
 #include <cstring>
 #include <type_traits>
@@ -462,7 +463,8 @@ __device__ inline bool choose_few(const float (&x)[V], float top, const Exp& ex,
     }
     above += __builtin_popcount(bits);
   }
-  const float least = group_least<G>(above < k ? top : __builtin_inff());
+  float least = group_least<G>(above < k ? top : __builtin_inff());
+  least = least == 0.0f ? -0.0f : least;                   // so that x - least is no -0 for an x of -0
   uint32_t below = 0;
 #pragma unroll
   for (int i = V - 1; i >= 0; --i) below = append(below, x[i] - least);      // bit i: element i

@@ -33,6 +33,8 @@ def bounds(T, K, rng):
 
 def logits(T, E, kind, rng):
     x = rng.normal(0, 1.5, (T, E))
+    if kind == "zeros":                         # a few other values, then zeros of either sign
+        x = np.where(rng.random((T, E)) < rng.choice([0.0, 0.01, 0.05], (T, 1)), x, np.where(rng.random((T, E)) < 0.5, 0.0, -0.0))
     if kind == "ties":
         x = np.round(x * 2) / 2 + 0.0 * x
         x[rng.random((T, E)) < 0.1] = -0.0
@@ -113,9 +115,9 @@ def test_shapes(sc, shape, bf16):
 
 
 @pytest.mark.parametrize("bf16", [False, True])
-@pytest.mark.parametrize("kind", ["ties", "masked", "lowest", "large"])
-@pytest.mark.parametrize("shape", [(5, 3, 3, 2), (300, 16, 16, 4), (1000, 60, 4, 8), (400, 255, 16, 3), (100, 500, 8, 2), (71, 1024, 3, 1)],
-                         ids=str)
+@pytest.mark.parametrize("kind", ["ties", "masked", "lowest", "large", "zeros"])
+@pytest.mark.parametrize("shape", [(5, 3, 3, 2), (300, 16, 16, 4), (1000, 60, 4, 8), (400, 255, 16, 3), (100, 500, 8, 2), (71, 1024, 3, 1),
+                                   (600, 100, 8, 2), (600, 200, 3, 2)], ids=str)
 def test_values(sc, shape, kind, bf16):
     log(f"router {kind} {shape} bf16={bf16}")
     for renormalise in (False, True):
