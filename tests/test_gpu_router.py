@@ -33,8 +33,9 @@ def bounds(T, K, rng):
 
 def logits(T, E, kind, rng):
     x = rng.normal(0, 1.5, (T, E))
-    if kind == "zeros":                         # a few other values, then zeros of either sign
-        x = np.where(rng.random((T, E)) < rng.choice([0.0, 0.01, 0.05], (T, 1)), x, np.where(rng.random((T, E)) < 0.5, 0.0, -0.0))
+    if kind == "zeros":                         # a few other values, then zeros, half or few of them positive
+        sign = rng.random((T, E)) < rng.choice([0.02, 0.05, 0.5], (T, 1))
+        x = np.where(rng.random((T, E)) < rng.choice([0.0, 0.01], (T, 1)), x, np.where(sign, 0.0, -0.0))
     if kind == "ties":
         x = np.round(x * 2) / 2 + 0.0 * x
         x[rng.random((T, E)) < 0.1] = -0.0
