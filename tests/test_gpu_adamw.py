@@ -356,3 +356,29 @@ def test_after_the_aggregation(sc):
     assert np.array_equal(got == 0, dense == 0)
     big = np.abs(dense) > 1e-4                      # the first step moves by lr towards -sign(g)
     assert np.allclose(got[big], -0.5 * np.sign(dense[big]), rtol=1e-3)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_more_than_2_to_32_bytes(sc, bits):
+    """A tensor whose offsets pass 32 bits: its end is updated as a short tensor is."""
+    torch, dev = torch_dev()
+    n, tail = 2**30 + 2**20 + 3, 2**20 + 3                    # the tail starts a block of 8-bit moments
+    log(f"adamw n={n} bits={bits}")
+    p, g = torch.zeros(n, device=dev), torch.zeros(n, device=dev)
+    rng = np.random.default_rng(19)
+    g[-tail:] = torch.from_numpy(rng.normal(0, 1e-3, tail).astype(np.float32)).to(dev)
+    q, h = p[-tail:].clone(), g[-tail:].clone()
+    a = sc.AdamW([p], [g], state_bits=bits)
+    b = sc.AdamW([q], [h], state_bits=bits)
+    x, y = a.grad_norm(1e-2).tolist(), b.grad_norm(1e-2).tolist()
+    assert abs(x[0] / y[0] - 1) <= 4 * U
+    a.step(1e-3)
+    b.step(1e-3)
+    assert torch.equal(p[-tail:], q) and not bool(p[:-tail].any())
+    m, v = a.moments()
+    if bits == 32:                                            # the dither of 8 bits goes by the element's number
+        assert torch.equal(m[-tail:], b.m) and torch.equal(v[-tail:], b.v)
+    else:
+        m1, v1 = b.moments()
+        assert float((m[-tail:] / m1 - 1).abs().nan_to_num().max()) <= 0.3 and bool((v[-tail:] > 0).eq(v1 > 0).all())
+    assert not bool(m[:-tail].any()) and not bool(v[:-tail].any())

@@ -310,3 +310,32 @@ def test_graph(sc):
             for a in ("idx", "gate", "lse", "counts", "load", "loss"):
                 assert torch.equal(getattr(f, a), getattr(g, a)), (i, a)
             assert torch.equal(dx, dy)
+
+
+def test_more_than_2_to_32_logits(sc):
+    """Rows whose offsets pass 32 bits, in more workgroups than one launch usually has."""
+    torch, dev = torch_dev()
+    B, E, k, times = 4096, 64, 2, 16_400
+    log(f"router {B * times} x {E}")
+    block = torch.from_numpy(logits(B, E, "normal", np.random.default_rng(11))).to(dev).to(torch.bfloat16)
+    x = block.repeat(times, 1)
+    T = x.shape[0]
+    assert T * E > 2**32
+    small = sc.Router(B, E, k)
+    f = small.forward(block)
+    dg = torch.ones(B, k, device=dev)
+    dl = torch.ones(2, device=dev)
+    dx = small.backward(block, f, dg, dl)
+    r = sc.Router(T, E, k, devices=2)
+    off = [0, B * 5000, T]
+    g = r.forward(x, tok_off=off)
+    for lo in (0, B * 5000, T - B):
+        assert torch.equal(g.idx[lo:lo + B], f.idx) and torch.equal(g.gate[lo:lo + B], f.gate) and torch.equal(g.lse[lo:lo + B], f.lse)
+    assert torch.equal(g.counts[0], f.counts[0] * 5000) and torch.equal(g.counts[1], f.counts[0] * (times - 5000))
+    assert torch.allclose(g.load, f.load, rtol=1e-6) and torch.allclose(g.loss, f.loss, rtol=1e-5)
+    # the losses' part is times as small per row: without it the gradient is the block's own
+    own = small.backward(block, f, dg, None)
+    dy = r.backward(x, g, dg.repeat(times, 1), None)
+    for lo in (0, B * 5000, T - B):
+        assert torch.equal(dy[lo:lo + B], own)
+    assert not torch.equal(dx, own)
