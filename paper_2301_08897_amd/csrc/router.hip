@@ -33,7 +33,7 @@ constexpr uint32_t kMaxExperts = SCADLES_ROUTER_MAX_EXPERTS;
 constexpr uint32_t kFinishExperts = 16;    // experts of one workgroup of k_route_finish
 constexpr int kFinishBlock = 1024;
 constexpr int kFewLanes = 16;              // lanes per row from which choices are made by a threshold,
-constexpr uint32_t kFewFrom = 3;           // if there are so many (see choose_few)
+constexpr uint32_t few_from(int G) { return G < 64 ? 3 : 4; }    // if there are so many (see choose_few)
 constexpr uint32_t kRouteBlocks = 1024;    // workgroups, at most, unless they would take
 constexpr uint32_t kBackBlocks = 1280;     // the same for the backward pass, which has no sums
 constexpr uint32_t kMaxRounds = 256;       // more rounds each than this: they sum probabilities in float
@@ -416,9 +416,11 @@ __device__ inline void choose_in_turn(float (&x)[V], float mx, const Exp& ex, ui
     for (int i = V - 1; i >= 0; --i) mine = x[i] == top ? (uint32_t)i : mine;
     const uint32_t e = mine < (uint32_t)V ? expert_of<G>(mine, l4) : ~0u, at = group_min<G>(e);
     const bool some = top > -__builtin_inff() && at != ~0u;
-    if (e != at) mine = V;
+    if (c + 1 < k) {
+      if (e != at) mine = V;
 #pragma unroll
-    for (int i = 0; i < V; ++i) x[i] = (uint32_t)i == mine ? -__builtin_inff() : x[i];
+      for (int i = 0; i < V; ++i) x[i] = (uint32_t)i == mine ? -__builtin_inff() : x[i];
+    }
     if (l4 == 0) {
       m.idx[group][c] = some ? at : ~0u;
       m.ex[group][c] = some ? ex(top) : 0.0f;
@@ -436,9 +438,9 @@ __device__ inline void choose_in_turn(float (&x)[V], float mx, const Exp& ex, ui
 // on average for 8 of 16 lanes, standard deviation 2). Comparisons are taken
 // from the sign of a difference and gathered bit by bit: a compare's result
 // would have to be waited for.
-// 2^25 logits by 3, 4 and 8 choices so, and in turn: 49, 49, 55 and 53, 60, 92 us
-// for 128 experts, 38, 38, 44 and 43, 49, 72 for 256, 42, 42, 42 and 45, 51, 75
-// for 512, 52, 51, 52 and 48, 54, 82 for 1024; two choices, 38 to 52 and 38 to 45.
+// 2^25 logits, 3, 4 and 8 choices so, and in turn: 38, 38, 44 and 41, 46, 68 us for
+// 256 experts, 42, 42, 42 and 43, 49, 72 for 512, 52, 52, 52 and 46, 52, 77 for
+// 1024; 8 choices of 128 experts 55 and 88; two of 256 37 and 37, of 1024 52 and 40.
 template <int G, int V>
 __device__ inline bool choose_few(const float (&x)[V], float top, const Exp& ex, uint32_t k, uint32_t l, uint32_t group, RouteLds<G, V>& m)
 {
@@ -550,7 +552,7 @@ __global__ __launch_bounds__(kBlock, kOne ? 1 : V >= 16 ? 4 : 5) void k_route(Ro
     rows += (uint32_t)__builtin_popcountll(__ballot(counted)) / G;          // of the wave
     bool done = false;
     if constexpr (G >= kFewLanes)
-      if (r.k >= kFewFrom && 2 * r.k <= G) done = choose_few<G, V>(x, top, ex, r.k, l, group, m);
+      if (r.k >= few_from(G) && 2 * r.k <= G) done = choose_few<G, V>(x, top, ex, r.k, l, group, m);
     if (!done)
       choose_in_turn<G, V>(x, mx, ex, r.k, l4, group, m);
     wave_sync();
@@ -697,12 +699,12 @@ __global__ __launch_bounds__(kBlock) void k_route_back(Rows r, const X* logits, 
 // Lanes per row and elements per lane. The more elements a lane has, the fewer
 // exchanges and rounds of choosing per row; the more lanes, the better their
 // loads lie together, and from kFewLanes on choices can be made by a threshold.
-// Forward with 2 choices, 2^25 logits: 8 experts by 1, 2 and 4 lanes 57, 68 and
-// 114 us; 16 by 1, 2 and 4: 64, 50, 63; 32 by 2, 4 and 8: 60, 48, 62; 64 by 4, 8
-// and 16: 41, 45, 63; 128 by 8 and 16: 37, 45; with 8 choices 128 by 8 and 16: 71,
-// 55; 256 by 16 and 32: 38, 47. Backward (8 choices) 8 experts by 1, 2 and 4 lanes
-// 486, 292 and 307 us; 16 by 1, 2 and 4: 280, 168, 173; 32 by 2, 4 and 8: 118, 89,
-// 111; 64 by 4, 8 and 16: 69, 68, 111; 128 by 8 and 16: 54, 68; 256 by 16 and 32:
+// Forward with 2 choices, 2^25 logits: 8 experts by 1, 2 and 4 lanes 54, 66 and
+// 112 us; 16 by 1, 2 and 4: 66, 49, 62; 32 by 2, 4 and 8: 58, 46, 62; 64 by 4, 8
+// and 16: 41, 44, 63; 128 by 8 and 16: 37, 44; with 8 choices 128 by 8 and 16: 68,
+// 55; 256 by 16 and 32: 37, 46. Backward (8 choices) 8 experts by 1, 2 and 4 lanes
+// 486, 292 and 307 us; 16 by 1, 2 and 4: 280, 168, 173; 32 by 2, 4 and 8: 118, 88,
+// 111; 64 by 4, 8 and 16: 68, 69, 111; 128 by 8 and 16: 55, 68; 256 by 16 and 32:
 // 53, 68.
 template <int G, int V, class F>
 void shape(F f)
