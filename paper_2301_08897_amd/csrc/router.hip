@@ -153,8 +153,12 @@ __device__ inline float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog
 
 // exp(x - mid) of a row, as 2^(x log2 e - mid log2 e) with one rounding for the
 // product and the difference; the rounding of mid log2 e is a factor of the
-// whole row and cancels in its probabilities. In a row whose products could
-// overflow (`far`), of the difference.
+// whole row and cancels in its probabilities. Below kFar it is within 2^(1/16) of
+// one (half a unit of a number below 2^21) and moves lse by less than lse's own
+// rounding; beyond, where it would pass the range of a float, the exponential
+// is that of the difference (`far`).
+constexpr float kFar = 0x1p20f;
+
 struct Exp {
   float mid, c;
   bool far;
@@ -531,7 +535,7 @@ __global__ __launch_bounds__(kBlock, kOne ? 1 : V >= 16 ? 4 : 5) void k_route(Ro
     // a row without a value above -inf sums to zero: it routes nowhere and is not counted
     const float mid = mx == -__builtin_inff() ? 0.0f : mx;
     float p[V], sum = 0.0f;
-    const Exp ex = {mid, mid * kLog2e, !(__builtin_fabsf(mid) < 1e30f)};
+    const Exp ex = {mid, mid * kLog2e, !(__builtin_fabsf(mid) < kFar)};
     if (__ballot(ex.far)) {
 #pragma unroll
       for (int i = 0; i < V; ++i) p[i] = ex(x[i]);
@@ -544,7 +548,7 @@ __global__ __launch_bounds__(kBlock, kOne ? 1 : V >= 16 ? 4 : 5) void k_route(Ro
     for (int i = 0; i < V; ++i) sum += p[i];
     sum = group_sum<G>(sum);
     const bool counted = !(sum == 0.0f);
-    const float inv = counted ? __builtin_amdgcn_rcpf(sum) : 0.0f;       // 1 <= sum <= E
+    const float inv = counted ? __builtin_amdgcn_rcpf(sum) : 0.0f;       // sum is 1 to E, times the row's factor
     const float lse = counted ? mid + __builtin_amdgcn_logf(sum) * kLn2 : 0.0f;
 #pragma unroll
     for (int i = 0; i < V; ++i) acc[i] = __builtin_fmaf(p[i], inv, acc[i]);
