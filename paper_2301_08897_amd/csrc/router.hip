@@ -631,7 +631,8 @@ __global__ __launch_bounds__(kBlock) void k_route_back(Rows r, const X* logits, 
                                                        const float* dloss, X* dlogits, uint64_t ld_out)
 {
   constexpr int kGroups = kBlock / G;
-  __shared__ float s_part[kGroups][G * V];      // the gates' part of the group's row, zero elsewhere
+  __shared__ alignas(16) float s_part[kGroups][G * V];      // the gates' part of the group's row, zero elsewhere
+  static_assert(__alignof__(s_part) >= sizeof(f4), "read by 16 bytes");
   const uint32_t tid = threadIdx.x, l = tid % G, l4 = 4 * l, group = tid / G;
   const Share mine = share_of(r, blockIdx.x);
   const uint64_t row0 = mine.row0, row1 = mine.row1;
