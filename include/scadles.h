@@ -540,7 +540,8 @@ scadles_status scadles_router_forward(const scadles_router* router, const void* 
  *            sum to 1: the forward's give the gradient of its losses; ones
  *            give each device's own share, for scadles_weighted_aggregate
  *            to weight.
- *   out      the forward pass's; counts and loss are not read.
+ *   out      the forward pass's; counts and loss are not read. An index outside
+ *            [0, experts) is a missing choice.
  *   dgate    (dev, tokens x k floats) or NULL (zero).
  *   dloss    (dev, 2 floats) or NULL (zero).
  *   dlogits  (dev, tokens rows of experts elements of the logits' type, ld_out

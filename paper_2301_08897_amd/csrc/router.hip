@@ -650,7 +650,13 @@ __global__ __launch_bounds__(kBlock) void k_route_back(Rows r, const X* logits, 
     const uint64_t row = base + lane_id() / G;
     const bool in = row < row1;
     const float lse = in ? o.lse[row] : 0.0f;
-    const bool on = in && (o.idx[row * r.k] >= 0 || lse != lse);   // routed, or NaN
+    // a choice's expert, or one past the experts for a missing choice: whatever idx
+    // holds, nothing outside s_part is written
+    auto chosen = [&](uint32_t c) {
+      const uint32_t e = (uint32_t)o.idx[row * r.k + c];
+      return e < r.E ? e : r.E;
+    };
+    const bool on = in && (chosen(0) < r.E || lse != lse);         // routed, or NaN
     float x[V];
     load_row<X, G, V>(x, logits + row * r.ld, l4, r.E, on);
     float sum = 0.0f, mean = 0.0f;
@@ -665,11 +671,11 @@ __global__ __launch_bounds__(kBlock) void k_route_back(Rows r, const X* logits, 
     float part = 0.0f;
     if (dgate) {
       for (uint32_t c = l; c < r.k; c += G)    // what is given for a choice that is missing does not count
-        if (on && o.idx[row * r.k + c] >= 0) part += o.gate[row * r.k + c] * dgate[row * r.k + c];
+        if (on && chosen(c) < r.E) part += o.gate[row * r.k + c] * dgate[row * r.k + c];
       part = group_sum<G>(part);
       for (uint32_t c = l; c < r.k; c += G) {
-        const int32_t e = on ? o.idx[row * r.k + c] : -1;
-        if (e >= 0) s_part[group][e] = o.gate[row * r.k + c] * (dgate[row * r.k + c] - (r.renormalise ? part : 0.0f));
+        const uint32_t e = on ? chosen(c) : r.E;
+        if (e < r.E) s_part[group][e] = o.gate[row * r.k + c] * (dgate[row * r.k + c] - (r.renormalise ? part : 0.0f));
       }
       if (r.renormalise) part = 0.0f;
       wave_sync();
@@ -692,8 +698,8 @@ __global__ __launch_bounds__(kBlock) void k_route_back(Rows r, const X* logits, 
     if (dgate) {
       wave_sync();
       for (uint32_t c = l; c < r.k; c += G) {
-        const int32_t e = on ? o.idx[row * r.k + c] : -1;
-        if (e >= 0) s_part[group][e] = 0.0f;
+        const uint32_t e = on ? chosen(c) : r.E;
+        if (e < r.E) s_part[group][e] = 0.0f;
       }
       wave_sync();
     }
