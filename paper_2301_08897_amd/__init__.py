@@ -806,6 +806,17 @@ class RouterOutputs:
     loss: object         # float32 [2]: balance, z
 
 
+class _Pass:
+    """What the library reads of a router's pass: bounds, weights and shapes. The
+    backward pass has weights of its own (``w_back``) for when they are given."""
+
+    def __init__(self, E, k, K, renormalise):
+        off, w, w_back = (_u64 * (K + 1))(), (ctypes.c_float * K)(), (ctypes.c_float * K)()
+        self.off = np.frombuffer(off, dtype=np.uint64)
+        self.w, self.w_back = (np.frombuffer(x, dtype=np.float32) for x in (w, w_back))
+        self.shape, self.back = (RouterShape(0, E, off, x, E, k, K, 0, renormalise) for x in (w, w_back))
+
+
 class Router:
     """Routes the tokens of K devices to ``experts`` experts, ``k`` each, with the
     balance loss and the z loss over all devices (scadles_router_forward), and
@@ -833,11 +844,8 @@ class Router:
         self._order = _Order()
         self._order.record(torch.cuda.current_stream(dev), [self.idx, self.gate, self.lse, self.counts, self.load,
                                                             self.share, self.loss, self.ws])
-        self._off, self._w, self._w_back = (_u64 * (K + 1))(), (ctypes.c_float * K)(), (ctypes.c_float * K)()
-        self._off_view = np.frombuffer(self._off, dtype=np.uint64)
-        self._w_view, self._w_back_view = (np.frombuffer(w, dtype=np.float32) for w in (self._w, self._w_back))
-        self._shape, self._back_shape = (
-            RouterShape(0, E, self._off, w, E, self.k, K, 0, self.renormalise) for w in (self._w, self._w_back))
+        # the last pass, and the one that takes its place once the library has accepted it
+        self._last, self._next = (_Pass(E, self.k, K, self.renormalise) for _ in range(2))
 
     def _logits(self, x, name):
         """(address, elements between rows) of a [tokens, experts] tensor."""
@@ -871,19 +879,21 @@ class Router:
         T = logits.shape[0]
         if T > self.max_tokens:
             raise ValueError(f"more than max_tokens = {self.max_tokens} rows")
-        self._fill(self._off_view, (0, T) if tok_off is None else tok_off, "tok_off")
+        n = self._next
+        self._fill(n.off, (0, T) if tok_off is None else tok_off, "tok_off")
         if weights is None:
-            weights = np.diff(self._off_view.astype(np.int64)) / T if T else [1.0 / self.devices] * self.devices
-        self._fill(self._w_view, weights, "weights")
+            weights = np.diff(n.off.astype(np.int64)) / T if T else [1.0 / self.devices] * self.devices
+        self._fill(n.w, weights, "weights")
         if valid is not None:
             if valid.dtype not in (torch.bool, torch.uint8) or not valid.is_cuda or not valid.is_contiguous():
                 raise TypeError("valid must be a contiguous bool GPU tensor")
             if valid.numel() != T:
                 raise ValueError("valid must have one entry per row")
-        f = self._shape
+        f = n.shape
         f.tokens, f.ld, f.logits_type = T, ld, logits.dtype == torch.bfloat16
         _check(_router_forward(f, p, None if valid is None else valid.data_ptr(), self._out, self.ws.data_ptr(),
                                self.ws.numel(), self._order.enter(stream)))
+        self._last, self._next = n, self._last
         if T == self.max_tokens:
             return RouterOutputs(self.idx, self.gate, self.lse, self.counts, self.load, self.share, self.loss)
         return RouterOutputs(self.idx[:T], self.gate[:T], self.lse[:T], self.counts, self.load, self.share, self.loss)
@@ -896,7 +906,7 @@ class Router:
         ``d_logits`` if given."""
         torch = _torch()
         p, ld = self._logits(logits, "logits")
-        f, T = self._shape, logits.shape[0]
+        f, T = self._last.shape, logits.shape[0]
         if out.load is not self.load or out.lse.shape[0] != f.tokens:
             raise ValueError("out is not this router's last forward pass")
         if T != f.tokens or f.logits_type != (logits.dtype == torch.bfloat16):
@@ -911,9 +921,9 @@ class Router:
         if d_logits.dtype != logits.dtype or d_logits.shape[0] != T:
             raise ValueError("d_logits must be like logits")
         if weights is not None:
-            self._fill(self._w_back_view, weights, "weights")
-            f = self._back_shape
-            f.tokens, f.logits_type = T, self._shape.logits_type
+            self._fill(self._last.w_back, weights, "weights")
+            f = self._last.back
+            f.tokens, f.logits_type = T, self._last.shape.logits_type
         f.ld = ld
         _check(_router_backward(f, p, self._out, None if d_gate is None else _dev_f32(d_gate, "d_gate"),
                                 None if d_loss is None else _dev_f32(d_loss, "d_loss"), q, ld_out,
