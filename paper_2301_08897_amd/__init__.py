@@ -11,6 +11,7 @@ from __future__ import annotations
 import ctypes
 import math
 import os
+import weakref
 from dataclasses import dataclass
 from typing import Optional, Sequence
 
@@ -804,17 +805,43 @@ class RouterOutputs:
     load: object         # float32 [experts]
     share: object        # float32 [devices]: 1 / counted rows
     loss: object         # float32 [2]: balance, z
+    mark: object = None  # the pass's, for the backward pass's check
+
+
+class _Mark:
+    """A router's pass, held by its outputs: the router sees whether any are left."""
+    __slots__ = ("__weakref__",)
+
+
+def _seen(x):
+    """A tensor and its version, without holding it."""
+    return weakref.ref(x), 0 if x.is_inference() else x._version
+
+
+def _same(a, b):
+    return a[1] == b[1] and a[0]() is b[0]()
 
 
 class _Pass:
     """What the library reads of a router's pass: bounds, weights and shapes. The
-    backward pass has weights of its own (``w_back``) for when they are given."""
+    backward pass has weights of its own (``w_back``) for when they are given.
+    Beside them what tells the pass from others: its logits and mask."""
 
     def __init__(self, E, k, K, renormalise):
         off, w, w_back = (_u64 * (K + 1))(), (ctypes.c_float * K)(), (ctypes.c_float * K)()
         self.off = np.frombuffer(off, dtype=np.uint64)
         self.w, self.w_back = (np.frombuffer(x, dtype=np.float32) for x in (w, w_back))
         self.shape, self.back = (RouterShape(0, E, off, x, E, k, K, 0, renormalise) for x in (w, w_back))
+        self.logits = self.valid = None
+
+    def repeats(self, other):
+        """Whether this pass has the inputs of ``other``, so that it writes the same
+        once more. A mask that no longer exists is taken for the same one."""
+        if not _same(self.logits, other.logits) or (self.valid is None) != (other.valid is None):
+            return False
+        if self.valid is not None and other.valid[0]() is not None and not _same(self.valid, other.valid):
+            return False
+        return self.off.tobytes() == other.off.tobytes() and self.w.tobytes() == other.w.tobytes()
 
 
 class Router:
@@ -846,6 +873,7 @@ class Router:
                                                             self.share, self.loss, self.ws])
         # the last pass, and the one that takes its place once the library has accepted it
         self._last, self._next = (_Pass(E, self.k, K, self.renormalise) for _ in range(2))
+        self._mark = lambda: None                # a weak reference to the last pass's
 
     def _logits(self, x, name):
         """(address, elements between rows) of a [tokens, experts] tensor."""
@@ -893,21 +921,27 @@ class Router:
         f.tokens, f.ld, f.logits_type = T, ld, logits.dtype == torch.bfloat16
         _check(_router_forward(f, p, None if valid is None else valid.data_ptr(), self._out, self.ws.data_ptr(),
                                self.ws.numel(), self._order.enter(stream)))
+        n.logits, n.valid = _seen(logits), None if valid is None else _seen(valid)
+        mark = self._mark()
+        if mark is None or not n.repeats(self._last):
+            mark = _Mark()
+            self._mark = weakref.ref(mark)
         self._last, self._next = n, self._last
         if T == self.max_tokens:
-            return RouterOutputs(self.idx, self.gate, self.lse, self.counts, self.load, self.share, self.loss)
-        return RouterOutputs(self.idx[:T], self.gate[:T], self.lse[:T], self.counts, self.load, self.share, self.loss)
+            return RouterOutputs(self.idx, self.gate, self.lse, self.counts, self.load, self.share, self.loss, mark)
+        return RouterOutputs(self.idx[:T], self.gate[:T], self.lse[:T], self.counts, self.load, self.share, self.loss, mark)
 
     def backward(self, logits, out: RouterOutputs, d_gate=None, d_loss=None, *, weights=None, d_logits=None, stream=None):
         """Gradient of ``logits`` under ``d_gate`` [T, k] (or None) of the gates and
         ``d_loss`` [2] (or None) of the losses, both float32; ``out`` is the last
-        forward pass's. ``weights``: as in the forward pass by default; ones give
+        forward pass's: one that another pass has overwritten is refused.
+        ``weights``: as in the forward pass by default; ones give
         each device's own share, before the aggregation weights it. Returned in
         ``d_logits`` if given."""
         torch = _torch()
         p, ld = self._logits(logits, "logits")
         f, T = self._last.shape, logits.shape[0]
-        if out.load is not self.load or out.lse.shape[0] != f.tokens:
+        if out.mark is None or out.mark is not self._mark():
             raise ValueError("out is not this router's last forward pass")
         if T != f.tokens or f.logits_type != (logits.dtype == torch.bfloat16):
             raise ValueError("logits are not those of the forward pass")

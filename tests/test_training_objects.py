@@ -50,3 +50,54 @@ def test_refused_forward_leaves_the_last_pass(sc, lib, T):
     g = r.forward(x, tok_off=[0, 3, 12], weights=[0.5, 0.5])
     r.backward(x, g, weights=[1.0, 2.0])
     assert bounds_of(lib.calls()[-1], 2) == ([0, 3, 12], [1.0, 2.0], 12)
+
+
+def test_backward_of_an_overwritten_pass_is_refused(sc, lib):
+    r = sc.Router(12, 8, 2, devices=2)
+    a, b = logits(), logits()
+    off, w = [0, 4, 12], [0.25, 0.75]
+    f = r.forward(a, tok_off=off, weights=w)
+    r.backward(a, f)
+    g = r.forward(b, tok_off=off, weights=w)
+    with pytest.raises(ValueError):
+        r.backward(a, f)                        # f's memory holds g's choices
+    r.backward(b, g)
+    r.backward(logits(), g)                     # logits computed again
+    old = g
+    for change in (dict(tok_off=[0, 5, 12]), dict(weights=[0.5, 0.5]), dict(valid=fake.on(0, torch.ones(12, dtype=torch.bool)))):
+        g = r.forward(b, **{**dict(tok_off=off, weights=w), **change})
+        with pytest.raises(ValueError):
+            r.backward(b, old)
+        r.backward(b, g)
+        old = g
+    mask = fake.on(0, torch.ones(12, dtype=torch.bool))
+    g = r.forward(b, tok_off=off, weights=w, valid=mask)
+    mask[3] = False
+    for valid in (mask, mask.clone()):
+        h = r.forward(b, tok_off=off, weights=w, valid=valid)
+        with pytest.raises(ValueError):
+            r.backward(b, g)
+        g = h
+    h = r.forward(b, tok_off=off, weights=w)
+    b += 1.0
+    r.forward(b, tok_off=off, weights=w)
+    with pytest.raises(ValueError):
+        r.backward(b, h)
+    with pytest.raises(ValueError):
+        sc.Router(12, 8, 2, devices=2).backward(b, h)
+
+
+def test_a_repeated_pass_is_the_same_pass(sc, lib):
+    """The same logits, bounds, weights and mask give the same results, so that the
+    first call's outputs are still right."""
+    r = sc.Router(12, 8, 2, devices=2)
+    x, mask = logits(), fake.on(0, torch.ones(12, dtype=torch.bool))
+    for valid in (None, mask):
+        f = r.forward(x, tok_off=[0, 4, 12], valid=valid)
+        r.forward(x, tok_off=np.array([0, 4, 12]), weights=[4 / 12, 8 / 12], valid=valid)
+        r.backward(x, f)
+    with torch.inference_mode():                # tensors without a version
+        y = logits()
+        f = r.forward(y, tok_off=[0, 4, 12])
+        r.forward(y, tok_off=[0, 4, 12])
+        r.backward(y, f)
