@@ -101,3 +101,93 @@ def test_a_repeated_pass_is_the_same_pass(sc, lib):
         f = r.forward(y, tok_off=[0, 4, 12])
         r.forward(y, tok_off=[0, 4, 12])
         r.backward(y, f)
+
+
+def in_order(log, names):
+    """Whether every library call runs after all before it: on their streams, or
+    behind events recorded on those after them and waited for."""
+    before, events, made = {}, {}, set()             # what is ordered before a stream's next work; an event's
+    for i, x in enumerate(log):
+        mine = before.setdefault(x[1], set())
+        if x[0] == "record":
+            events[x[1], i] = set(mine)
+        elif x[0] == "wait":
+            mine |= events[x[2]]
+        elif x[0] in names:
+            if mine != made:
+                return False
+            made.add(i)
+            mine.add(i)
+    return True
+
+
+def tensors(*sizes, gpu=0, dtype=torch.float32):
+    return [fake.on(gpu, torch.zeros(n, dtype=dtype)) for n in sizes]
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_adamw_calls_on_several_streams_run_in_order(sc, lib, bits):
+    """The plan's table, the norm's counter, the moments and the parameters are
+    touched by every call: no call may overtake one on another stream."""
+    a, b = lib.stream(11), lib.stream(12)
+    opt = sc.AdamW(tensors(300, 5), tensors(300, 5), state_bits=bits)
+    opt.step(1e-3, stream=a)
+    opt.set_grads(tensors(300, 5))                       # rewrites what the step reads
+    opt.grad_norm(1.0, stream=b)
+    opt.set_grads(tensors(300, 5), stream=a)             # and what the norm counts in
+    opt.step(1e-3, clip=opt.grad_norm(1.0, stream=b))
+    m, v = opt.moments(stream=a)
+    opt.load(3, fake.on(0, torch.zeros(305)), fake.on(0, torch.zeros(305)), stream=b)
+    opt.step(1e-3)
+    opt.step(1e-3)
+    opt.step(1e-3, stream=a)
+    assert in_order(lib.log, lib.CALLS)
+    assert [x[1] for x in lib.calls()][-4:] == [12, 0, 0, 11]
+    uses = [x for x in lib.log if x[0] == "use"]
+    assert {11, 12} <= {x[1] for x in uses}              # the allocator knows of both streams
+    n = len(lib.log)
+    opt.step(1e-3, stream=a)
+    assert len(lib.log) == n + 1                         # nothing but the call where the stream stays
+
+
+def test_moments_wait_for_the_steps(sc, lib):
+    a = lib.stream(11)
+    opt = sc.AdamW(tensors(300), tensors(300))
+    opt.step(1e-3, stream=a)
+    n = len(lib.log)
+    opt.moments()                                        # the object's own memory: no call, but the stream waits
+    assert [x[:2] for x in lib.log[n:]][:2] == [("record", 11), ("wait", 0)]
+
+
+def test_router_calls_on_several_streams_run_in_order(sc, lib):
+    a, b = lib.stream(11), lib.stream(12)
+    r = sc.Router(12, 8, 2)
+    x = logits()
+    f = r.forward(x, stream=a)
+    r.backward(x, f, stream=b)                           # reads what the forward pass writes
+    f = r.forward(x)                                     # overwrites what the backward pass reads
+    r.backward(x, f, stream=a)
+    r.forward(x, stream=b)
+    assert in_order(lib.log, lib.CALLS)
+
+
+def test_captures_do_not_wait_for_work_outside(sc, lib):
+    """A capture cannot wait for work that it does not hold, nor eager work for what
+    was only captured; streams of one capture wait for one another."""
+    a, b = lib.stream(11), lib.stream(12)
+    r = sc.Router(12, 8, 2)
+    x = logits()
+    r.forward(x)
+    a.capturing = b.capturing = True
+    n = len(lib.log)
+    f = r.forward(x, stream=a)
+    assert not [x for x in lib.log[n:] if x[0] in ("record", "wait")]
+    n = len(lib.log)
+    r.backward(x, f, stream=b)
+    assert [x[:2] for x in lib.log[n:] if x[0] in ("record", "wait")] == [("record", 11), ("wait", 12)]
+    n = len(lib.log)
+    r.forward(x)
+    assert not [x for x in lib.log[n:] if x[0] in ("record", "wait")]
+    a.capturing = b.capturing = False
+    r.forward(x, stream=a)
+    assert lib.log[-2][:2] == ("wait", 11)
