@@ -183,12 +183,14 @@ def _stream_ptr(stream) -> Optional[int]:
     return stream.cuda_stream
 
 
-def _dev_f32(t, name):
+def _dev_f32(t, name, device=None):
     torch = _torch()
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a GPU tensor")
     if t.dtype != torch.float32 or not t.is_contiguous():
         raise TypeError(f"{name} must be a contiguous float32 tensor")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name} must be on {device}")
     return t.data_ptr()
 
 
@@ -633,25 +635,43 @@ class _Order:
     call reads and writes memory of the object, so that none may overtake another.
     A call on another stream than the last one's waits for that one; a call that
     is captured waits for captured ones only, a call that is not for those that
-    are not."""
+    are not. The calls are made with the buffers' GPU as the current one, whose
+    default stream the address 0 means."""
 
     def __init__(self, stream, buffers):
         """The buffers belong to the stream."""
         torch = _torch()
-        self.stream, self.address, self.seen, self.buffers = stream, stream.cuda_stream, {stream.cuda_stream}, buffers
-        self.event, self.current = torch.cuda.Event(), torch.cuda.current_stream
+        self.gpu, self.cuda = buffers[0].device.index, torch.cuda
         # the current stream's address without the object around it: a fifth of the time
-        self.raw, self.gpu = torch._C._cuda_getCurrentRawStream, torch.cuda.current_device
+        self.current_device, self.raw = torch.cuda.current_device, torch._C._cuda_getCurrentRawStream
+        self.stream = self.on(stream)
+        self.address, self.seen, self.buffers = stream.cuda_stream, {stream.cuda_stream}, buffers
+        self.event = torch.cuda.Event()
+
+    def on(self, stream):
+        """The stream to run on: the GPU's current one for None."""
+        if stream is None:
+            return self.cuda.current_stream(self.gpu)
+        if stream.device_index != self.gpu:
+            raise ValueError(f"the stream must be one of cuda:{self.gpu}")
+        return stream
 
     def enter(self, stream):
-        """The address of the stream to run on (the current one for None)."""
-        if stream is None:
-            if self.raw(self.gpu()) == self.address:
-                return self.address
-            stream = self.current()
+        """The address of the stream to run on."""
+        if stream is None and self.raw(self.gpu) == self.address:
+            return self.address
+        stream = self.on(stream)
         if stream.cuda_stream != self.address:
             self._change(stream)
         return self.address
+
+    def run(self, call, *args, stream):
+        """A library call, with the stream's address as its last argument."""
+        p = self.enter(stream)
+        if self.current_device() == self.gpu:
+            return _check(call(*args, p))
+        with self.cuda.device(self.gpu):
+            _check(call(*args, p))
 
     def _change(self, stream):
         if _capturing(stream) == _capturing(self.stream):
@@ -692,7 +712,7 @@ class AdamW:
         if state_bits not in (8, 32):
             raise ValueError("state_bits must be 32 or 8")
         for i, p in enumerate(self.params):
-            _dev_f32(p, f"params[{i}]")
+            _dev_f32(p, f"params[{i}]", self.params[0].device if i else None)
         self.device = self.params[0].device
         self.sizes = [p.numel() for p in self.params]
         self.n = sum(self.sizes)
@@ -710,7 +730,7 @@ class AdamW:
         self._tensors = (AdamWTensor * L)()
         self._plan, self._options = AdamWPlan(), AdamWOptions(0.0, self.betas[0], self.betas[1], self.eps, 0)
         self.t = 0
-        stream = torch.cuda.current_stream() if stream is None else stream
+        stream = torch.cuda.current_stream(self.device) if stream is None else stream
         with torch.cuda.stream(stream):
             if self.state_bits == 8:
                 blocks = [-(-x // MOMENT_BLOCK) for x in self.sizes]
@@ -752,15 +772,16 @@ class AdamW:
             if g.device != self.device or g.numel() != self.sizes[i]:
                 raise ValueError(f"grads[{i}] must be on the parameters' GPU and of their size")
             self._tensors[i].grad = g.data_ptr()
-        _check(_adamw_plan_build(self._tensors, len(grads), self.state_bits, 1 if grads[0].dtype == torch.bfloat16 else 0,
-                                 self._table.data_ptr(), self._table.numel(), self._plan, self._order.enter(stream)))
+        self._order.run(_adamw_plan_build, self._tensors, len(grads), self.state_bits,
+                        1 if grads[0].dtype == torch.bfloat16 else 0, self._table.data_ptr(), self._table.numel(),
+                        self._plan, stream=stream)
         self.grads = grads
 
     def grad_norm(self, max_norm: float = math.inf, *, stream=None):
         """float32[2] = (global norm of the gradients, factor that clips it to
         ``max_norm``), for ``step``; the factor is NaN when the norm is not
         finite. The tensor is the object's own and overwritten by the next call."""
-        _check(_grad_norm(self._plan, float(max_norm), self.clip.data_ptr(), self._order.enter(stream)))
+        self._order.run(_grad_norm, self._plan, float(max_norm), self.clip.data_ptr(), stream=stream)
         return self.clip
 
     def step(self, lr: float, *, clip=None, stream=None):
@@ -770,8 +791,8 @@ class AdamW:
         o.lr, o.step = float(lr), self.t + 1
         if clip is not None and clip.numel() != 2:
             raise ValueError("clip must have two entries")
-        _check(_adamw_step(self._plan, o, None if clip is None else _dev_f32(clip, "clip"),
-                           self._order.enter(stream)))
+        self._order.run(_adamw_step, self._plan, o, None if clip is None else _dev_f32(clip, "clip", self.device),
+                        stream=stream)
         self.t += 1
 
     def moments(self, *, stream=None):
@@ -781,7 +802,7 @@ class AdamW:
             self._order.enter(stream)
             return self.m, self.v
         m, v = (_empty(self.n, _torch().float32, self.device, stream) for _ in range(2))
-        _check(_adamw_get_moments(self._plan, m.data_ptr(), v.data_ptr(), self._order.enter(stream)))
+        self._order.run(_adamw_get_moments, self._plan, m.data_ptr(), v.data_ptr(), stream=stream)
         return m, v
 
     def load(self, t: int, m, v, *, tops=None, stream=None):
@@ -790,21 +811,22 @@ class AdamW:
         torch = _torch()
         if t < 0:
             raise ValueError("t must not be negative")
-        stream = torch.cuda.current_stream() if stream is None else stream
-        p = self._order.enter(stream)
+        stream = self._order.on(stream)
         if tops is not None:
             if self.state_bits != 8:
                 raise ValueError("tops belongs to 8-bit moments")
             for x, mine, name in ((m, self.m, "m"), (v, self.v, "v"), (tops, self.tops, "tops")):
                 if x.dtype != mine.dtype or x.shape != mine.shape:
                     raise ValueError(f"{name} must be {mine.dtype} of shape {tuple(mine.shape)}")
+            self._order.enter(stream)
             with torch.cuda.stream(stream):
                 for x, mine in ((m, self.m), (v, self.v), (tops, self.tops)):
                     mine.copy_(x)
         else:
             if m.numel() != self.n or v.numel() != self.n:
                 raise ValueError("m and v must hold every element")
-            _check(_adamw_set_moments(self._plan, _dev_f32(m, "m"), _dev_f32(v, "v"), int(t), p))
+            self._order.run(_adamw_set_moments, self._plan, _dev_f32(m, "m", self.device), _dev_f32(v, "v", self.device),
+                            int(t), stream=stream)
         self.t = int(t)
 
 
@@ -886,8 +908,9 @@ class Router:
         self.ws = _workspace(need, dev)
         self._out = RouterOut(*[x.data_ptr() for x in (self.idx, self.gate, self.lse, self.counts, self.load, self.share,
                                                        self.loss)])
-        self._order = _Order(torch.cuda.current_stream(dev), [self.idx, self.gate, self.lse, self.counts, self.load,
-                                                              self.share, self.loss, self.ws])
+        self.device = self.idx.device
+        self._order = _Order(torch.cuda.current_stream(self.device), [self.idx, self.gate, self.lse, self.counts,
+                                                                      self.load, self.share, self.loss, self.ws])
         # the last pass, and the one that takes its place once the library has accepted it
         self._last, self._next = (_Pass(E, self.k, K, self.renormalise) for _ in range(2))
         self._mark = lambda: None                # a weak reference to the last pass's
@@ -897,6 +920,8 @@ class Router:
         torch = _torch()
         if not isinstance(x, torch.Tensor) or not x.is_cuda or x.dtype not in (torch.float32, torch.bfloat16):
             raise TypeError(f"{name} must be a float32 or bfloat16 GPU tensor")
+        if x.device != self.device:
+            raise ValueError(f"{name} must be on {self.device}")
         if x.dim() != 2 or x.shape[1] != self.experts:
             raise ValueError(f"{name} must be [tokens, {self.experts}]")
         row, step = x.stride()
@@ -932,12 +957,12 @@ class Router:
         if valid is not None:
             if valid.dtype not in (torch.bool, torch.uint8) or not valid.is_cuda or not valid.is_contiguous():
                 raise TypeError("valid must be a contiguous bool GPU tensor")
-            if valid.numel() != T:
-                raise ValueError("valid must have one entry per row")
+            if valid.numel() != T or valid.device != self.device:
+                raise ValueError(f"valid must have one entry per row and be on {self.device}")
         f = n.shape
         f.tokens, f.ld, f.logits_type = T, ld, logits.dtype == torch.bfloat16
-        _check(_router_forward(f, p, None if valid is None else valid.data_ptr(), self._out, self.ws.data_ptr(),
-                               self.ws.numel(), self._order.enter(stream)))
+        self._order.run(_router_forward, f, p, None if valid is None else valid.data_ptr(), self._out,
+                        self.ws.data_ptr(), self.ws.numel(), stream=stream)
         n.logits, n.valid = _seen(logits), None if valid is None else _seen(valid)
         mark = self._mark()
         if mark is None or not n.repeats(self._last):
@@ -976,7 +1001,7 @@ class Router:
             f = self._last.back
             f.tokens, f.logits_type = T, self._last.shape.logits_type
         f.ld = ld
-        _check(_router_backward(f, p, self._out, None if d_gate is None else _dev_f32(d_gate, "d_gate"),
-                                None if d_loss is None else _dev_f32(d_loss, "d_loss"), q, ld_out,
-                                self._order.enter(stream)))
+        self._order.run(_router_backward, f, p, self._out,
+                        None if d_gate is None else _dev_f32(d_gate, "d_gate", self.device),
+                        None if d_loss is None else _dev_f32(d_loss, "d_loss", self.device), q, ld_out, stream=stream)
         return d_logits

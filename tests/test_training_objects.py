@@ -191,3 +191,65 @@ def test_captures_do_not_wait_for_work_outside(sc, lib):
     a.capturing = b.capturing = False
     r.forward(x, stream=a)
     assert lib.log[-2][:2] == ("wait", 11)
+
+
+def test_tensors_of_another_gpu_are_refused(sc, lib):
+    here, there = tensors(300, 5), tensors(300, 5, gpu=1)
+    mixed = [here[0], there[1]]
+    for params, grads in ((mixed, here), (here, mixed), (there, here)):
+        with pytest.raises(ValueError):
+            sc.AdamW(params, grads)
+    with pytest.raises(ValueError):
+        sc.AdamW(here, here, copies=tensors(300, 5, gpu=1, dtype=torch.bfloat16))
+    opt = sc.AdamW(here, here)
+    calls = len(lib.calls())
+    with pytest.raises(ValueError):
+        opt.set_grads(there)
+    with pytest.raises(ValueError):
+        opt.step(1e-3, clip=fake.on(1, torch.ones(2)))
+    for m, v in ((0, 1), (1, 0)):
+        with pytest.raises(ValueError):
+            opt.load(3, fake.on(m, torch.zeros(305)), fake.on(v, torch.zeros(305)))
+    r = sc.Router(12, 8, 2)
+    f = r.forward(logits())
+    for more in (dict(logits=logits(gpu=1)), dict(logits=logits(), valid=fake.on(1, torch.ones(12, dtype=torch.bool)))):
+        with pytest.raises(ValueError):
+            r.forward(**more)
+    x = logits()
+    f = r.forward(x)
+    for more in (dict(logits=logits(gpu=1)), dict(d_gate=fake.on(1, torch.zeros(12, 2))), dict(d_loss=fake.on(1, torch.zeros(2))),
+                 dict(d_logits=logits(gpu=1))):
+        with pytest.raises(ValueError):
+            r.backward(**{**dict(logits=x, out=f), **more})
+    assert len(lib.calls()) == calls + 2 and opt.t == 0
+
+
+def test_calls_run_on_the_objects_gpu(sc, lib):
+    """Default streams all have the address 0: a call means its object's GPU's, whatever
+    GPU is current."""
+    cuda = lib.torch.cuda
+    cuda.current[1] = lib.stream(0, gpu=1)
+    opt = sc.AdamW(tensors(300, 5, gpu=1), tensors(300, 5, gpu=1), state_bits=8)
+    r = sc.Router(12, 8, 2, device="cuda:1")
+    x = logits(gpu=1)
+    assert cuda.gpu == 0 and opt.m.device.index == 1 and r.idx.device.index == 1
+    opt.step(1e-3, clip=opt.grad_norm(1.0))
+    opt.load(4, *opt.moments())
+    opt.set_grads(tensors(300, 5, gpu=1))
+    r.backward(x, r.forward(x))
+    with cuda.device(1):
+        opt.step(1e-3)
+    cuda.current[1] = lib.stream(21, gpu=1)              # another current stream there
+    opt.step(1e-3)
+    opt.step(1e-3, stream=lib.stream(22, gpu=1))
+    assert [x[2] for x in lib.calls()] == [1] * len(lib.calls())
+    assert [x[1] for x in lib.calls()][-3:] == [0, 21, 22] and not any(x[1] for x in lib.calls()[:-2])
+    calls = len(lib.calls())
+    for call in (lambda s: opt.step(1e-3, stream=s), lambda s: opt.grad_norm(1.0, stream=s), lambda s: opt.moments(stream=s),
+                 lambda s: opt.load(4, opt.m, opt.v, tops=opt.tops, stream=s), lambda s: opt.set_grads(opt.grads, stream=s),
+                 lambda s: r.forward(x, stream=s)):
+        with pytest.raises(ValueError):
+            call(lib.stream(11, gpu=0))
+    assert len(lib.calls()) == calls
+    with pytest.raises(ValueError):
+        sc.AdamW(tensors(300, gpu=1), tensors(300, gpu=1), stream=lib.stream(11, gpu=0))
