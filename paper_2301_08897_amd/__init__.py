@@ -621,6 +621,16 @@ def _empty(shape, dtype, device, stream):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
+def _wholes(tensors):
+    """The tensors that these are, or are parts of: parts share their version counter."""
+    return tuple({id(x): x for x in (t if t._base is None else t._base for t in tensors)}.values())
+
+
+def _written(tensors):
+    """Tells autograd, by their version counters, that the library has written the tensors."""
+    _torch().autograd.graph.increment_version(tensors)
+
+
 def _capturing(stream):
     torch = _torch()
     if stream.cuda_stream == 0:                # the default stream cannot be captured
@@ -756,6 +766,8 @@ class AdamW:
             self._table = _workspace(int(_adamw_plan_bytes(self._tensors, L)), self.device)
             self.clip = torch.zeros(2, dtype=torch.float32, device=self.device)
         self._order = _Order(stream, [x for x in (self.m, self.v, self.tops, self._table, self.clip) if x is not None])
+        moments = [x for x in (self.m, self.v, self.tops) if x is not None]
+        self._moments, self._steps = _wholes(moments), _wholes(self.params + (self.copies or []) + moments)
         self.set_grads(grads, stream=stream)
 
     def set_grads(self, grads, *, stream=None):
@@ -782,6 +794,7 @@ class AdamW:
         ``max_norm``), for ``step``; the factor is NaN when the norm is not
         finite. The tensor is the object's own and overwritten by the next call."""
         self._order.run(_grad_norm, self._plan, float(max_norm), self.clip.data_ptr(), stream=stream)
+        _written((self.clip,))
         return self.clip
 
     def step(self, lr: float, *, clip=None, stream=None):
@@ -793,6 +806,7 @@ class AdamW:
             raise ValueError("clip must have two entries")
         self._order.run(_adamw_step, self._plan, o, None if clip is None else _dev_f32(clip, "clip", self.device),
                         stream=stream)
+        _written(self._steps)
         self.t += 1
 
     def moments(self, *, stream=None):
@@ -827,6 +841,7 @@ class AdamW:
                 raise ValueError("m and v must hold every element")
             self._order.run(_adamw_set_moments, self._plan, _dev_f32(m, "m", self.device), _dev_f32(v, "v", self.device),
                             int(t), stream=stream)
+            _written(self._moments)
         self.t = int(t)
 
 
@@ -911,6 +926,7 @@ class Router:
         self.device = self.idx.device
         self._order = _Order(torch.cuda.current_stream(self.device), [self.idx, self.gate, self.lse, self.counts,
                                                                       self.load, self.share, self.loss, self.ws])
+        self._outs = (self.idx, self.gate, self.lse, self.counts, self.load, self.share, self.loss)
         # the last pass, and the one that takes its place once the library has accepted it
         self._last, self._next = (_Pass(E, self.k, K, self.renormalise) for _ in range(2))
         self._mark = lambda: None                # a weak reference to the last pass's
@@ -963,6 +979,7 @@ class Router:
         f.tokens, f.ld, f.logits_type = T, ld, logits.dtype == torch.bfloat16
         self._order.run(_router_forward, f, p, None if valid is None else valid.data_ptr(), self._out,
                         self.ws.data_ptr(), self.ws.numel(), stream=stream)
+        _written(self._outs)
         n.logits, n.valid = _seen(logits), None if valid is None else _seen(valid)
         mark = self._mark()
         if mark is None or not n.repeats(self._last):
@@ -991,7 +1008,8 @@ class Router:
             raise ValueError(f"d_gate must have {T * self.k} entries")
         if d_loss is not None and d_loss.numel() != 2:
             raise ValueError("d_loss must have 2 entries")
-        if d_logits is None:
+        given = d_logits is not None
+        if not given:
             d_logits = _empty((T, self.experts), logits.dtype, logits.device, stream)
         q, ld_out = self._logits(d_logits, "d_logits")
         if d_logits.dtype != logits.dtype or d_logits.shape[0] != T:
@@ -1004,4 +1022,6 @@ class Router:
         self._order.run(_router_backward, f, p, self._out,
                         None if d_gate is None else _dev_f32(d_gate, "d_gate", self.device),
                         None if d_loss is None else _dev_f32(d_loss, "d_loss", self.device), q, ld_out, stream=stream)
+        if given:
+            _written((d_logits,))
         return d_logits

@@ -253,3 +253,55 @@ def test_calls_run_on_the_objects_gpu(sc, lib):
     assert len(lib.calls()) == calls
     with pytest.raises(ValueError):
         sc.AdamW(tensors(300, gpu=1), tensors(300, gpu=1), stream=lib.stream(11, gpu=0))
+
+
+def raised(tensors, call):
+    """Which of the tensors' version counters a call raises."""
+    before = [x._version for x in tensors]
+    call()
+    return [x._version > n for x, n in zip(tensors, before)]
+
+
+def test_what_is_written_has_a_new_version(sc, lib):
+    """autograd refuses a backward pass that needs a tensor written since; it sees by
+    the version that one was."""
+    flat, flat_copy = tensors(500)[0], tensors(500, dtype=torch.bfloat16)[0]
+    params, grads = list(torch.split(flat, [300, 200])) + tensors(7), tensors(300, 200, 7)
+    copies = list(torch.split(flat_copy, [300, 200])) + tensors(7, dtype=torch.bfloat16)
+    opt = sc.AdamW(params, grads, copies=copies)
+    seen = [flat, flat_copy, *params, *copies, opt.m, opt.v]
+    assert all(raised(seen, lambda: opt.step(1e-3)))
+    assert not any(raised(grads + [opt.clip], lambda: opt.step(1e-3)))
+    assert raised([opt.clip, *seen], lambda: opt.grad_norm(1.0)) == [True] + [False] * len(seen)
+    assert all(raised([opt.m, opt.v], lambda: opt.load(3, fake.on(0, torch.zeros(507)), fake.on(0, torch.zeros(507)))))
+    small = sc.AdamW(params, grads, state_bits=8)
+    assert all(raised([flat, params[2], small.m, small.v, small.tops], lambda: small.step(1e-3)))
+    lib.status = 1
+    for call in (lambda: opt.step(1e-3), lambda: opt.grad_norm(1.0)):
+        with pytest.raises(sc.ScadlesError):
+            assert not any(raised(seen + [opt.clip], call))
+    lib.status = 0
+
+    r = sc.Router(12, 8, 2)
+    outs = [r.idx, r.gate, r.lse, r.counts, r.load, r.share, r.loss]
+    x, d = logits(), logits()
+    f = r.forward(x)
+    assert all(raised(outs + [f.gate], lambda: r.forward(x)))
+    assert raised([d, x, *outs], lambda: r.backward(x, f, d_logits=d)) == [True] + [False] * 8
+    w = torch.ones(12, 2, requires_grad=True)
+    y = (w * r.forward(x).gate).sum()
+    r.forward(logits())
+    with pytest.raises(RuntimeError):
+        y.backward()
+
+
+def test_inference_tensors(sc, lib):
+    """Tensors without a version are taken as well."""
+    with torch.inference_mode():
+        params, copies = tensors(300, 5), tensors(300, 5, dtype=torch.bfloat16)
+        opt, r, x, d = sc.AdamW(params, tensors(300, 5), copies=copies), sc.Router(12, 8, 2), logits(), logits()
+    for mode in (True, False):
+        with torch.inference_mode(mode):
+            opt.step(1e-3, clip=opt.grad_norm(1.0))
+            opt.load(3, fake.on(0, torch.zeros(305)), fake.on(0, torch.zeros(305)))
+            r.backward(x, r.forward(x), d_logits=d)
