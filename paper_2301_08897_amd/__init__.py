@@ -654,7 +654,7 @@ class _Order:
         self.gpu, self.cuda = buffers[0].device.index, torch.cuda
         # the current stream's address without the object around it: a fifth of the time
         self.current_device, self.raw = torch.cuda.current_device, torch._C._cuda_getCurrentRawStream
-        self.stream = self.on(stream)
+        self.stream = self.launched = self.on(stream)      # of the last call, and of the last that was not captured
         self.address, self.seen, self.buffers = stream.cuda_stream, {stream.cuda_stream}, buffers
         self.event = torch.cuda.Event()
 
@@ -673,7 +673,7 @@ class _Order:
         stream = self.on(stream)
         if stream.cuda_stream != self.address:
             self._change(stream)
-        return self.address
+        return stream.cuda_stream
 
     def run(self, call, *args, stream):
         """A library call, with the stream's address as its last argument."""
@@ -684,14 +684,20 @@ class _Order:
             _check(call(*args, p))
 
     def _change(self, stream):
-        if _capturing(stream) == _capturing(self.stream):
-            self.event.record(self.stream)
+        p, captured = stream.cuda_stream, _capturing(stream)
+        last = self.launched if not captured else self.stream if _capturing(self.stream) else stream
+        if last.cuda_stream != p:
+            self.event.record(last)
             stream.wait_event(self.event)
-        if stream.cuda_stream not in self.seen:
+        if p not in self.seen:
             for x in self.buffers:
                 x.record_stream(stream)
-            self.seen.add(stream.cuda_stream)
-        self.stream, self.address = stream, stream.cuda_stream
+            self.seen.add(p)
+        self.stream = stream
+        if captured:
+            self.address = None                # whether the next call is captured too has to be asked
+        else:
+            self.launched, self.address = stream, p
 
 
 class AdamW:

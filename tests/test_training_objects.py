@@ -305,3 +305,29 @@ def test_inference_tensors(sc, lib):
             opt.step(1e-3, clip=opt.grad_norm(1.0))
             opt.load(3, fake.on(0, torch.zeros(305)), fake.on(0, torch.zeros(305)))
             r.backward(x, r.forward(x), d_logits=d)
+
+
+def test_order_across_a_capture(sc, lib):
+    """Calls after a capture wait for the calls before it, on whatever streams the
+    captured ones were."""
+    a, b = lib.stream(11), lib.stream(12)
+    for after in (a, b):
+        r = sc.Router(12, 8, 2)
+        x = logits()
+        r.forward(x)
+        a.capturing = True
+        r.backward(x, r.forward(x, stream=a), stream=a)
+        a.capturing = False
+        n = len(lib.log)
+        r.forward(x, stream=after)
+        r.forward(x, stream=after)
+        assert [x[:2] for x in lib.log[n:] if x[0] in ("record", "wait")] == [("record", 0), ("wait", after.cuda_stream)]
+    r = sc.Router(12, 8, 2)
+    r.forward(x, stream=a)
+    a.capturing = b.capturing = True                     # the same stream, then one that joins its capture
+    f = r.forward(x, stream=a)
+    n = len(lib.log)
+    r.backward(x, f, stream=b)
+    a.capturing = b.capturing = False
+    r.forward(x)
+    assert [x[:2] for x in lib.log[n:] if x[0] in ("record", "wait")] == [("record", 11), ("wait", 12), ("record", 11), ("wait", 0)]
