@@ -425,7 +425,8 @@ size_t scadles_adamw_plan_bytes(const scadles_adamw_tensor* tensors, uint32_t co
  *   plan   (host) receives the handle.
  * The table is written by launches on `stream`; later calls on other streams
  * must be ordered after them. Calls with the same plan must not overlap.
- * Build again when a pointer, a size or a weight decay changes.              */
+ * Build again when a pointer, a size or a weight decay changes: a step goes on
+ * with the addresses that it was built with.                                 */
 scadles_status scadles_adamw_plan_build(const scadles_adamw_tensor* tensors, uint32_t count, int moment_bits,
                                         int grad_type, void* table, size_t table_bytes, scadles_adamw_plan* plan,
                                         void* stream);
@@ -479,11 +480,15 @@ scadles_status scadles_adamw_set_moments(const scadles_adamw_plan* plan, const f
  *   prob_e = sum_d weights[d] / n_d * sum_t p_e
  *   loss[0] = E * sum_e load_e * prob_e           (balance; 1 when even)
  *   loss[1] = sum_d weights[d] / n_d * sum_t lse^2    (z)
- * Softmax statistics are kept in float, sums over rows in double in a fixed
- * order. An expert at -infinity is never chosen: missing choices have index -1
- * and gate 0. A row with `valid` 0, or with every logit at -infinity, routes
- * nowhere: indices -1, gates, lse and gradient 0, not counted. A device without
- * counted rows adds nothing. A NaN or +infinity makes its row's gates, lse and
+ * Softmax statistics are kept in float. Sums over rows are taken in a fixed
+ * order: of lse^2 in double; of probabilities in float over the rows of a
+ * workgroup and then of up to 16 workgroups, fewer than 300 additions of values
+ * that are not negative (relative error below 300 * 2^-24), and from there in
+ * double. All of this holds for finite logits of any size; loss[1] is infinite
+ * where it passes the largest float. An expert at -infinity is never chosen:
+ * missing choices have index -1 and gate 0. A row with `valid` 0, or with every
+ * logit at -infinity, routes nowhere: indices -1, gates, lse and gradient 0, not
+ * counted. A device without counted rows adds nothing. A NaN or +infinity makes its row's gates, lse and
  * gradient and the losses NaN; indices stay within [-1, E).                  */
 #define SCADLES_ROUTER_MAX_EXPERTS 1024
 #define SCADLES_ROUTER_MAX_K 16

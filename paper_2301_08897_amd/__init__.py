@@ -704,11 +704,12 @@ class AdamW:
     """AdamW over many tensors at once, one launch per step, with moments in 32
     bits or in blocks of 8-bit codes (format: scadles.h).
 
-    ``params``: contiguous float32 tensors, updated in place; ``grads``: as many
-    contiguous tensors of the same sizes, all float32 or all bfloat16, read at
-    every step where they are (a part of a flat gradient will do, at any
-    offset). ``weight_decay``: one value, or one per tensor. ``copies``:
-    bfloat16 tensors that receive the updated parameters, or None.
+    ``params``: contiguous float32 tensors, updated in place, no two overlapping (a
+    tensor used twice is listed once); ``grads``: as many contiguous tensors of the
+    same sizes, all float32 or all bfloat16, read at every step where they are (a
+    part of a flat gradient will do, at any offset). ``weight_decay``: one value,
+    or one per tensor. ``copies``: bfloat16 tensors that receive the updated
+    parameters, or None.
 
     Calls may be given any streams: they run in the order in which they are made (a
     stream has to exist until the call after its last one is made). What the caller
@@ -777,7 +778,9 @@ class AdamW:
         self.set_grads(grads, stream=stream)
 
     def set_grads(self, grads, *, stream=None):
-        """Point the optimizer at other gradients of the same sizes (writes the plan anew)."""
+        """Point the optimizer at other gradients of the same sizes (writes the plan
+        anew). Needed before the next step whenever gradients were allocated anew:
+        the object keeps the ones it has, and a step goes on reading them."""
         torch = _torch()
         grads = list(grads)
         if len(grads) != len(self.params):
@@ -909,7 +912,8 @@ class Router:
     gives the logits' gradient. Outputs and workspace are allocated once, for up
     to ``max_tokens`` rows. Calls may be given any streams: they run in the order
     in which they are made (a stream has to exist until the call after its last one
-    is made)."""
+    is made). Outside autograd: the outputs have no history, and the gradient that
+    ``backward`` returns goes on with ``logits.backward(d_logits)``."""
 
     def __init__(self, max_tokens: int, experts: int, k: int, *, devices: int = 1, renormalise: bool = False,
                  device=None):

@@ -548,7 +548,10 @@ __global__ __launch_bounds__(kBlock, kOne ? 1 : V >= 16 ? 4 : 5) void k_route(Ro
     for (int i = 0; i < V; ++i) sum += p[i];
     sum = group_sum<G>(sum);
     const bool counted = !(sum == 0.0f);
-    const float inv = counted ? __builtin_amdgcn_rcpf(sum) : 0.0f;       // sum is 1 to E, times the row's factor
+    // sum is 1 to E, times the row's factor; reciprocal, exponential and logarithm are
+    // the hardware's, within a unit: gates and lse are off by up to 1.4 times as much as
+    // with exact ones (7.5e-8 against 5.3e-8 for 256 experts)
+    const float inv = counted ? __builtin_amdgcn_rcpf(sum) : 0.0f;
     const float lse = counted ? mid + __builtin_amdgcn_logf(sum) * kLn2 : 0.0f;
 #pragma unroll
     for (int i = 0; i < V; ++i) acc[i] = __builtin_fmaf(p[i], inv, acc[i]);
@@ -712,9 +715,9 @@ __global__ __launch_bounds__(kBlock) void k_route_back(Rows r, const X* logits, 
 // loads lie together, and from kFewLanes on choices can be made by a threshold.
 // Forward with 2 choices, 2^25 logits: 8 experts by 1, 2 and 4 lanes 54, 66 and
 // 112 us; 16 by 1, 2 and 4: 66, 49, 62; 32 by 2, 4 and 8: 58, 46, 62; 64 by 4, 8
-// and 16: 41, 44, 63; 128 by 8 and 16: 37, 44; with 8 choices 128 by 8 and 16: 68,
-// 55; 256 by 16 and 32: 37, 46. Backward (8 choices) 8 experts by 1, 2 and 4 lanes
-// 486, 292 and 307 us; 16 by 1, 2 and 4: 280, 168, 173; 32 by 2, 4 and 8: 118, 88,
+// and 16: 41, 44, 63; 128 by 8 and 16: 37, 44, with 4, 5 and 8 choices 45, 51, 68
+// and 49, 50, 55; 256 by 16 and 32: 37, 46. Backward (8 choices) 8 experts by 1,
+// 2 and 4 lanes 486, 292 and 307 us; 16 by 1, 2 and 4: 280, 168, 173; 32 by 2, 4 and 8: 118, 88,
 // 111; 64 by 4, 8 and 16: 68, 69, 111; 128 by 8 and 16: 55, 68; 256 by 16 and 32:
 // 53, 68.
 template <int G, int V, class F>
