@@ -1,0 +1,467 @@
+"""What lies between tokens and logits when language models are trained on K
+devices of uneven streams, as cases that can be timed and compared: tokens
+sorted by expert and back with the gates, the embedding's rows and its gradient
+by sorted tokens, layer norm with the reduction of its weights' gradients, and
+the cross entropy of a linear layer over a large vocabulary with its gradient.
+Every gradient of weights is one per device.
+
+With ``own`` false every pass is computed with plain torch operations in 32
+bits.
+"""
+from __future__ import annotations
+
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+EPS = 1e-5
+SCALE = 0.75                     # the embedding's factor
+
+ORDER = {"op": "order", "tokens": 64, "experts": 8, "k": 2, "dim": 64, "devices": 1, "type": "f32", "padding": False, "train": False}
+EMBED = {"op": "embed", "tokens": 16, "vocab": 32768, "dim": 1024, "devices": 1, "type": "bf16", "grads": "f32", "padding": False,
+         "train": False, "add": False}
+NORM = {"op": "norm", "tokens": 64, "dim": 256, "devices": 1, "type": "f32", "bias": True, "train": False}
+LOSS = {"op": "loss", "tokens": 64, "vocab": 1000, "dim": 128, "devices": 1, "type": "f32", "grads": "f32", "padding": False,
+        "train": True}
+
+
+def listed():
+    return [
+        # One short batch answered: its tokens to the experts and back.
+        dict(ORDER, name="order_64x8"),
+        # Training on eight devices: odd numbers of experts, tokens and
+        # elements, padded batches.
+        dict(ORDER, name="order_train_16k_60", tokens=16381, experts=60, k=4, dim=1001, devices=8, type="bf16", padding=True, train=True),
+        # Training with many experts and many choices, long rows.
+        dict(ORDER, name="order_train_32k_256", tokens=32768, experts=256, k=8, dim=2048, devices=8, type="bf16", train=True),
+        # One token for each of sixteen answers under way.
+        dict(EMBED, name="embed_16"),
+        # Four devices' gradients of a table of odd size, 32-bit.
+        dict(EMBED, name="embed_train_8k", tokens=8190, vocab=50001, dim=515, devices=4, type="f32", padding=True, train=True),
+        # The largest batch; the table is the logits' too, so that the gradient
+        # is added to what that one left.
+        dict(EMBED, name="embed_train_128k", tokens=131072, vocab=65536, dim=1024, train=True, add=True),
+        # A short batch through a small layer.
+        dict(NORM, name="norm_64x256", train=True),
+        # Answers: no gradient.
+        dict(NORM, name="norm_4k_1k", tokens=4096, dim=1024, type="bf16"),
+        # The largest batch, one gradient of the weights for each of 32 devices.
+        dict(NORM, name="norm_train_128k_2k", tokens=131072, dim=2048, devices=32, type="bf16", train=True),
+        # A small model's loss with its gradient.
+        dict(LOSS, name="loss_64x1000"),
+        # 32-bit training on four devices, each with its gradient.
+        dict(LOSS, name="loss_train_2k_20k", tokens=2039, vocab=20011, dim=500, devices=4, padding=True),
+        # A large vocabulary and batch in bf16, matrix products throughout.
+        dict(LOSS, name="loss_train_8k_64k", tokens=8192, vocab=65536, dim=1024, type="bf16", grads="bf16"),
+    ]
+
+
+def draw(rng):
+    log = lambda lo, hi: int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))  # noqa: E731
+    near = lambda n: max(1, n + rng.choice([0, 0, 0, -1, 1, -3, 5]))  # noqa: E731
+    wide = lambda lo, hi: near(8 * log(lo // 8, hi // 8))  # noqa: E731
+    devices = rng.choice([1, 1, 2, 5, 8, 16, 32])
+    kind = rng.choice(["f32", "bf16"])
+    op = rng.choice(["order", "embed", "norm", "loss"])
+    if op == "order":
+        experts, dim = log(4, 256), wide(64, 2048)
+        k = rng.randint(1, min(8, experts))
+        most = 2**29 // (k * dim * (2 if kind == "f32" else 1))          # the largest case's elements
+        return dict(ORDER, tokens=log(16, max(17, min(131072, most))), experts=experts, k=k, dim=dim, devices=devices, type=kind,
+                    padding=rng.random() < 0.4, train=rng.random() < 0.6)
+    if op == "embed":
+        train, vocab, dim = rng.random() < 0.7, near(log(500, 131072)), wide(64, 2048)
+        devices = max(1, min(devices, 2**26 // (vocab * dim)))
+        return dict(EMBED, tokens=log(1, min(131072, 2**27 // dim)), vocab=vocab, dim=dim, devices=devices, type=kind,
+                    grads=rng.choice(["f32", "f32", "bf16"]), padding=rng.random() < 0.4, train=train, add=train and rng.random() < 0.4)
+    if op == "norm":
+        dim = wide(32, 8192)
+        most = 2**28 // (dim * (2 if kind == "f32" else 1))
+        return dict(NORM, tokens=log(1, min(131072, most)), dim=dim, devices=devices, type=kind, bias=rng.random() < 0.7,
+                    train=rng.random() < 0.6)
+    vocab, dim, train = near(log(500, 131072)), wide(64, 2048), rng.random() < 0.75
+    if train:
+        devices = max(1, min(devices, 2**26 // (vocab * dim)))
+    most = (2**39 if kind == "bf16" else 2**36) // (vocab * dim * (1 if train else 1))
+    return dict(LOSS, tokens=log(16, max(17, min(16384, most, 2**30 // vocab))), vocab=vocab, dim=dim, devices=devices, type=kind,
+                grads="bf16" if kind == "bf16" and rng.random() < 0.5 else "f32", padding=rng.random() < 0.4, train=train)
+
+
+# ---- inputs -----------------------------------------------------------------------------------
+
+def generator(seed, salt):
+    return torch.Generator(device="cuda").manual_seed(seed * 7919 + salt)
+
+
+def normal(seed, salt, *shape):
+    return torch.empty(*shape, dtype=torch.float32, device="cuda").normal_(generator=generator(seed, salt))
+
+
+def uniform(seed, salt, *shape):
+    return torch.empty(*shape, dtype=torch.float32, device="cuda").uniform_(generator=generator(seed, salt))
+
+
+def typed(case, x, key="type"):
+    return x.to(torch.bfloat16) if case[key] == "bf16" else x
+
+
+def bounds_of(case):
+    """Rows of the devices, whose streams run from slow to fast."""
+    share = 128.0 ** (np.arange(case["devices"]) / max(case["devices"] - 1, 1))
+    b = np.round(np.cumsum(share) / share.sum() * case["tokens"]).astype(np.int64)
+    b[-1] = case["tokens"]
+    return [0] + [int(x) for x in b]
+
+
+def words(case, seed, salt):
+    """Tokens as text has them: the id of rank r as often as 1 / r, in random places of
+    the vocabulary; -1 for padding."""
+    V, T = case["vocab"], case["tokens"]
+    rank = torch.exp(uniform(seed, salt, T) * math.log(V + 1.0)).to(torch.int64).clamp(1, V) - 1
+    ids = torch.randperm(V, generator=generator(seed, salt + 1), device="cuda")[rank]
+    if case["padding"]:
+        ids = torch.where(uniform(seed, salt + 2, T) < 0.9, ids, -1)
+    return ids
+
+
+def order_inputs(case, seed, s):
+    T, E, k, d = case["tokens"], case["experts"], case["k"], case["dim"]
+    score = normal(seed, 11, T, E) + normal(seed, 12, E) * 0.5
+    top = torch.sort(score, dim=1, descending=True, stable=True)
+    s["idx"] = top.indices[:, :k].to(torch.int32)
+    s["gate"] = torch.softmax(top.values[:, :k], dim=1)
+    if case["padding"]:
+        there = uniform(seed, 13, T) < 0.9
+        s["idx"] = torch.where(there[:, None], s["idx"], -1)
+        s["gate"] = torch.where(there[:, None], s["gate"], 0.0)
+    s["idx"], s["gate"] = s["idx"].contiguous(), s["gate"].contiguous()
+    s["x"], s["y"] = typed(case, normal(seed, 14, T, d)), typed(case, normal(seed, 15, T * k, d))
+    s["rows"] = torch.zeros_like(s["y"])         # the experts' inputs; rows behind the last choice stay zero
+    if case["train"]:
+        s["d_out"], s["d_rows"] = typed(case, normal(seed, 16, T, d)), typed(case, normal(seed, 17, T * k, d))
+        s["d_y"] = torch.zeros_like(s["y"])
+
+
+def embed_inputs(case, seed, s):
+    T, V, d, K = case["tokens"], case["vocab"], case["dim"], case["devices"]
+    s["tokens"] = words(case, seed, 21)
+    s["weight"] = typed(case, normal(seed, 25, V, d).mul_(0.1))
+    if case["train"]:
+        s["d_out"] = typed(case, normal(seed, 26, T, d).mul_(1e-3))
+        s["d_weight"] = typed(case, normal(seed, 27, K, V, d).mul_(1e-3), "grads")
+
+
+def norm_inputs(case, seed, s):
+    T, d, K = case["tokens"], case["dim"], case["devices"]
+    s["x"] = typed(case, normal(seed, 31, T, d) * (uniform(seed, 32, T, 1) * 2 + 0.5) + normal(seed, 33, T, 1) * 0.5)
+    s["weight"] = normal(seed, 34, d).mul_(0.1).add_(1.0)
+    s["bias"] = normal(seed, 35, d).mul_(0.1) if case["bias"] else None
+    if case["train"]:
+        s["d_y"] = typed(case, normal(seed, 36, T, d).mul_(1e-2))
+        s["d_weight"] = torch.zeros(K, d, dtype=torch.float32, device="cuda")
+        s["d_bias"] = torch.zeros_like(s["d_weight"]) if case["bias"] else None
+
+
+def loss_inputs(case, seed, s):
+    T, V, d, K = case["tokens"], case["vocab"], case["dim"], case["devices"]
+    s["x"] = typed(case, normal(seed, 41, T, d))
+    s["weight"] = typed(case, normal(seed, 42, V, d).mul_(1.5 / math.sqrt(d)))
+    s["target"] = words(case, seed, 43)
+    count = np.diff(s["off"])
+    s["weights"] = (count / max(1, count.sum())).astype(np.float32)
+    if case["train"]:
+        s["d_weight"] = torch.zeros(K, V, d, dtype=torch.bfloat16 if case["grads"] == "bf16" else torch.float32, device="cuda")
+
+
+def inputs(case, seed):
+    s = {"case": case, "off": bounds_of(case)}
+    {"order": order_inputs, "embed": embed_inputs, "norm": norm_inputs, "loss": loss_inputs}[case["op"]](case, seed, s)
+    s["device"] = torch.repeat_interleave(torch.arange(case["devices"], device="cuda"), torch.tensor(np.diff(s["off"]), device="cuda"))
+    return s
+
+
+def handle(s):
+    """What a program keeps of an operator from step to step."""
+    import paper_2301_08897_amd as sc
+    case = s["case"]
+    if case["op"] == "order":
+        return sc.ExpertOrder(case["experts"], case["k"], devices=case["devices"])
+    if case["op"] == "embed":
+        return sc.Embedding(case["vocab"], case["dim"], scale=SCALE, devices=case["devices"])
+    if case["op"] == "norm":
+        return sc.LayerNorm(case["dim"], eps=EPS, devices=case["devices"])
+    return sc.LinearCrossEntropy(case["vocab"], case["dim"], devices=case["devices"])
+
+
+def prepare(case, seed):
+    s = inputs(case, seed)
+    if own:
+        s["handle"] = handle(s)
+    return s
+
+
+# ---- plain forms --------------------------------------------------------------------------------
+
+def plain_order(s):
+    case = s["case"]
+    T, E, k, K, d = case["tokens"], case["experts"], case["k"], case["devices"], case["dim"]
+    kind, cells = s["x"].dtype, E * K
+    cell = torch.where(s["idx"] >= 0, s["idx"].to(torch.int64) * K + s["device"][:, None], cells).flatten()
+    src = torch.sort(cell, stable=True).indices
+    count = torch.zeros(cells + 1, dtype=torch.int64, device="cuda").scatter_add_(0, cell, torch.ones_like(cell))
+    bounds = torch.cumsum(count, 0) - count
+    there = (torch.arange(T * k, device="cuda") < bounds[cells])
+    pos = torch.empty_like(src).scatter_(0, src, torch.arange(T * k, device="cuda"))
+    here = (cell < cells)[:, None]
+    rows = torch.where(there[:, None], s["x"][src // k], 0)
+    part = torch.where(here, s["y"].float()[pos], 0.0).view(T, k, d)
+    gate = torch.where(here.view(T, k), s["gate"], 0.0)
+    out = {"pos": torch.where(here[:, 0], pos, -1).view(T, k).to(torch.int32), "src": torch.where(there, src, -1).to(torch.int32),
+           "bounds": bounds.to(torch.int32), "rows": rows, "out": (part * gate[:, :, None]).sum(dim=1).to(kind)}
+    if case["train"]:
+        g = s["d_out"].float()
+        out["d_gate"] = (part * g[:, None, :]).sum(dim=2)
+        out["d_y"] = torch.where(there[:, None], g[src // k] * gate.flatten()[src][:, None], 0.0).to(kind)
+        out["d_x"] = torch.where(here, s["d_rows"].float()[pos], 0.0).view(T, k, d).sum(dim=1).to(kind)
+    return out
+
+
+def plain_embed(s):
+    case, ids = s["case"], s["tokens"]
+    there, at = ids >= 0, ids.clamp(min=0)
+    out = {"out": torch.where(there[:, None], s["weight"][at].float() * SCALE, 0.0).to(s["weight"].dtype)}
+    if case["train"]:
+        V, d, K = case["vocab"], case["dim"], case["devices"]
+        g = s["d_out"].float() * SCALE * there[:, None]
+        total = torch.zeros(K * V, d, dtype=torch.float32, device="cuda").index_add_(0, s["device"] * V + at, g).view(K, V, d)
+        if case["add"]:
+            s["d_weight"].copy_(total + s["d_weight"].float())
+        else:
+            s["d_weight"].copy_(total)
+        out["d_weight"] = s["d_weight"]
+    return out
+
+
+def plain_norm(s):
+    case, x = s["case"], s["x"].float()
+    mean = x.mean(dim=1, keepdim=True)
+    c = x - mean
+    rstd = 1.0 / torch.sqrt((c * c).mean(dim=1, keepdim=True) + EPS)
+    h = c * rstd
+    y = h * s["weight"]
+    if case["bias"]:
+        y = y + s["bias"]
+    out = {"y": y.to(s["x"].dtype), "mean": mean[:, 0], "rstd": rstd[:, 0]}
+    if case["train"]:
+        g = s["d_y"].float()
+        w = g * s["weight"]
+        out["d_x"] = (rstd * (w - w.mean(dim=1, keepdim=True) - h * (w * h).mean(dim=1, keepdim=True))).to(s["x"].dtype)
+        cut = [b - a for a, b in zip(s["off"], s["off"][1:])]
+        out["d_weight"] = torch.stack([p.sum(dim=0) for p in torch.split(g * h, cut)])
+        if case["bias"]:
+            out["d_bias"] = torch.stack([p.sum(dim=0) for p in torch.split(g, cut)])
+    return out
+
+
+def plain_loss(s):
+    case, x, w = s["case"], s["x"].float(), s["weight"].float()
+    T, K = case["tokens"], case["devices"]
+    there, at = s["target"] >= 0, s["target"].clamp(min=0)[:, None]
+    z = x @ w.T
+    top = z.amax(dim=1, keepdim=True)
+    e = torch.exp(z - top)
+    total = e.sum(dim=1, keepdim=True)
+    lse = (top + total.log())[:, 0]
+    nll = torch.where(there, lse - z.gather(1, at)[:, 0], 0.0)
+    del z
+    one = there.float()
+    rows = torch.zeros(K, device="cuda").scatter_add_(0, s["device"], one)
+    share = 1.0 / rows.clamp(min=1.0)
+    each = torch.zeros(K, device="cuda").scatter_add_(0, s["device"], nll) * share
+    out = {"nll": nll, "lse": lse * one, "device_loss": each,
+           "loss": (each * torch.tensor(s["weights"], device="cuda")).sum()[None]}
+    if case["train"]:
+        g = (e / total).scatter_add_(1, at, torch.full((T, 1), -1.0, device="cuda"))
+        g = g * (share[s["device"]] * one)[:, None]
+        out["d_x"] = (g @ w).to(s["x"].dtype)
+        cut = [b - a for a, b in zip(s["off"], s["off"][1:])]
+        for d, (gd, xd) in enumerate(zip(torch.split(g, cut), torch.split(x, cut))):
+            s["d_weight"][d].copy_(gd.T @ xd)
+        out["d_weight"] = s["d_weight"]
+    return out
+
+
+# ---- one pass -----------------------------------------------------------------------------------
+
+def own_order(s, h):
+    r = h.sort(s["idx"], tok_off=s["off"])
+    out = {"pos": r.pos, "src": r.src, "bounds": r.bounds, "rows": h.dispatch(s["x"], r, out=s["rows"]),
+           "out": h.combine(s["y"], s["gate"], r)}
+    if s["case"]["train"]:
+        out["d_y"], out["d_gate"] = h.combine_backward(s["d_out"], s["y"], s["gate"], r, d_y=s["d_y"])
+        out["d_x"] = h.dispatch_backward(s["d_rows"], r)
+    return out
+
+
+def own_embed(s, h):
+    out = {"out": h.forward(s["tokens"], s["weight"])}
+    if s["case"]["train"]:
+        h.backward(s["tokens"], s["d_out"], s["d_weight"], tok_off=s["off"], accumulate=s["case"]["add"])
+        out["d_weight"] = s["d_weight"]
+    return out
+
+
+def own_norm(s, h):
+    f = h.forward(s["x"], s["weight"], s["bias"])
+    out = {"y": f.y, "mean": f.mean, "rstd": f.rstd}
+    if s["case"]["train"]:
+        out["d_x"] = h.backward(s["x"], s["weight"], f, s["d_y"], s["d_weight"], s["d_bias"], tok_off=s["off"])
+        out["d_weight"] = s["d_weight"]
+        if s["bias"] is not None:
+            out["d_bias"] = s["d_bias"]
+    return out
+
+
+def own_loss(s, h):
+    f = h.forward(s["x"], s["weight"], s["target"], tok_off=s["off"], weights=s["weights"])
+    out = {"nll": f.nll, "lse": f.lse, "device_loss": f.device_loss, "loss": f.loss}
+    if s["case"]["train"]:
+        # every device's own gradient, before the aggregation weights it
+        out["d_x"] = h.backward(s["x"], s["weight"], s["target"], f, s["d_weight"], tok_off=s["off"])
+        out["d_weight"] = s["d_weight"]
+    return out
+
+
+def run(s):
+    op = s["case"]["op"]
+    if not own:
+        return {"order": plain_order, "embed": plain_embed, "norm": plain_norm, "loss": plain_loss}[op](s)
+    return {"order": own_order, "embed": own_embed, "norm": own_norm, "loss": own_loss}[op](s, s["handle"])
+
+
+def work(case):
+    T, d, K, e = case["tokens"], case["dim"], case["devices"], 2 if case["type"] == "bf16" else 4
+    if case["op"] == "order":
+        n, k = T * case["k"], case["k"]
+        there = n * (0.9 if case["padding"] else 1.0)
+        byte, flop = n * 16 + case["experts"] * K * 4 + (T * 2 + there * 2) * d * e, 2 * there * d
+        if case["train"]:
+            byte, flop = byte + n * 4 + (T * 2 + there * 2) * d * e, flop + 4 * there * d
+        return {"bytes": int(byte), "flops": int(flop)}
+    if case["op"] == "embed":
+        byte, flop = T * 8 + (min(T, case["vocab"]) + T) * d * e, T * d
+        if case["train"]:
+            g = 2 if case["grads"] == "bf16" else 4
+            hit = min(T, K * case["vocab"]) * 2 if case["add"] else K * case["vocab"]
+            byte, flop = byte + T * d * e + hit * d * g, flop + 2 * T * d
+        return {"bytes": byte, "flops": flop}
+    if case["op"] == "norm":
+        byte, flop = T * d * 2 * e + T * 8 + d * 8, 8 * T * d
+        if case["train"]:
+            byte, flop = byte + T * d * 2 * e + K * d * 8, flop + 14 * T * d
+        return {"bytes": byte, "flops": flop}
+    V = case["vocab"]
+    byte, flop = (T + V) * d * e + T * 16, 2 * T * V * d
+    if case["train"]:
+        byte, flop = byte + T * d * e + K * V * d * (2 if case["grads"] == "bf16" else 4), 3 * flop
+    return {"bytes": byte, "flops": flop}
+
+
+# ---- the definition in 64 bits ------------------------------------------------------------------
+
+def exact(case, seed):
+    s = inputs(case, seed)
+    T, d, K = case["tokens"], case["dim"], case["devices"]
+    spans = list(zip(s["off"], s["off"][1:]))
+
+    def order():
+        E, k = case["experts"], case["k"]
+        idx = s["idx"].cpu().numpy().reshape(-1)
+        dev = np.repeat(np.arange(K), [(b - a) * k for a, b in spans])
+        key = np.where(idx >= 0, idx.astype(np.int64) * K + dev, E * K)
+        who = np.lexsort((np.arange(T * k), key))
+        n = int((idx >= 0).sum())
+        pos = np.full(T * k, -1, dtype=np.int32)
+        pos[who[:n]] = np.arange(n)
+        src = np.full(T * k, -1, dtype=np.int32)
+        src[:n] = who[:n]
+        bounds = np.searchsorted(key[who], np.arange(E * K + 1)).astype(np.int32)
+        tok = torch.from_numpy(who[:n] // k).cuda()
+        which = torch.from_numpy(who[:n]).cuda()
+        rows = torch.zeros_like(s["y"])
+        rows[:n] = s["x"][tok]
+        scale = s["gate"].flatten()[which].double()[:, None]
+        sums = lambda v: torch.zeros(T, d, dtype=torch.float64, device="cuda").index_add_(0, tok, v)  # noqa: E731
+        out = {"pos": torch.from_numpy(pos.reshape(T, k)), "src": torch.from_numpy(src), "bounds": torch.from_numpy(bounds), "rows": rows,
+               "out": sums(s["y"][:n].double() * scale)}
+        if case["train"]:
+            up = s["d_out"].double()[tok]
+            out["d_gate"] = torch.zeros(T * k, dtype=torch.float64, device="cuda")
+            out["d_gate"][which] = torch.linalg.vecdot(up, s["y"][:n].double())
+            out["d_gate"] = out["d_gate"].view(T, k)
+            out["d_y"] = torch.zeros(T * k, d, dtype=torch.float64, device="cuda")
+            out["d_y"][:n] = up.mul_(scale)
+            del up
+            out["d_x"] = sums(s["d_rows"][:n].double())
+        return out
+
+    def embed():
+        V, ids = case["vocab"], s["tokens"]
+        on = torch.nonzero(ids >= 0)[:, 0]
+        out = {"out": torch.zeros(T, d, dtype=torch.float64, device="cuda")}
+        out["out"][on] = s["weight"].double()[ids[on]] * SCALE
+        if case["train"]:
+            total = s["d_weight"].double() if case["add"] else torch.zeros(K, V, d, dtype=torch.float64, device="cuda")
+            for j, (a, b) in enumerate(spans):
+                mine = on[(on >= a) & (on < b)]
+                total[j].index_add_(0, ids[mine], s["d_out"][mine].double(), alpha=SCALE)
+            out["d_weight"] = total
+        return out
+
+    def norm():
+        x, w = s["x"].double(), s["weight"].double()
+        var, mean = torch.var_mean(x, dim=1, correction=0)
+        rstd = torch.rsqrt(var + EPS)
+        h = x.sub_(mean[:, None]).mul_(rstd[:, None])
+        y = h * w if s["bias"] is None else torch.addcmul(s["bias"].double()[None], h, w[None])
+        out = {"y": y, "mean": mean, "rstd": rstd}
+        if case["train"]:
+            g = s["d_y"].double()
+            out["d_weight"] = torch.stack([torch.linalg.vecdot(g[a:b], h[a:b], dim=0) for a, b in spans])
+            if s["bias"] is not None:
+                out["d_bias"] = torch.stack([g[a:b].sum(dim=0) for a, b in spans])
+            g.mul_(w)
+            along = torch.linalg.vecdot(g, h) / d
+            out["d_x"] = torch.addcmul(g - g.mean(dim=1, keepdim=True), h, along[:, None], value=-1).mul_(rstd[:, None])
+        return out
+
+    def loss():
+        V, x, w = case["vocab"], s["x"].double(), s["weight"].double()
+        ids = s["target"]
+        out = {"nll": torch.zeros(T, dtype=torch.float64, device="cuda"), "lse": torch.zeros(T, dtype=torch.float64, device="cuda"),
+               "device_loss": torch.zeros(K, dtype=torch.float64, device="cuda")}
+        if case["train"]:
+            out["d_x"] = torch.zeros_like(x)
+            out["d_weight"] = torch.zeros(K, V, d, dtype=torch.float64, device="cuda")
+        for j, (a, b) in enumerate(spans):
+            on = a + torch.nonzero(ids[a:b] >= 0)[:, 0]
+            for piece in torch.split(on, max(1, 2**28 // V)) if len(on) else []:
+                p = x[piece] @ w.T
+                top = torch.logsumexp(p, dim=1)
+                out["lse"][piece] = top
+                out["nll"][piece] = top - torch.gather(p, 1, ids[piece][:, None])[:, 0]
+                if case["train"]:
+                    p.sub_(top[:, None]).exp_()
+                    p[torch.arange(len(piece), device="cuda"), ids[piece]] -= 1.0
+                    p.div_(len(on))
+                    out["d_x"][piece] = p @ w
+                    out["d_weight"][j].addmm_(p.T.contiguous(), x[piece])
+            if len(on):
+                out["device_loss"][j] = out["nll"][a:b].sum() / len(on)
+        out["loss"] = torch.dot(out["device_loss"], torch.tensor(s["weights"], device="cuda").double())[None]
+        return out
+
+    return {"order": order, "embed": embed, "norm": norm, "loss": loss}[case["op"]]()
