@@ -301,7 +301,7 @@ def own_order(s, h):
     out = {"pos": r.pos, "src": r.src, "bounds": r.bounds, "rows": h.dispatch(s["x"], r, out=s["rows"]),
            "out": h.combine(s["y"], s["gate"], r)}
     if s["case"]["train"]:
-        out["d_y"], out["d_gate"] = h.combine_backward(s["d_out"], s["y"], s["gate"], r, d_y=s["d_y"])
+        out["d_y"], out["d_gate"] = h.combine_backward(s["d_out"], s["y"], s["gate"], r, d_rows=s["d_y"])
         out["d_x"] = h.dispatch_backward(s["d_rows"], r)
     return out
 
