@@ -555,6 +555,74 @@ scadles_status scadles_router_backward(const scadles_router* router, const void*
                                        const float* dgate, const float* dloss, void* dlogits, uint64_t ld_out,
                                        void* stream);
 
+/* ---- between tokens and logits of language models ------------------------------------------
+ * What a model trained on the K devices' streams needs beside the router and
+ * AdamW. The devices' rows lie one after the other in one batch, and every
+ * gradient of weights is one per device, without the devices' weights, for
+ * scadles_step_fused to compress and scadles_weighted_aggregate to weight.
+ * Elements are floats or bfloat16; sums, softmax statistics and means are kept
+ * in float at least and rounded once, to nearest, on the way out. Rows may lie
+ * `ld` elements apart (ld >= dim) at any address aligned to their elements; what
+ * lies between them is neither read nor written. Outputs may not overlap inputs
+ * or each other unless it is said.                                           */
+
+/* The rows of a batch: [tok_off[d], tok_off[d + 1]) are device d's.
+ *   tokens   0 <= tokens <= 2^31 - 1.
+ *   devices  1 <= devices <= SCADLES_MAX_DEVICES.
+ *   tok_off  (host[devices + 1]) from 0 to tokens, not decreasing.            */
+typedef struct scadles_batch {
+  uint64_t tokens;
+  const uint64_t* tok_off;
+  uint32_t devices;
+} scadles_batch;
+
+/* Tokens sorted by expert. The choices idx[t][c] of the tokens, k each, are
+ * sorted by expert, those of an expert by token (so by device), those of a token
+ * by c; an index outside [0, experts) is a missing choice and has no row.
+ *   idx     (dev, tokens x k, as scadles_router_forward gives it).
+ *   pos     (dev, tokens x k) row of each choice, -1 for a missing one.
+ *   src     (dev, tokens x k) src[r] = t * k + c of the choice in row r, -1
+ *           behind the last row.
+ *   bounds  (dev, experts * devices + 1) rows [bounds[e * devices + d],
+ *           bounds[e * devices + d + 1]) are the choices of expert e by device
+ *           d; the last entry is the number of rows.
+ * tokens * k <= 2^31 - 1; experts and k as for the router.                   */
+size_t scadles_order_workspace_bytes(uint64_t tokens, uint32_t experts, uint32_t k);
+scadles_status scadles_order_sort(const scadles_batch* batch, const int32_t* idx, uint32_t experts, uint32_t k,
+                                  int32_t* pos, int32_t* src, int32_t* bounds, void* ws, size_t ws_bytes, void* stream);
+
+/* The order that rows are moved by.
+ *   tokens, k, pos  as above; an entry of pos outside [0, tokens * k) is a
+ *                   missing choice. No two entries may be the same row.
+ *   dim             1 <= dim < 2^24.
+ *   type            SCADLES_F32 or SCADLES_BF16, of all rows.                 */
+typedef struct scadles_order {
+  uint64_t tokens;
+  const int32_t* pos;
+  uint32_t k, dim;
+  int32_t type;
+} scadles_order;
+
+/* rows[pos[t][c]] = x[t]: the experts' inputs. Rows behind the last one are left
+ * as they were. `rows` has tokens * k rows.                                  */
+scadles_status scadles_dispatch(const scadles_order* order, const void* x, uint64_t ld_x, void* rows, uint64_t ld_rows,
+                                void* stream);
+
+/* out[t] = sum_c gate[t][c] * rows[pos[t][c]], the gates (dev, tokens x k floats)
+ * all 1 for NULL, which is the gradient of scadles_dispatch. Choices are added in
+ * their order; a token without choices gets zeros. Neither the row nor the gate
+ * of a missing choice is read.                                               */
+scadles_status scadles_combine(const scadles_order* order, const void* rows, uint64_t ld_rows, const float* gate,
+                               void* out, uint64_t ld_out, void* stream);
+
+/* The gradient of scadles_combine: d_rows[pos[t][c]] = gate[t][c] * d_out[t], rows
+ * behind the last one left as they were, and d_gate[t][c] = the product of d_out[t]
+ * and rows[pos[t][c]], 0 for a missing choice. d_rows may be `rows` (with the same
+ * ld); d_rows or d_gate may be NULL.                                          */
+scadles_status scadles_combine_backward(const scadles_order* order, const void* d_out, uint64_t ld_d_out,
+                                        const void* rows, uint64_t ld_rows, const float* gate, void* d_rows,
+                                        uint64_t ld_d_rows, float* d_gate, void* stream);
+
 /* Message for the last non-OK status returned on the calling thread.        */
 const char* scadles_last_error(void);
 

@@ -1035,3 +1035,8 @@ class Router:
         if given:
             _written((d_logits,))
         return d_logits
+
+
+# ---- between tokens and logits ------------------------------------------------------------------------
+
+from .language import Batch, ExpertOrder, ExpertRows, OrderShape  # noqa: E402,F401

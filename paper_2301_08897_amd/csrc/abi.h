@@ -11,6 +11,7 @@
 namespace scadles {
 
 scadles_status fail(scadles_status st, const char* fmt, ...);
+scadles_status check_batch(const scadles_batch* b);
 
 inline scadles_status launch_status(hipError_t e, const char* where)
 {

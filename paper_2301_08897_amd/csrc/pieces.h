@@ -1,0 +1,127 @@
+// pieces.h -- 16 bytes of a row of float or bfloat16 elements that starts at
+// any address aligned to its elements (the memory system takes wide accesses
+// at that alignment), and how a workgroup's lanes share the pieces of rows.
+// Internal to libscadles.
+#pragma once
+
+#include "abi.h"
+#include "frame.h"
+
+namespace scadles {
+
+typedef u4 u4at4 __attribute__((aligned(4)));
+typedef u4 u4at2 __attribute__((aligned(2)));
+typedef float f8 __attribute__((ext_vector_type(8)));
+typedef __bf16 b8 __attribute__((ext_vector_type(8)));
+
+// What a type's 16 bytes are: N elements, as floats F.
+template <class X>
+struct Piece;
+template <>
+struct Piece<float> {
+  static constexpr uint32_t N = 4;
+  typedef f4 F;
+  typedef u4at4 Any;
+};
+template <>
+struct Piece<uint16_t> {     // bfloat16
+  static constexpr uint32_t N = 8;
+  typedef f8 F;
+  typedef u4at2 Any;
+};
+
+// The first k elements (all of them if there are N or more) at p; the rest read as zero.
+template <class X>
+__device__ inline u4 load_piece(const X* p, uint32_t k)
+{
+  if (k >= Piece<X>::N) return *(const GLOBAL typename Piece<X>::Any*)gptr(p);
+  u4 x = {0, 0, 0, 0};
+#pragma unroll
+  for (uint32_t q = 0; q < Piece<X>::N - 1; ++q)
+    if (q < k) {
+      if constexpr (sizeof(X) == 4) x[q] = __float_as_uint(gptr(p)[q]);
+      else x[q / 2] |= (uint32_t)gptr(p)[q] << (q % 2 * 16);
+    }
+  return x;
+}
+
+template <class X>
+__device__ inline void store_piece(X* p, u4 x, uint32_t k)
+{
+  if (k >= Piece<X>::N) {
+    *(GLOBAL typename Piece<X>::Any*)gptr(p) = x;
+    return;
+  }
+#pragma unroll
+  for (uint32_t q = 0; q < Piece<X>::N - 1; ++q)
+    if (q < k) {
+      if constexpr (sizeof(X) == 4) gptr(p)[q] = __uint_as_float(x[q]);
+      else gptr(p)[q] = (uint16_t)(x[q / 2] >> (q % 2 * 16));
+    }
+}
+
+// The same for data that is not read again soon.
+template <class X>
+__device__ inline void store_piece_once(X* p, u4 x, uint32_t k)
+{
+  if (k >= Piece<X>::N) __builtin_nontemporal_store((typename Piece<X>::Any)x, (GLOBAL typename Piece<X>::Any*)gptr(p));
+  else store_piece(p, x, k);
+}
+
+template <class X>
+__device__ inline typename Piece<X>::F unpack(u4 x)
+{
+  typename Piece<X>::F f;
+  if constexpr (sizeof(X) == 4) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) f[q] = __uint_as_float(x[q]);
+  } else {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      f[2 * q] = __uint_as_float(x[q] << 16);
+      f[2 * q + 1] = __uint_as_float(x[q] & 0xFFFF0000u);
+    }
+  }
+  return f;
+}
+
+// To bfloat16 to nearest, ties to even; floats as they are.
+template <class X>
+__device__ inline u4 pack(typename Piece<X>::F f)
+{
+  if constexpr (sizeof(X) == 4) return __builtin_bit_cast(u4, f);
+  else return __builtin_bit_cast(u4, __builtin_convertvector(f, b8));
+}
+
+// A workgroup of kBlock lanes takes `rows` rows of `pieces` pieces each, piece by
+// piece: place i is piece i % pieces of row i / pieces. The division is a
+// multiplication, exact for i * pieces < 2^32; with rows = 1 it is not needed.
+struct Share {
+  uint32_t pieces, rows, magic;
+};
+
+inline Share share_rows(uint64_t rows, uint64_t pieces)
+{
+  // enough pieces for every lane of a workgroup, and several where there are far
+  // more than the GPU's lanes
+  uint64_t each = rows * pieces / ((uint64_t)kBlock * 4096);
+  each = each < 1 ? 1 : each > 4 ? 4 : each;
+  uint64_t n = pieces > 1024 ? 1 : div_up(kBlock * each, pieces);
+  if (n > rows) n = rows ? rows : 1;
+  return {(uint32_t)pieces, (uint32_t)n, (uint32_t)(n == 1 ? 0 : div_up(1ull << 32, pieces))};
+}
+
+// Calls f(row of the workgroup, piece) for every place of this lane.
+template <class F>
+__device__ inline void for_pieces(const Share& s, F f)
+{
+  for (uint32_t i = threadIdx.x; i < s.rows * s.pieces; i += kBlock) {
+    const uint32_t r = s.rows == 1 ? 0u : s.pieces == 1 ? i : __umulhi(i, s.magic);
+    f(r, i - r * s.pieces);
+  }
+}
+
+// Bytes from the first to the last element of `rows` rows.
+inline uint64_t rows_bytes(uint64_t rows, uint64_t dim, uint64_t ld, uint64_t esize) { return rows ? ((rows - 1) * ld + dim) * esize : 0; }
+
+}  // namespace scadles
