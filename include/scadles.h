@@ -623,6 +623,69 @@ scadles_status scadles_combine_backward(const scadles_order* order, const void* 
                                         const void* rows, uint64_t ld_rows, const float* gate, void* d_rows,
                                         uint64_t ld_d_rows, float* d_gate, void* stream);
 
+/* Embedding: out[t] = scale * weight[tokens[t]], and the gradients of the table.
+ * A token outside [0, vocab) is padding: its row is zero and adds no gradient.
+ *   vocab       1 <= vocab; vocab * devices < 2^32 - 1.
+ *   dim         1 <= dim < 2^24.
+ *   type        of weight, out and d_out: SCADLES_F32 or SCADLES_BF16.
+ *   grad_type   of d_weight, the same.
+ *   token_bytes 4 or 8: signed integers of 32 or 64 bits.
+ *   scale       finite.                                                       */
+typedef struct scadles_embedding {
+  uint64_t vocab;
+  uint32_t dim;
+  int32_t type, grad_type, token_bytes;
+  float scale;
+} scadles_embedding;
+
+/*   weight  (dev, vocab rows).  out  (dev, tokens rows); tokens <= 2^31 - 1.   */
+scadles_status scadles_embedding_forward(const scadles_embedding* e, uint64_t tokens, const void* ids, const void* weight,
+                                         uint64_t ld_weight, void* out, uint64_t ld_out, void* stream);
+
+/* d_weight[d][v] = scale * sum of d_out[t] over device d's tokens t of id v, with
+ * `accumulate` added to what is there (rows without a token are then neither
+ * read nor written, else they become zero). The sums are taken over the tokens
+ * sorted by id, in pieces of 32 and then over those, in float and in an order
+ * that depends on the ids alone.
+ *   d_weight  (host[devices]) pointers to vocab x dim elements each (dev, no
+ *             two overlapping, aligned to their elements: parts of the devices'
+ *             flat gradients, at any offset).                                  */
+size_t scadles_embedding_workspace_bytes(uint64_t tokens, uint64_t vocab, uint32_t dim);
+scadles_status scadles_embedding_backward(const scadles_embedding* e, const scadles_batch* batch, const void* ids,
+                                          const void* d_out, uint64_t ld_d_out, void* const* d_weight, int accumulate,
+                                          void* ws, size_t ws_bytes, void* stream);
+
+/* Layer norm: h = (x - mean) * rstd over a row, rstd = 1 / sqrt(variance + eps),
+ * y = h * weight + bias. The variance is the mean of (x - mean)^2, in a second
+ * pass over the row that is kept on the chip.
+ *   dim          1 <= dim < 2^24.
+ *   type         of x, y, d_y and d_x: SCADLES_F32 or SCADLES_BF16.
+ *   weight_type  of weight and bias, the same.
+ *   eps          finite, >= 0.
+ *   bias         NULL for none.
+ *   mean, rstd   (dev, tokens floats) for the backward pass.                   */
+typedef struct scadles_norm {
+  uint32_t dim;
+  int32_t type, weight_type;
+  float eps;
+} scadles_norm;
+scadles_status scadles_layer_norm_forward(const scadles_norm* norm, uint64_t tokens, const void* x, uint64_t ld_x,
+                                          const void* weight, const void* bias, void* y, uint64_t ld_y, float* mean,
+                                          float* rstd, void* stream);
+
+/* With w = d_y * weight: d_x = rstd * (w - mean(w) - h * mean(w * h)), and for
+ * every device d_weight[d] = sum of d_y * h and d_bias[d] = sum of d_y over its
+ * rows (zero without rows), in float over the rows of a workgroup and then over
+ * the workgroups, in a fixed order.
+ *   d_weight, d_bias  (host[devices]) pointers to dim floats each (dev, no two
+ *                     overlapping), or NULL where they are not wanted.         */
+size_t scadles_layer_norm_workspace_bytes(uint64_t tokens, uint32_t dim);
+scadles_status scadles_layer_norm_backward(const scadles_norm* norm, const scadles_batch* batch, const void* x,
+                                           uint64_t ld_x, const void* weight, const float* mean, const float* rstd,
+                                           const void* d_y, uint64_t ld_d_y, void* d_x, uint64_t ld_d_x,
+                                           float* const* d_weight, float* const* d_bias, void* ws, size_t ws_bytes,
+                                           void* stream);
+
 /* Message for the last non-OK status returned on the calling thread.        */
 const char* scadles_last_error(void);
 

@@ -25,3 +25,42 @@ def combine(rows, gate, pos):
     on = (pos >= 0)[:, :, None]
     part = np.where(on, rows.astype(np.float64)[np.maximum(pos, 0)] * np.where(on, gate[:, :, None], 0.0), 0.0)
     return part.sum(axis=1), np.abs(part).sum(axis=1)
+
+
+# ---- embedding ------------------------------------------------------------------------------
+
+def embed(ids, weight, scale):
+    there = (ids >= 0) & (ids < len(weight))
+    return np.where(there[:, None], weight.astype(np.float64)[np.where(there, ids, 0)] * scale, 0.0)
+
+
+def embed_gradients(ids, d_out, vocab, scale, off):
+    """(gradients [devices, vocab, dim], sums of the terms' magnitudes)."""
+    K = len(off) - 1
+    total = np.zeros((K, vocab, d_out.shape[1]))
+    size = np.zeros_like(total)
+    for d in range(K):
+        for t in range(off[d], off[d + 1]):
+            if 0 <= ids[t] < vocab:
+                total[d, ids[t]] += scale * d_out[t]
+                size[d, ids[t]] += abs(scale) * np.abs(d_out[t])
+    return total, size
+
+
+# ---- layer norm -------------------------------------------------------------------------------
+
+def layer_norm(x, weight, bias, eps):
+    """(y, mean, rstd, h)."""
+    x = x.astype(np.float64)
+    mean = x.mean(axis=1, keepdims=True)
+    rstd = 1.0 / np.sqrt(((x - mean) ** 2).mean(axis=1, keepdims=True) + eps)
+    h = (x - mean) * rstd
+    return h * weight + (0.0 if bias is None else bias), mean[:, 0], rstd[:, 0], h
+
+
+def layer_norm_gradients(h, rstd, weight, d_y, off):
+    """(d_x, d_weight [devices, dim], d_bias)."""
+    w = d_y * weight
+    d_x = rstd[:, None] * (w - w.mean(axis=1, keepdims=True) - h * (w * h).mean(axis=1, keepdims=True))
+    cut = list(zip(off, off[1:]))
+    return d_x, np.stack([(d_y * h)[a:b].sum(axis=0) for a, b in cut]), np.stack([d_y[a:b].sum(axis=0) for a, b in cut])

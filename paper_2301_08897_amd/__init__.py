@@ -1039,4 +1039,5 @@ class Router:
 
 # ---- between tokens and logits ------------------------------------------------------------------------
 
-from .language import Batch, ExpertOrder, ExpertRows, OrderShape  # noqa: E402,F401
+from .language import (Batch, Embedding, EmbeddingShape, ExpertOrder, ExpertRows, LayerNorm,  # noqa: E402,F401
+                       LayerNormOutputs, NormShape, OrderShape)

@@ -432,15 +432,8 @@ extern "C" {
 size_t scadles_order_workspace_bytes(uint64_t tokens, uint32_t experts, uint32_t k)
 {
   if (!experts || experts > kMaxExperts || !k || k > kMaxChoices || k > experts || tokens > 0x7FFFFFFFull / k) return 0;
-  // the most chunks of any call of so many tokens or fewer: every device's last one may be partly filled
-  const uint64_t N = tokens * k;
-  uint64_t most = 0;
-  for (uint32_t r = 1; r <= kSortRounds; r *= 2) {
-    const uint64_t cap = (uint64_t)r * kSortBlock * 256;     // a call of more items takes more rounds
-    const uint64_t n = r < kSortRounds && N > cap ? cap : N;
-    if (n / (r * kSortBlock) > most) most = n / (r * kSortBlock);
-  }
-  return (size_t)sort_bytes(most + kMaxK, experts + 1);
+  // every device's last chunk may be partly filled
+  return (size_t)sort_bytes(sort_chunks(tokens * k) + kMaxK, experts + 1);
 }
 
 scadles_status scadles_order_sort(const scadles_batch* batch, const int32_t* idx, uint32_t experts, uint32_t k, int32_t* pos, int32_t* src,

@@ -158,4 +158,11 @@ inline uint32_t sort_rounds(uint64_t N)
   return r;
 }
 
+// The most chunks of any sort of N items or fewer.
+inline uint64_t sort_chunks(uint64_t N)
+{
+  const uint64_t few = div_up(N, kSortBlock), many = div_up(N, kSortChunk);
+  return many > 256 ? many : few < 256 ? few : 256;
+}
+
 }  // namespace scadles

@@ -1,5 +1,5 @@
 """What lies between tokens and logits of language models trained on K devices:
-tokens sorted by expert and back, beside the router. Part of the package's
+tokens sorted by expert and back, beside the router, the embedding and layer norm. Part of the package's
 binding (``scadles.h``, "between tokens and logits"): checks of tensors and
 marshalling.
 
@@ -30,6 +30,17 @@ class OrderShape(ctypes.Structure):
     _fields_ = [("tokens", _u64), ("pos", _vp), ("k", _u32), ("dim", _u32), ("type", ctypes.c_int32)]
 
 
+class EmbeddingShape(ctypes.Structure):
+    """scadles_embedding: a table and its types."""
+    _fields_ = [("vocab", _u64), ("dim", _u32), ("type", ctypes.c_int32), ("grad_type", ctypes.c_int32),
+                ("token_bytes", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class NormShape(ctypes.Structure):
+    """scadles_norm: a layer norm and its types."""
+    _fields_ = [("dim", _u32), ("type", ctypes.c_int32), ("weight_type", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
 _order_ws_bytes = _sc._sig("scadles_order_workspace_bytes", ctypes.c_size_t, _u64, _u32, _u32)
 _order_sort = _sc._sig("scadles_order_sort", ctypes.c_int, ctypes.POINTER(Batch), _vp, _u32, _u32, _vp, _vp, _vp, _vp,
                        ctypes.c_size_t, _vp)
@@ -37,6 +48,18 @@ _dispatch = _sc._sig("scadles_dispatch", ctypes.c_int, ctypes.POINTER(OrderShape
 _combine = _sc._sig("scadles_combine", ctypes.c_int, ctypes.POINTER(OrderShape), _vp, _u64, _vp, _vp, _u64, _vp)
 _combine_backward = _sc._sig("scadles_combine_backward", ctypes.c_int, ctypes.POINTER(OrderShape), _vp, _u64, _vp, _u64,
                              _vp, _vp, _u64, _vp, _vp)
+_embedding_forward = _sc._sig("scadles_embedding_forward", ctypes.c_int, ctypes.POINTER(EmbeddingShape), _u64, _vp, _vp, _u64,
+                              _vp, _u64, _vp)
+_embedding_ws_bytes = _sc._sig("scadles_embedding_workspace_bytes", ctypes.c_size_t, _u64, _u64, _u32)
+_embedding_backward = _sc._sig("scadles_embedding_backward", ctypes.c_int, ctypes.POINTER(EmbeddingShape),
+                               ctypes.POINTER(Batch), _vp, _vp, _u64, ctypes.POINTER(_vp), ctypes.c_int, _vp,
+                               ctypes.c_size_t, _vp)
+_layer_norm_forward = _sc._sig("scadles_layer_norm_forward", ctypes.c_int, ctypes.POINTER(NormShape), _u64, _vp, _u64, _vp,
+                               _vp, _vp, _u64, _vp, _vp, _vp)
+_layer_norm_ws_bytes = _sc._sig("scadles_layer_norm_workspace_bytes", ctypes.c_size_t, _u64, _u32)
+_layer_norm_backward = _sc._sig("scadles_layer_norm_backward", ctypes.c_int, ctypes.POINTER(NormShape),
+                                ctypes.POINTER(Batch), _vp, _u64, _vp, _vp, _vp, _vp, _u64, _vp, _u64,
+                                ctypes.POINTER(_vp), ctypes.POINTER(_vp), _vp, ctypes.c_size_t, _vp)
 
 
 # ---- arguments --------------------------------------------------------------------------------------
@@ -52,12 +75,13 @@ def _gpu(t, name, *dtypes):
 
 def _rows(t, name, rows, dim, *dtypes, like=None):
     """(address, elements between rows) of a [rows, dim] tensor whose rows' elements
-    are adjacent; any number of rows for None."""
+    are adjacent; any number for None."""
     _gpu(t, name, *dtypes)
     if like is not None and t.device != like.device:
         raise ValueError(f"{name} must be on {like.device}")
-    if t.dim() != 2 or t.shape[1] != dim or (rows is not None and t.shape[0] != rows):
-        raise ValueError(f"{name} must be [{'rows' if rows is None else rows}, {dim}], not {list(t.shape)}")
+    if t.dim() != 2 or rows not in (None, t.shape[0]) or dim not in (None, t.shape[1]):
+        raise ValueError(f"{name} must be [{'rows' if rows is None else rows}, {'dim' if dim is None else dim}], not {list(t.shape)}")
+    dim = t.shape[1]
     ld, step = t.stride()
     if dim > 1 and step != 1:
         raise ValueError(f"{name}: a row's elements must be adjacent")
@@ -140,6 +164,21 @@ def _output(t, name, rows, dim, dtype, like, stream):
     return (t,) + _rows(t, name, rows, dim, dtype, like=like)
 
 
+def _each(tensors, name, devices, shape, *dtypes, like):
+    """(the tensors, their addresses): one contiguous tensor of the shape for each device,
+    as a list or as a tensor [devices, ...]."""
+    torch, n = _sc._torch(), int(np.prod(shape, dtype=np.int64))
+    each = list(tensors) if not isinstance(tensors, torch.Tensor) else [tensors] if tuple(tensors.shape) == shape and devices == 1 \
+        else list(tensors.unbind(0)) if tensors.dim() == len(shape) + 1 else []
+    if len(each) != devices:
+        raise ValueError(f"{name} must be a tensor of {list(shape)} for each of {devices} devices")
+    for i, t in enumerate(each):
+        _whole(t, f"{name}[{i}]", n, *dtypes, like=like)
+        if t.dtype != each[0].dtype:
+            raise TypeError(f"{name} must be of one type")
+    return each, (_vp * devices)(*[t.data_ptr() for t in each])
+
+
 def _wrote(*tensors):
     """Tells autograd that the caller's tensors have been written."""
     given = [t for t in tensors if t is not None and not t.is_inference()]
@@ -199,7 +238,7 @@ class ExpertOrder:
 
     def dispatch(self, x, order: ExpertRows, *, out=None, stream=None):
         """The experts' input rows [T * k, dim]: row ``pos[t, c]`` is ``x[t]``."""
-        p, ld = _rows(x, "x", None, x.shape[-1], *_types())
+        p, ld = _rows(x, "x", None, None, *_types())
         T, dim = x.shape
         rows, q, ld_rows = _output(out, "out", T * self.k, dim, x.dtype, x, stream)
         _run(_dispatch, self._shape(order, x, T), p, ld, q, ld_rows, like=x, stream=stream)
@@ -218,7 +257,7 @@ class ExpertOrder:
 
     def _combine(self, rows, name, gate, order, out, out_name, stream):
         T = order.pos.shape[0]
-        p, ld = _rows(rows, name, T * self.k, rows.shape[-1], *_types())
+        p, ld = _rows(rows, name, T * self.k, None, *_types())
         sums, q, ld_out = _output(out, out_name, T, rows.shape[1], rows.dtype, rows, stream)
         _run(_combine, self._shape(order, rows, T), p, ld, gate, q, ld_out, like=rows, stream=stream)
         _wrote(out)
@@ -228,7 +267,7 @@ class ExpertOrder:
         """Gradients of ``rows`` [T * k, dim] (in ``d_rows`` if given, which may be ``rows``
         itself) and of the gates, float32 [T, k], 0 where a choice is missing."""
         T, f32 = order.pos.shape[0], _types()[0]
-        p, ld = _rows(rows, "rows", T * self.k, rows.shape[-1], *_types())
+        p, ld = _rows(rows, "rows", T * self.k, None, *_types())
         up, ld_up = _rows(d_out, "d_out", T, rows.shape[1], rows.dtype, like=rows)
         g = _whole(gate, "gate", T * self.k, f32, like=rows)
         to, q, ld_to = _output(d_rows, "d_rows", T * self.k, rows.shape[1], rows.dtype, rows, stream)
@@ -236,3 +275,119 @@ class ExpertOrder:
         _run(_combine_backward, self._shape(order, rows, T), up, ld_up, p, ld, g, q, ld_to, d_gate.data_ptr(), like=rows, stream=stream)
         _wrote(d_rows)
         return to, d_gate
+
+
+# ---- embedding ------------------------------------------------------------------------------------------
+
+class Embedding:
+    """Rows of a table [vocab, dim] by token, times ``scale``, and the table's gradients
+    by sorted tokens, one for each device (scadles_embedding_forward, _backward). Tokens
+    outside the vocabulary are padding: rows of zeros, without gradient."""
+
+    def __init__(self, vocab: int, dim: int, *, scale: float = 1.0, devices: int = 1):
+        self.vocab, self.dim, self.scale, self.devices = int(vocab), int(dim), float(scale), int(devices)
+        if not 1 <= self.devices <= _sc.MAX_DEVICES or not 1 <= self.dim < 2**24 or not 1 <= self.vocab * self.devices < 2**32 - 1 \
+                or not np.isfinite(np.float32(self.scale)):
+            raise _sc.ScadlesError(1, f"invalid vocab={vocab}, dim={dim}, scale={scale} or devices={devices}")
+
+    def _tokens(self, tokens, like):
+        torch = _sc._torch()
+        return _whole(tokens, "tokens", tokens.numel(), torch.int32, torch.int64, like=like)
+
+    def _shape(self, tokens, x, grad=0):
+        return EmbeddingShape(self.vocab, self.dim, _type_of(x), grad, tokens.element_size(), self.scale)
+
+    def forward(self, tokens, weight, *, out=None, stream=None):
+        """``tokens`` int32 or int64, contiguous, of any shape; ``weight`` [vocab, dim]
+        float32 or bfloat16. Returns [tokens, dim] of the weight's type."""
+        p, ld = _rows(weight, "weight", self.vocab, self.dim, *_types())
+        ids, T = self._tokens(tokens, weight), tokens.numel()
+        rows, q, ld_out = _output(out, "out", T, self.dim, weight.dtype, weight, stream)
+        _run(_embedding_forward, self._shape(tokens, weight), T, ids, p, ld, q, ld_out, like=weight, stream=stream)
+        _wrote(out)
+        return rows
+
+    def backward(self, tokens, d_out, d_weight, *, tok_off=None, accumulate: bool = False, stream=None):
+        """Writes the table's gradients under ``d_out`` [tokens, dim] into ``d_weight``: a
+        contiguous tensor of vocab * dim elements for each device, float32 or bfloat16 (a
+        part of its flat gradient will do, at any offset), or one tensor [devices, vocab,
+        dim]. ``accumulate`` adds to what is there (a table that the logits use too). Tokens
+        ``tok_off[d]`` to ``tok_off[d + 1]`` are device d's. Returns ``d_weight``."""
+        p, ld = _rows(d_out, "d_out", None, self.dim, *_types())
+        T = d_out.shape[0]
+        ids = self._tokens(tokens, d_out)
+        if tokens.numel() != T:
+            raise ValueError(f"tokens must have {T} entries")
+        batch = _batch(T, tok_off, self.devices)
+        each, at = _each(d_weight, "d_weight", self.devices, (self.vocab, self.dim), *_types(), like=d_out)
+        ws = _scratch(_embedding_ws_bytes(T, self.vocab, self.dim), d_out, stream)
+        _run(_embedding_backward, self._shape(tokens, d_out, _type_of(each[0])), batch, ids, p, ld, at, int(bool(accumulate)),
+             ws.data_ptr(), ws.numel(), like=d_out, stream=stream)
+        _wrote(*each)
+        return d_weight
+
+
+# ---- layer norm -----------------------------------------------------------------------------------------
+
+@dataclass
+class LayerNormOutputs:
+    """What ``LayerNorm.forward`` returns."""
+    y: object            # [T, dim]
+    mean: object         # float32 [T]
+    rstd: object         # float32 [T]: 1 / sqrt(variance + eps)
+
+
+class LayerNorm:
+    """Layer norm over rows of ``dim`` elements, float32 or bfloat16, and its gradients,
+    those of the weights one for each device (scadles_layer_norm_forward, _backward).
+    Weight and bias are both float32 or both bfloat16."""
+
+    def __init__(self, dim: int, *, eps: float = 1e-5, devices: int = 1):
+        self.dim, self.eps, self.devices = int(dim), float(eps), int(devices)
+        if not 1 <= self.dim < 2**24 or not 1 <= self.devices <= _sc.MAX_DEVICES or not 0 <= np.float32(self.eps) < np.inf:
+            raise _sc.ScadlesError(1, f"invalid dim={dim}, eps={eps} or devices={devices}")
+
+    def _shape(self, x, weight):
+        return NormShape(self.dim, _type_of(x), _type_of(weight), self.eps)
+
+    def forward(self, x, weight, bias=None, *, out=None, stream=None) -> LayerNormOutputs:
+        """``x`` [T, dim]; ``y`` is of its type."""
+        f32 = _types()[0]
+        p, ld = _rows(x, "x", None, self.dim, *_types())
+        w = _whole(weight, "weight", self.dim, *_types(), like=x)
+        b = None if bias is None else _whole(bias, "bias", self.dim, weight.dtype, like=x)
+        T = x.shape[0]
+        y, q, ld_y = _output(out, "out", T, self.dim, x.dtype, x, stream)
+        both = _new((2, T), f32, x, stream)
+        m = both.data_ptr()
+        _run(_layer_norm_forward, self._shape(x, weight), T, p, ld, w, b, q, ld_y, m, m + 4 * T, like=x, stream=stream)
+        _wrote(out)
+        return LayerNormOutputs(y, both[0], both[1])
+
+    def backward(self, x, weight, out: LayerNormOutputs, d_y, d_weight=None, d_bias=None, *, tok_off=None, d_x=None, stream=None):
+        """The gradient of ``x`` [T, dim] (in ``d_x`` if given) under ``d_y``, and those of
+        weight and bias into ``d_weight`` and ``d_bias``: a contiguous float32 tensor of
+        dim elements for each device (a part of its flat gradient will do), or one tensor
+        [devices, dim]; None where they are not wanted. ``out`` is the forward pass's
+        (its mean and rstd are read); rows ``tok_off[d]`` to ``tok_off[d + 1]`` are device d's."""
+        f32 = _types()[0]
+        p, ld = _rows(x, "x", None, self.dim, *_types())
+        T = x.shape[0]
+        w = _whole(weight, "weight", self.dim, *_types(), like=x)
+        g, ld_g = _rows(d_y, "d_y", T, self.dim, x.dtype, like=x)
+        mean, rstd = _whole(out.mean, "mean", T, f32, like=x), _whole(out.rstd, "rstd", T, f32, like=x)
+        if tok_off is None and d_weight is None and d_bias is None:
+            batch = _batch(T, None, 1)
+        else:
+            batch = _batch(T, tok_off, self.devices)
+        given, at = [], []
+        for t, name in ((d_weight, "d_weight"), (d_bias, "d_bias")):
+            each, where = ([], None) if t is None else _each(t, name, self.devices, (self.dim,), f32, like=x)
+            given += each
+            at.append(where)
+        dx, q, ld_dx = _output(d_x, "d_x", T, self.dim, x.dtype, x, stream)
+        ws = _scratch(_layer_norm_ws_bytes(T, self.dim), x, stream)
+        _run(_layer_norm_backward, self._shape(x, weight), batch, p, ld, w, mean, rstd, g, ld_g, q, ld_dx, at[0], at[1],
+             ws.data_ptr(), ws.numel(), like=x, stream=stream)
+        _wrote(d_x, *given)
+        return dx
