@@ -686,6 +686,71 @@ scadles_status scadles_layer_norm_backward(const scadles_norm* norm, const scadl
                                            float* const* d_weight, float* const* d_bias, void* ws, size_t ws_bytes,
                                            void* stream);
 
+/* Cross entropy of a linear layer over a vocabulary, without its logits being kept:
+ *   z = weight x[t], lse[t] = log sum_v exp(z_v), nll[t] = lse[t] - z_target,
+ *   device_loss[d] = share[d] * sum of nll over device d's counted rows, with
+ *   share[d] = 1 / counted rows (0 without rows),
+ *   loss = sum_d weights[d] * device_loss[d].
+ * A row whose target is outside [0, vocab) is not counted: nll, lse and gradient
+ * are 0, and nothing of the row goes into any other result. The backward pass
+ * computes the logits again, a piece of the vocabulary at a time:
+ *   G = weights[d] * share[d] * d_loss * (softmax(z) - onehot(target)),
+ *   d_x = G weight, d_weight[d] = G^T x over device d's rows.
+ * Products are bfloat16 matrix products with sums in float. Floats are taken
+ * apart into three bfloat16 parts (all of their 24 bits), whose six largest
+ * products are added; G is rounded to bfloat16 for gradients in bfloat16, and
+ * taken apart alike for gradients in float. Elements that are not finite make
+ * what they go into NaN (infinities of bfloat16 x and weight as in exact
+ * arithmetic in the forward pass).
+ *   vocab         1 <= vocab <= 2^22; tokens <= 2^22.
+ *   dim           1 <= dim <= 65536.
+ *   type          of x, weight and d_x: SCADLES_F32 or SCADLES_BF16.
+ *   grad_type     of d_weight, the same.
+ *   target_bytes  4 or 8: signed integers of 32 or 64 bits.                    */
+typedef struct scadles_cross_entropy {
+  uint64_t vocab;
+  uint32_t dim;
+  int32_t type, grad_type, target_bytes;
+} scadles_cross_entropy;
+
+/* What the forward pass writes and the backward pass reads (dev, 4-byte aligned):
+ * nll and lse tokens, device_loss and share devices, loss 1.                 */
+typedef struct scadles_cross_entropy_out {
+  float* nll;
+  float* lse;
+  float* device_loss;
+  float* share;
+  float* loss;
+} scadles_cross_entropy_out;
+
+/* Workspace bytes of a call for so many tokens or fewer, of the forward pass or
+ * (backward = 1) of the backward pass; 0 for arguments that the call would reject. */
+size_t scadles_cross_entropy_workspace_bytes(const scadles_cross_entropy* ce, uint64_t tokens, uint32_t devices,
+                                             int backward);
+
+/*   weights  (host[devices]) finite and >= 0, as of Eqn 4a (they need not sum to 1).
+ *   target   (dev, tokens integers).                                          */
+scadles_status scadles_cross_entropy_forward(const scadles_cross_entropy* ce, const scadles_batch* batch,
+                                             const float* weights, const void* x, uint64_t ld_x, const void* weight,
+                                             uint64_t ld_weight, const void* target,
+                                             const scadles_cross_entropy_out* out, void* ws, size_t ws_bytes,
+                                             void* stream);
+
+/*   weights   the forward pass's give the gradient of loss; ones give each device's
+ *             of its own device_loss, for scadles_weighted_aggregate to weight.
+ *   out       the forward pass's; only lse and share are read.
+ *   d_loss    (dev, 1 float) or NULL (1).
+ *   d_x       (dev, tokens rows), the sum over the vocabulary.
+ *   d_weight  (host[devices]) pointers to vocab x dim elements each (dev, no two
+ *             overlapping, aligned to their elements: parts of the devices' flat
+ *             gradients, at any offset), or NULL where they are not wanted.    */
+scadles_status scadles_cross_entropy_backward(const scadles_cross_entropy* ce, const scadles_batch* batch,
+                                              const float* weights, const void* x, uint64_t ld_x, const void* weight,
+                                              uint64_t ld_weight, const void* target,
+                                              const scadles_cross_entropy_out* out, const float* d_loss, void* d_x,
+                                              uint64_t ld_d_x, void* const* d_weight, void* ws, size_t ws_bytes,
+                                              void* stream);
+
 /* Message for the last non-OK status returned on the calling thread.        */
 const char* scadles_last_error(void);
 

@@ -64,3 +64,29 @@ def layer_norm_gradients(h, rstd, weight, d_y, off):
     d_x = rstd[:, None] * (w - w.mean(axis=1, keepdims=True) - h * (w * h).mean(axis=1, keepdims=True))
     cut = list(zip(off, off[1:]))
     return d_x, np.stack([(d_y * h)[a:b].sum(axis=0) for a, b in cut]), np.stack([d_y[a:b].sum(axis=0) for a, b in cut])
+
+
+# ---- cross entropy of a linear layer --------------------------------------------------------------
+
+def cross_entropy(x, weight, target, off, weights):
+    """(logits, nll, lse, device_loss, share, loss); rows of other targets are not counted."""
+    z = x.astype(np.float64) @ weight.astype(np.float64).T
+    on = (target >= 0) & (target < len(weight))
+    top = z.max(axis=1)
+    with np.errstate(invalid="ignore"):
+        lse = np.where(on, top + np.log(np.exp(z - top[:, None]).sum(axis=1)), 0.0)
+    nll = np.where(on, lse - z[np.arange(len(z)), np.where(on, target, 0)], 0.0)
+    rows = np.array([on[a:b].sum() for a, b in zip(off, off[1:])])
+    share = np.where(rows > 0, 1.0 / np.maximum(rows, 1), 0.0)
+    each = np.array([nll[a:b].sum() for a, b in zip(off, off[1:])]) * share
+    return z, nll, lse, each, share, float((each * weights).sum())
+
+
+def cross_entropy_gradients(x, weight, target, off, z, lse, scale):
+    """(G, d_x, d_weight [devices, vocab, dim]) with scale [devices] = weight * share."""
+    on = (target >= 0) & (target < len(weight))
+    g = np.exp(z - lse[:, None])
+    g[np.arange(len(z))[on], target[on]] -= 1.0
+    g = np.where(on[:, None], g * np.repeat(scale, np.diff(off))[:, None], 0.0)
+    x = np.where(on[:, None], x, 0.0)
+    return g, g @ weight, np.stack([g[a:b].T @ x[a:b] for a, b in zip(off, off[1:])])

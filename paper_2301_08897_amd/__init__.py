@@ -1039,5 +1039,6 @@ class Router:
 
 # ---- between tokens and logits ------------------------------------------------------------------------
 
-from .language import (Batch, Embedding, EmbeddingShape, ExpertOrder, ExpertRows, LayerNorm,  # noqa: E402,F401
-                       LayerNormOutputs, NormShape, OrderShape)
+from .language import (Batch, CrossEntropyOut, CrossEntropyOutputs, CrossEntropyShape, Embedding,  # noqa: E402,F401
+                       EmbeddingShape, ExpertOrder, ExpertRows, LayerNorm, LayerNormOutputs, LinearCrossEntropy,
+                       NormShape, OrderShape)

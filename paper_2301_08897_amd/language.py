@@ -41,6 +41,17 @@ class NormShape(ctypes.Structure):
     _fields_ = [("dim", _u32), ("type", ctypes.c_int32), ("weight_type", ctypes.c_int32), ("eps", ctypes.c_float)]
 
 
+class CrossEntropyShape(ctypes.Structure):
+    """scadles_cross_entropy: a linear layer over a vocabulary and its types."""
+    _fields_ = [("vocab", _u64), ("dim", _u32), ("type", ctypes.c_int32), ("grad_type", ctypes.c_int32),
+                ("target_bytes", ctypes.c_int32)]
+
+
+class CrossEntropyOut(ctypes.Structure):
+    """scadles_cross_entropy_out: what the forward pass writes."""
+    _fields_ = [("nll", _vp), ("lse", _vp), ("device_loss", _vp), ("share", _vp), ("loss", _vp)]
+
+
 _order_ws_bytes = _sc._sig("scadles_order_workspace_bytes", ctypes.c_size_t, _u64, _u32, _u32)
 _order_sort = _sc._sig("scadles_order_sort", ctypes.c_int, ctypes.POINTER(Batch), _vp, _u32, _u32, _vp, _vp, _vp, _vp,
                        ctypes.c_size_t, _vp)
@@ -60,6 +71,15 @@ _layer_norm_ws_bytes = _sc._sig("scadles_layer_norm_workspace_bytes", ctypes.c_s
 _layer_norm_backward = _sc._sig("scadles_layer_norm_backward", ctypes.c_int, ctypes.POINTER(NormShape),
                                 ctypes.POINTER(Batch), _vp, _u64, _vp, _vp, _vp, _vp, _u64, _vp, _u64,
                                 ctypes.POINTER(_vp), ctypes.POINTER(_vp), _vp, ctypes.c_size_t, _vp)
+_cross_entropy_ws_bytes = _sc._sig("scadles_cross_entropy_workspace_bytes", ctypes.c_size_t,
+                                   ctypes.POINTER(CrossEntropyShape), _u64, _u32, ctypes.c_int)
+_cross_entropy_forward = _sc._sig("scadles_cross_entropy_forward", ctypes.c_int, ctypes.POINTER(CrossEntropyShape),
+                                  ctypes.POINTER(Batch), ctypes.POINTER(ctypes.c_float), _vp, _u64, _vp, _u64, _vp,
+                                  ctypes.POINTER(CrossEntropyOut), _vp, ctypes.c_size_t, _vp)
+_cross_entropy_backward = _sc._sig("scadles_cross_entropy_backward", ctypes.c_int, ctypes.POINTER(CrossEntropyShape),
+                                   ctypes.POINTER(Batch), ctypes.POINTER(ctypes.c_float), _vp, _u64, _vp, _u64, _vp,
+                                   ctypes.POINTER(CrossEntropyOut), _vp, _vp, _u64, ctypes.POINTER(_vp), _vp,
+                                   ctypes.c_size_t, _vp)
 
 
 # ---- arguments --------------------------------------------------------------------------------------
@@ -390,4 +410,85 @@ class LayerNorm:
         _run(_layer_norm_backward, self._shape(x, weight), batch, p, ld, w, mean, rstd, g, ld_g, q, ld_dx, at[0], at[1],
              ws.data_ptr(), ws.numel(), like=x, stream=stream)
         _wrote(d_x, *given)
+        return dx
+
+
+# ---- cross entropy of a linear layer ----------------------------------------------------------------------
+
+@dataclass
+class CrossEntropyOutputs:
+    """What ``LinearCrossEntropy.forward`` returns, all float32."""
+    nll: object          # [T]: 0 where the target is outside the vocabulary
+    lse: object          # [T]: log sum exp of the logits, 0 alike
+    device_loss: object  # [devices]: mean of nll over the device's counted rows
+    share: object        # [devices]: 1 / counted rows
+    loss: object         # [1]: the devices' losses with their weights
+
+
+class LinearCrossEntropy:
+    """The cross entropy of a linear layer ``x @ weight.T`` over a vocabulary, without its
+    logits being kept, and the gradients, those of the weight one for each device
+    (scadles_cross_entropy_forward, _backward). ``x`` [T, dim] and ``weight`` [vocab, dim]
+    are both float32 or both bfloat16; ``target`` int32 or int64 [T], outside the
+    vocabulary for rows that are not counted."""
+
+    def __init__(self, vocab: int, dim: int, *, devices: int = 1):
+        self.vocab, self.dim, self.devices = int(vocab), int(dim), int(devices)
+        if not 1 <= self.vocab <= 2**22 or not 1 <= self.dim <= 65536 or not 1 <= self.devices <= _sc.MAX_DEVICES:
+            raise _sc.ScadlesError(1, f"invalid vocab={vocab}, dim={dim} or devices={devices}")
+
+    def _arguments(self, x, weight, target, tok_off, grad):
+        torch = _sc._torch()
+        p, ld = _rows(x, "x", None, self.dim, *_types())
+        w, ld_w = _rows(weight, "weight", self.vocab, self.dim, x.dtype, like=x)
+        T = x.shape[0]
+        ids = _whole(target, "target", T, torch.int32, torch.int64, like=x)
+        batch = _batch(T, tok_off, self.devices)
+        return T, CrossEntropyShape(self.vocab, self.dim, _type_of(x), grad, target.element_size()), batch, (p, ld, w, ld_w, ids)
+
+    def _weights(self, weights):
+        if len(weights) != self.devices:
+            raise ValueError(f"weights must have {self.devices} entries")
+        return (ctypes.c_float * self.devices)(*[float(w) for w in weights])
+
+    def forward(self, x, weight, target, *, tok_off=None, weights=None, stream=None) -> CrossEntropyOutputs:
+        """Rows ``tok_off[d]`` to ``tok_off[d + 1]`` are device d's. ``weights``: Eqn 4a, by
+        default the devices' shares of the rows."""
+        f32 = _types()[0]
+        T, shape, batch, args = self._arguments(x, weight, target, tok_off, 0)
+        if weights is None:
+            weights = [(batch.tok_off[d + 1] - batch.tok_off[d]) / T if T else 1.0 / self.devices for d in range(self.devices)]
+        K = self.devices
+        buf = _new((2 * T + 2 * K + 1,), f32, x, stream)
+        q = buf.data_ptr()
+        at = CrossEntropyOut(q, q + 4 * T, q + 8 * T, q + 8 * T + 4 * K, q + 8 * T + 8 * K)
+        ws = _scratch(_cross_entropy_ws_bytes(shape, T, K, 0), x, stream)
+        _run(_cross_entropy_forward, shape, batch, self._weights(weights), *args, at, ws.data_ptr(), ws.numel(), like=x, stream=stream)
+        return CrossEntropyOutputs(buf[:T], buf[T:2 * T], buf[2 * T:2 * T + K], buf[2 * T + K:2 * T + 2 * K], buf[2 * T + 2 * K:])
+
+    def backward(self, x, weight, target, out: CrossEntropyOutputs, d_weight=None, *, tok_off=None, weights=None, d_loss=None, d_x=None,
+                 stream=None):
+        """The gradient of ``x`` [T, dim] (in ``d_x`` if given), and those of the weight into
+        ``d_weight``: a contiguous tensor of vocab * dim elements for each device, float32
+        or bfloat16 (a part of its flat gradient will do, at any offset), or one tensor
+        [devices, vocab, dim]; None where they are not wanted. ``out`` is the forward
+        pass's (its lse and share are read). ``weights``: by default ones, so that every
+        device has the gradient of its own loss, before the aggregation weights it; the
+        forward pass's give the gradient of its ``loss``. All of it times ``d_loss``, one
+        float32 on the GPU, if given."""
+        f32 = _types()[0]
+        each, where, grad = [], None, 0
+        if d_weight is not None:
+            each, where = _each(d_weight, "d_weight", self.devices, (self.vocab, self.dim), *_types(), like=x)
+            grad = _type_of(each[0])
+        elif isinstance(x, _sc._torch().Tensor):
+            grad = _type_of(x)
+        T, shape, batch, args = self._arguments(x, weight, target, tok_off, grad)
+        lse, share = _whole(out.lse, "lse", T, f32, like=x), _whole(out.share, "share", self.devices, f32, like=x)
+        d = None if d_loss is None else _whole(d_loss, "d_loss", 1, f32, like=x)
+        dx, q, ld_dx = _output(d_x, "d_x", T, self.dim, x.dtype, x, stream)
+        ws = _scratch(_cross_entropy_ws_bytes(shape, T, self.devices, 1), x, stream)
+        _run(_cross_entropy_backward, shape, batch, None if weights is None else self._weights(weights), *args,
+             CrossEntropyOut(None, lse, None, share, None), d, q, ld_dx, where, ws.data_ptr(), ws.numel(), like=x, stream=stream)
+        _wrote(d_x, *each)
         return dx
