@@ -696,12 +696,14 @@ scadles_status scadles_layer_norm_backward(const scadles_norm* norm, const scadl
  * computes the logits again, a piece of the vocabulary at a time:
  *   G = weights[d] * share[d] * d_loss * (softmax(z) - onehot(target)),
  *   d_x = G weight, d_weight[d] = G^T x over device d's rows.
- * Products are bfloat16 matrix products with sums in float. Floats are taken
- * apart into three bfloat16 parts (all of their 24 bits), whose six largest
- * products are added; G is rounded to bfloat16 for gradients in bfloat16, and
- * taken apart alike for gradients in float. Elements that are not finite make
- * what they go into NaN (infinities of bfloat16 x and weight as in exact
- * arithmetic in the forward pass).
+ * Products are those of the matrix cores, with sums in float. bfloat16 x and
+ * weight are multiplied as they are, and G is rounded to bfloat16 where all gradients
+ * are bfloat16. Else numbers are taken as sums of two half floats (22 bits), after
+ * a power of two has brought the largest of their row (for the logits) or column
+ * (for the gradients) to 2^13 .. 2^14, so that they are off by 2^-22 of their size or
+ * 2^-38 of that largest one; G alike, by 2^-22 of its size or 2^-38. Elements that are
+ * not finite make what they go into NaN (infinities of bfloat16 x and weight as
+ * in exact arithmetic in the forward pass).
  *   vocab         1 <= vocab <= 2^22; tokens <= 2^22.
  *   dim           1 <= dim <= 65536.
  *   type          of x, weight and d_x: SCADLES_F32 or SCADLES_BF16.
@@ -723,10 +725,9 @@ typedef struct scadles_cross_entropy_out {
   float* loss;
 } scadles_cross_entropy_out;
 
-/* Workspace bytes of a call for so many tokens or fewer, of the forward pass or
- * (backward = 1) of the backward pass; 0 for arguments that the call would reject. */
-size_t scadles_cross_entropy_workspace_bytes(const scadles_cross_entropy* ce, uint64_t tokens, uint32_t devices,
-                                             int backward);
+/* Workspace bytes of a call with this batch, of the forward pass or (backward = 1) of
+ * the backward pass; 0 for arguments that the call would reject.              */
+size_t scadles_cross_entropy_workspace_bytes(const scadles_cross_entropy* ce, const scadles_batch* batch, int backward);
 
 /*   weights  (host[devices]) finite and >= 0, as of Eqn 4a (they need not sum to 1).
  *   target   (dev, tokens integers).                                          */

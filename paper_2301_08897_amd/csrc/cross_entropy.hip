@@ -2,19 +2,30 @@
 // gradients, without the logits being kept.
 //
 //   z = weight x[t],  lse = log sum exp z,  nll = lse - z_target
-//   G = c_t (softmax(z) - onehot),  d_x = G weight,  d_weight[d] = G^T x over device d
+//   G = softmax(z) - onehot,  d_x = c_t G weight,  d_weight[d] = c_d G^T x over device d
 //
-// Forward: k_logits multiplies a tile of 256 vocabulary entries by 256 tokens and leaves,
-// in place of its logits, each token's maximum and sum of exponentials over the tile;
+// Forward: k_logits multiplies tiles of 256 vocabulary entries by 256 tokens and leaves,
+// in place of a tile's logits, each token's maximum and sum of exponentials over it;
 // k_loss_rows joins the tiles of a token. Backward, for a piece of the vocabulary at a
 // time: k_logits again, which now has lse and stores G of the piece both ways round,
 // tokens by vocabulary for d_x and vocabulary by tokens for d_weight; then k_gradients,
 // tiles of both products in one launch. x and weight are needed with the contraction's
 // index adjacent, so that k_turn writes both transposed once per call.
 //
+// Types. bfloat16 x and weight are multiplied where they lie; G is rounded to bfloat16 for
+// bfloat16 gradients. For the rest, numbers are sums of two half floats (22 bits), scaled by
+// powers of two: x and weight by row for the logits, by column for the gradients,
+// where the largest of a row or column comes to 2^13 .. 2^14; G by 2^13. Three
+// products of such parts, the fourth being below 2^-22 of the first, have the precision of
+// sums in float: six products of three bfloat16 parts have it too, and took twice
+// as long.
+//
 // Tokens are counted with every device's first one at a multiple of 64 (Tokens::place), so
 // that a step of the product over tokens belongs to one device. A token that is
 // not counted is a row of zeros wherever it is stored.
+//
+// A product's tiles are too few for the GPU where dim or a batch is small; its sum is then
+// split into units of about the same length, whose sums k_join_x and k_join_weight add.
 #include <cmath>
 #include <cstring>
 
@@ -25,10 +36,12 @@ using namespace scadles;
 
 namespace {
 
-constexpr uint64_t kPieceBytes = 256ull << 20;    // of G and its transpose
+constexpr uint64_t kPieceBytes = 256ull << 20;    // of G and its transpose, about
 constexpr uint32_t kLeastPiece = 2048;            // vocabulary entries of a piece, at least
 constexpr uint32_t kNone = ~0u;
-constexpr uint32_t kMost = 1u << 22;                // tokens and vocabulary entries: 32-bit offsets within a tile
+constexpr uint32_t kMost = 1u << 22;              // tokens and vocabulary entries: 32-bit offsets within a tile
+constexpr uint32_t kLeastSteps = 16;              // of a unit of a split sum, as long as its start and its store
+constexpr int kGBits = 13;                        // G in half floats is scaled by 2^13
 constexpr int kRowsBlock = 1024;
 constexpr uint32_t kRowSlices = kRowsBlock / 64;
 
@@ -61,7 +74,7 @@ __device__ inline uint32_t target_of(const Tokens& a, int64_t t)
   return v < a.vocab ? (uint32_t)v : kNone;
 }
 
-// An operand: rows of bfloat16 planes.
+// An operand: rows of planes of 16-bit floats.
 struct Matrix {
   const uint16_t* p;
   uint64_t plane;              // elements between planes
@@ -84,52 +97,121 @@ __device__ inline void tile_of(uint32_t id, uint32_t total, uint32_t rows, uint3
 
 // ---- operands ---------------------------------------------------------------------------------
 
-// Rows of X to rows of planes, zeros behind dim.
-template <class X>
-__global__ __launch_bounds__(kBlock) void k_planes(const X* x, uint64_t ld, uint64_t rows, uint32_t dim, uint32_t width, uint32_t planes,
-                                                   uint16_t* out, uint64_t plane)
+// The power of two that brings a largest magnitude, given by its bits, to 2^13 .. 2^14.
+__device__ inline int scale_of(uint32_t top) { return top ? 13 + 127 - (int)(top >> 23) : 0; }
+
+__device__ inline uint32_t finite_bits(float x)
 {
-  const uint32_t per = width / 8;
-  const uint64_t i = (uint64_t)blockIdx.x * kBlock + threadIdx.x;
-  if (i >= rows * per) return;
-  const uint64_t r = i / per;
-  const uint32_t at = (uint32_t)(i - r * per) * 8;
-  float v[8];
+  const uint32_t b = __float_as_uint(x) & 0x7FFFFFFFu;
+  return b < 0x7F800000u ? b : 0u;
+}
+
+__device__ inline uint16_t bits_of(__bf16 x) { return __builtin_bit_cast(uint16_t, x); }
+__device__ inline uint16_t bits_of(_Float16 x) { return __builtin_bit_cast(uint16_t, x); }
+
+// The first part of x, which becomes the rest; what is not finite has no rest.
+__device__ inline uint16_t half_part(float& x)
+{
+  const _Float16 h = (_Float16)x;
+  const float rest = x - (float)h;
+  x = rest - rest == 0.0f ? rest : 0.0f;
+  return bits_of(h);
+}
+
+// Rows of floats to rows of two planes, zeros behind dim, and the rows' powers of two: a wave
+// has a row.
+__global__ __launch_bounds__(kBlock) void k_planes(const float* x, uint64_t ld, uint32_t rows, uint32_t dim, uint32_t width, uint64_t stride,
+                                                   uint16_t* out, uint64_t plane, int32_t* scale)
+{
+  const uint32_t r = blockIdx.x * kWaves + threadIdx.x / 64, lane = threadIdx.x % 64;
+  if (r >= rows) return;
+  const float* row = x + r * ld;
+  uint32_t top = 0;
+  for (uint32_t at = lane * 4; at < dim; at += 256) {
+    const f4 v = load_f4(row + at, dim - at);
 #pragma unroll
-  for (uint32_t q = 0; q < 8; q += Piece<X>::N) {
-    const uint32_t k = at + q < dim ? dim - at - q : 0;
-    const auto f = unpack<X>(load_piece(x + r * ld + at + q, k));
-#pragma unroll
-    for (uint32_t e = 0; e < Piece<X>::N; ++e) v[q + e] = f[e];
+    for (int e = 0; e < 4; ++e) top = max(top, finite_bits(v[e]));
   }
-  for (uint32_t n = 0; n < planes; ++n) {
-    u4 w;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const uint32_t lo = next_plane(v[2 * q]), hi = next_plane(v[2 * q + 1]);
-      w[q] = lo | hi << 16;
+  for (int step = 1; step < 64; step *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, step, 64));
+  const int s = scale_of(top);
+  if (lane == 0) gptr(scale)[r] = s;
+  typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+  for (uint32_t at = lane * 4; at < width; at += 256) {
+    const f4 v = at < dim ? load_f4(row + at, dim - at) : f4{0, 0, 0, 0};
+    uint16_t h[2][4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float rest = ldexpf(v[e], s);
+      h[0][e] = half_part(rest);
+      h[1][e] = bits_of((_Float16)rest);
     }
-    *(GLOBAL u4*)gptr(out + n * plane + r * width + at) = w;
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+      *(GLOBAL u2*)gptr(out + n * plane + r * stride + at) = u2{h[n][0] | (uint32_t)h[n][1] << 16, h[n][2] | (uint32_t)h[n][3] << 16};
   }
 }
 
-// Rows of X transposed to planes [dim][width], 64 x 64 at a time. The rows are those of
-// a table (kTokens false: `rows` of them, then zeros) or the tokens in their places, zeros
-// where there is none or it is not counted.
+// Rows of bfloat16 to rows of whole steps, 16-byte aligned, zeros behind dim.
+__global__ __launch_bounds__(kBlock) void k_align(const uint16_t* x, uint64_t ld, uint64_t rows, uint32_t dim, uint32_t width, uint64_t stride,
+                                                  uint16_t* out)
+{
+  const uint32_t per = width / 8;
+  const uint64_t i = (uint64_t)blockIdx.x * kBlock + threadIdx.x, r = i / per;
+  const uint32_t at = (uint32_t)(i - r * per) * 8;
+  if (r >= rows) return;
+  *(GLOBAL u4*)gptr(out + r * stride + at) = load_piece(x + r * ld + at, at < dim ? dim - at : 0);
+}
+
+__global__ void k_clear(uint32_t* p, uint32_t n)
+{
+  const uint32_t i = blockIdx.x * blockDim.x + threadIdx.x;
+  if (i < n) gptr(p)[i] = 0;
+}
+
+// The row of x that is row r of the transposed operand: a table's own row, or the token in
+// a place if it is counted; -1 for zeros.
+template <bool kTokens>
+__device__ inline int64_t row_at(const Tokens& a, uint32_t r, uint32_t rows)
+{
+  if constexpr (!kTokens) return r < rows ? (int64_t)r : -1;
+  const int64_t t = token_at(a, r).t;
+  return t >= 0 && target_of(a, t) != kNone ? t : -1;
+}
+
+// The largest magnitude of every column, as bits, over 64 rows at a time (a maximum does
+// not depend on the order).
 template <class X, bool kTokens>
-__global__ __launch_bounds__(kBlock) void k_turn(Tokens a, const X* x, uint64_t ld, uint64_t rows, uint32_t dim, uint64_t width, uint32_t planes,
+__global__ __launch_bounds__(kBlock) void k_column_top(Tokens a, const X* x, uint64_t ld, uint32_t rows, uint32_t dim, uint32_t* top)
+{
+  constexpr uint32_t N = Piece<X>::N;
+  const uint32_t at = (blockIdx.y * 64 + threadIdx.x % 64) * N;
+  if (at >= dim) return;
+  uint32_t most[N] = {};
+#pragma unroll 4
+  for (uint32_t r = 0; r < 16; ++r) {
+    const int64_t from = row_at<kTokens>(a, blockIdx.x * 64 + threadIdx.x / 64 * 16 + r, rows);
+    if (from < 0) continue;
+    const auto f = unpack<X>(load_piece(x + from * ld + at, dim - at));
+#pragma unroll
+    for (uint32_t e = 0; e < N; ++e) most[e] = max(most[e], finite_bits(f[e]));
+  }
+#pragma unroll
+  for (uint32_t e = 0; e < N; ++e)
+    if (at + e < dim && most[e]) atomicMax(top + at + e, most[e]);
+}
+
+// Rows of X transposed to planes [dim][stride], 64 x 64 at a time; half floats are scaled by
+// the columns' largest magnitudes.
+template <class X, bool kTokens, class E, int kPlanes>
+__global__ __launch_bounds__(kBlock) void k_turn(Tokens a, const X* x, uint64_t ld, uint32_t rows, uint32_t dim, const uint32_t* top, uint64_t stride,
                                                  uint16_t* out, uint64_t plane)
 {
   __shared__ float tile[64][65];
-  const uint64_t r0 = (uint64_t)blockIdx.x * 64;
-  const uint32_t c0 = blockIdx.y * 64;
+  const uint32_t r0 = blockIdx.x * 64, c0 = blockIdx.y * 64;
   {
     const uint32_t r = threadIdx.x / 4, c = threadIdx.x % 4 * 16;
-    int64_t from = r0 + r < rows ? (int64_t)(r0 + r) : -1;
-    if constexpr (kTokens) {
-      from = token_at(a, (uint32_t)(r0 + r)).t;
-      if (from >= 0 && target_of(a, from) == kNone) from = -1;
-    }
+    const int64_t from = row_at<kTokens>(a, r0 + r, rows);
 #pragma unroll
     for (uint32_t q = 0; q < 16; q += Piece<X>::N) {
       const uint32_t at = c0 + c + q, k = from >= 0 && at < dim ? dim - at : 0;
@@ -141,19 +223,28 @@ __global__ __launch_bounds__(kBlock) void k_turn(Tokens a, const X* x, uint64_t 
   __syncthreads();
   const uint32_t c = threadIdx.x / 4, r = threadIdx.x % 4 * 16;
   if (c0 + c >= dim) return;
-  float v[16];
+  uint32_t w[kPlanes][8];
+  const int s = std::is_same<E, F16>::value ? scale_of(gptr(top)[c0 + c]) : 0;
 #pragma unroll
-  for (int e = 0; e < 16; ++e) v[e] = tile[r + e][c];
-  for (uint32_t n = 0; n < planes; ++n) {
-    u4 w[2];
+  for (int q = 0; q < 8; ++q) {
+    float lo = tile[r + 2 * q][c], hi = tile[r + 2 * q + 1][c];
+    if constexpr (std::is_same<E, F16>::value) {
+      lo = ldexpf(lo, s);
+      hi = ldexpf(hi, s);
 #pragma unroll
-    for (int q = 0; q < 8; ++q) {
-      const uint32_t lo = next_plane(v[2 * q]), hi = next_plane(v[2 * q + 1]);
-      w[q / 4][q % 4] = lo | hi << 16;
+      for (int n = 0; n < kPlanes; ++n) {
+        const uint32_t first = half_part(lo);
+        w[n][q] = first | (uint32_t)half_part(hi) << 16;
+      }
+    } else {
+      w[0][q] = bits_of((__bf16)lo) | (uint32_t)bits_of((__bf16)hi) << 16;
     }
-    GLOBAL u4* to = (GLOBAL u4*)gptr(out + n * plane + (uint64_t)(c0 + c) * width + r0 + r);
-    to[0] = w[0];
-    to[1] = w[1];
+  }
+#pragma unroll
+  for (int n = 0; n < kPlanes; ++n) {
+    GLOBAL u4* to = (GLOBAL u4*)gptr(out + n * plane + (uint64_t)(c0 + c) * stride + r0 + r);
+    to[0] = u4{w[n][0], w[n][1], w[n][2], w[n][3]};
+    to[1] = u4{w[n][4], w[n][5], w[n][6], w[n][7]};
   }
 }
 
@@ -166,6 +257,7 @@ struct Part {
 
 struct Logits {
   Matrix w, x;                 // vocabulary and tokens
+  const int32_t *w_scale, *x_scale;   // of half floats: the rows' powers of two
   uint32_t steps;
   Pairs pairs;
   uint32_t v0, v1;             // the vocabulary's piece
@@ -174,10 +266,9 @@ struct Logits {
   Part* part;                  // [tiles of the vocabulary][places]
   float* at_target;            // [places]
   // backward
-  const float *lse, *share, *d_loss;
-  uint16_t *g, *gt;            // [places][piece], [piece][places]
-  uint64_t plane;              // elements between their planes
-  uint32_t piece;
+  const float* lse;
+  uint16_t *g, *gt;            // [places][g_stride], [piece][gt_stride]
+  uint64_t g_stride, gt_stride, g_plane, gt_plane;
 };
 
 template <bool kExact>
@@ -187,138 +278,179 @@ __device__ inline float exp_of(float x)
   else return __builtin_amdgcn_exp2f(x * 1.44269504088896340736f);
 }
 
-// kExact: G in three planes, and exponentials to all of a float's bits.
-template <bool kBack, bool kExact>
+// E: of x and weight. kOut: planes of G, one of bfloat16 or two of half floats.
+template <bool kBack, class E, int kOut>
 __global__ __launch_bounds__(kProductBlock, 2) void k_logits(Tokens a, Logits q)
 {
+  constexpr bool kHalf = std::is_same<E, F16>::value, kExact = kHalf || kOut == 2;
   __shared__ __attribute__((aligned(128))) char lds[kProductLds];
-  uint32_t tm, tn;
-  tile_of(blockIdx.x, q.rows * q.columns, q.rows, q.columns, tm, tn);
-  const uint32_t m0 = q.v0 + tm * kEdge, n0 = tn * kEdge;
+  Pipe pipe(lds);
+  const uint32_t tiles = q.rows * q.columns;
+  uint32_t m0, n0, tm;
   Side sa, sb;
-  sa.base = q.w.p + (uint64_t)m0 * q.w.ld;
-  sa.plane = q.w.plane;
-  const int64_t first = token_at(a, n0).t;      // a tile begins with a device's tokens or within them
-  const int64_t t0 = first < 0 ? 0 : first;
-  sb.base = q.x.p + (uint64_t)t0 * q.x.ld;
-  sb.plane = q.x.plane;
+  auto enter = [&](uint32_t id) {
+    uint32_t tn;
+    tile_of(id, tiles, q.rows, q.columns, tm, tn);
+    m0 = q.v0 + tm * kEdge;
+    n0 = tn * kEdge;
+    sa.base = q.w.p + (uint64_t)m0 * q.w.ld;
+    sa.plane = q.w.plane;
+    const int64_t t0 = token_at(a, n0).t;       // there is one: a device's places begin with its tokens
+    sb.base = q.x.p + (uint64_t)t0 * q.x.ld;
+    sb.plane = q.x.plane;
 #pragma unroll
-  for (int it = 0; it < 4; ++it) {
-    const uint32_t r = lane_row(it), last = q.v1 - 1 - m0;
-    sa.off[it] = (uint32_t)((r < last ? r : last) * q.w.ld * 2) + lane_piece_a(it) * 16;
-    const int64_t t = token_at(a, n0 + r).t;
-    sb.off[it] = (uint32_t)((t < t0 ? 0 : t - t0) * q.x.ld * 2) + lane_piece_b(it) * 16;
-  }
-  f4 acc[8][4];
-  multiply(acc, sa, sb, q.steps, q.pairs, lds);
-
-  // the lane's tokens follow each other from a multiple of four on, so they are one device's
-  const uint32_t m = m0 + lane_m(), n = n0 + lane_n();
-  const Where w = token_at(a, n);
-  uint32_t target[4];
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const bool on = w.t >= 0 && (uint64_t)w.t + j < a.off[w.d + 1];
-    target[j] = on ? target_of(a, w.t + j) : kNone;
-  }
-  if (m0 + kEdge > q.v1) {                        // behind the vocabulary
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (m + 4 * i + e >= q.v1)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) acc[i][j][e] = -INFINITY;
-  }
-  if constexpr (!kBack) {
-    Part* both = reinterpret_cast<Part*>(lds);   // [2][256]: of the waves' two rows
+    for (int it = 0; it < 4; ++it) {
+      const uint32_t r = lane_row_a<8>(it), last = q.v1 - 1 - m0;
+      sa.off[it] = (uint32_t)((r < last ? r : last) * q.w.ld * 2) + lane_piece(it) * 16;
+      const int64_t t = token_at(a, n0 + lane_row_b(it)).t;
+      sb.off[it] = (uint32_t)((t < t0 ? 0 : t - t0) * q.x.ld * 2) + lane_piece(it) * 16;
+    }
+    pipe.begin(sa, sb, q.steps, q.pairs);
+  };
+  enter(blockIdx.x);
+  bool loaded = false;
+  for (uint32_t id = blockIdx.x; id < tiles; id += gridDim.x) {
+    f4 acc[8][4];
+    pipe.run<E>(acc, sa, sb, q.steps, q.pairs, loaded);
+    const uint32_t first = m0, n = n0 + lane_n(), tile = tm, tokens = n0;
+    if (id + gridDim.x < tiles) enter(id + gridDim.x);
+    // the lane's tokens follow each other from a multiple of four on, so they are one device's
+    const Where w = token_at(a, n);
+    uint32_t target[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      if (target[j] - m < 32) {                  // this lane has the target's logit
-        float z = 0.0f;
+      const bool on = w.t >= 0 && (uint64_t)w.t + j < a.off[w.d + 1];
+      target[j] = on ? target_of(a, w.t + j) : kNone;
+    }
+    if constexpr (kHalf) {
+      int s[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s[j] = target[j] != kNone ? gptr(q.x_scale)[w.t + j] : 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t v = first + lane_m<8>(i) + e;
+          const int t = gptr(q.w_scale)[v < q.v1 ? v : q.v1 - 1];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) acc[i][j][e] = ldexpf(acc[i][j][e], -(t + s[j]));
+        }
+    }
+    if (first + kEdge > q.v1) {                   // behind the vocabulary
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (first + lane_m<8>(i) + e >= q.v1)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[i][j][e] = -INFINITY;
+    }
+    // whether the lane has the target's logit, for a target of kNone never
+    const uint32_t m = first + lane_m<8>(0);
+    auto has = [&](uint32_t t) { return t - first < kEdge && (t - m) % 32 < 8 && (t - first) / 128 == (m - first) / 128; };
+    if constexpr (!kBack) {
+      Part* both = reinterpret_cast<Part*>(pipe.spare());   // [2][256]: of the waves' two rows
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (has(target[j])) {
+          float z = 0.0f;
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) z = target[j] == first + lane_m<8>(i) + e ? acc[i][j][e] : z;
+          gptr(q.at_target)[n + j] = z;
+        }
+        float top = acc[0][j][0], sum = 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; ++i)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) z = target[j] - m == 4 * i + e ? acc[i][j][e] : z;
-        gptr(q.at_target)[n + j] = z;
-      }
-      float top = acc[0][j][0], sum = 0.0f;
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) top = __builtin_fmaxf(top, acc[i][j][e]);
-      const float from = top == -INFINITY ? 0.0f : top;
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sum += exp_of<kExact>(acc[i][j][e] - from);
-#pragma unroll
-      for (int step = 16; step < 64; step *= 2) {
-        const float t = __shfl_xor(top, step, 64), s = __shfl_xor(sum, step, 64);
-        const float most = __builtin_fmaxf(top, t), base = most == -INFINITY ? 0.0f : most;
-        sum = sum * exp_of<kExact>(top - base) + s * exp_of<kExact>(t - base);
-        top = most;
-      }
-      if ((threadIdx.x & 48) == 0) both[(threadIdx.x >> 8) * kEdge + lane_n() + j] = {top, sum};
-    }
-    __syncthreads();
-    if (threadIdx.x < kEdge && n0 + threadIdx.x < a.places) {
-      const Part u = both[threadIdx.x], v = both[kEdge + threadIdx.x];
-      const float most = __builtin_fmaxf(u.top, v.top), base = most == -INFINITY ? 0.0f : most;
-      q.part[(uint64_t)tm * a.places + n0 + threadIdx.x] = {most, u.sum * exp_of<kExact>(u.top - base) + v.sum * exp_of<kExact>(v.top - base)};
-    }
-  } else {
-    if (n >= a.places) return;                   // places are a multiple of 64
-    const float c = w.t < 0 ? 0.0f : a.weight[w.d] * gptr(q.share)[w.d] * (q.d_loss ? gptr(q.d_loss)[0] : 1.0f);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const bool on = target[j] != kNone;
-      const float lse = on ? gptr(q.lse)[w.t + j] : 0.0f;
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[i][j][e] = exp_of<kExact>(acc[i][j][e] - lse);
-      if (target[j] - m < 32) {
+          for (int e = 0; e < 4; ++e) top = __builtin_fmaxf(top, acc[i][j][e]);
+        const float from = top == -INFINITY ? 0.0f : top;
 #pragma unroll
         for (int i = 0; i < 8; ++i)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) acc[i][j][e] -= target[j] - m == 4 * i + e ? 1.0f : 0.0f;
+          for (int e = 0; e < 4; ++e) sum += exp_of<kExact>(acc[i][j][e] - from);
+#pragma unroll
+        for (int step = 16; step < 64; step *= 2) {
+          const float t = __shfl_xor(top, step, 64), s = __shfl_xor(sum, step, 64);
+          const float most = __builtin_fmaxf(top, t), base = most == -INFINITY ? 0.0f : most;
+          sum = sum * exp_of<kExact>(top - base) + s * exp_of<kExact>(t - base);
+          top = most;
+        }
+        if ((threadIdx.x & 48) == 0) both[(threadIdx.x >> 8) * kEdge + lane_n() + j] = {top, sum};
       }
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");   // also for the next tile's loads, before the stores
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      if (threadIdx.x < kEdge && tokens + threadIdx.x < a.places) {
+        const Part u = both[threadIdx.x], v = both[kEdge + threadIdx.x];
+        const float most = __builtin_fmaxf(u.top, v.top), base = most == -INFINITY ? 0.0f : most;
+        q.part[(uint64_t)tile * a.places + tokens + threadIdx.x] = {most, u.sum * exp_of<kExact>(u.top - base) + v.sum * exp_of<kExact>(v.top - base)};
+      }
+    } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
+      for (int j = 0; j < 4; ++j) {
+        const bool on = target[j] != kNone;
+        const float lse = on ? gptr(q.lse)[w.t + j] : 0.0f;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[i][j][e] = on ? acc[i][j][e] * c : 0.0f;
-    }
-    // the rows of the piece have room for whole tiles
-    uint16_t* g = q.g + (uint64_t)n * q.piece + (m - q.v0);
-    uint16_t* gt = q.gt + (uint64_t)(m - q.v0) * a.places + n;
-    constexpr int planes = kExact ? 3 : 1;
+        for (int i = 0; i < 8; ++i)
 #pragma unroll
-    for (int i = 0; i < 8; i += 2)
+          for (int e = 0; e < 4; ++e) acc[i][j][e] = exp_of<kExact>(acc[i][j][e] - lse);
+        if (has(target[j])) {
 #pragma unroll
-      for (int pl = 0; pl < planes; ++pl) {
-        uint16_t h[4][8];
+          for (int i = 0; i < 8; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          u4 x;
+            for (int e = 0; e < 4; ++e) acc[i][j][e] -= target[j] == first + lane_m<8>(i) + e ? 1.0f : 0.0f;
+        }
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            float rest = acc[i + e / 4][j][e % 4];
-            h[j][e] = kExact ? next_plane(rest) : __builtin_bit_cast(uint16_t, (__bf16)rest);
-            acc[i + e / 4][j][e % 4] = rest;
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[i][j][e] = on ? acc[i][j][e] : 0.0f;
+      }
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // for the next tile's loads, before the stores
+      if (n < a.places) {                         // places are a multiple of 64
+        // the rows of the piece have room for whole tiles
+        uint16_t* g = q.g + (uint64_t)n * q.g_stride + (m - q.v0);
+        uint16_t* gt = q.gt + (uint64_t)(m - q.v0) * q.gt_stride + n;
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+          if constexpr (kOut == 2) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+              for (int e = 0; e < 8; ++e) acc[i + e / 4][j][e % 4] *= (float)(1 << kGBits);
           }
 #pragma unroll
-          for (int e = 0; e < 4; ++e) x[e] = h[j][2 * e] | (uint32_t)h[j][2 * e + 1] << 16;
-          *(GLOBAL u4*)gptr(g + pl * q.plane + j * (uint64_t)q.piece + 4 * i) = x;
-        }
+          for (int pl = 0; pl < kOut; ++pl) {
+            uint16_t h[4][8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          typedef uint32_t u2 __attribute__((ext_vector_type(2)));
-          const u2 x = {h[0][e] | (uint32_t)h[1][e] << 16, h[2][e] | (uint32_t)h[3][e] << 16};
-          *(GLOBAL u2*)gptr(gt + pl * q.plane + (4 * i + e) * (uint64_t)a.places) = x;
+            for (int j = 0; j < 4; ++j) {
+              u4 x;
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                float rest = acc[i + e / 4][j][e % 4];
+                h[j][e] = kOut == 2 ? half_part(rest) : bits_of((__bf16)rest);
+                acc[i + e / 4][j][e % 4] = rest;
+              }
+#pragma unroll
+              for (int e = 0; e < 4; ++e) x[e] = h[j][2 * e] | (uint32_t)h[j][2 * e + 1] << 16;
+              *(GLOBAL u4*)gptr(g + pl * q.g_plane + j * q.g_stride + 16 * i) = x;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+              const u2 x = {h[0][e] | (uint32_t)h[1][e] << 16, h[2][e] | (uint32_t)h[3][e] << 16};
+              *(GLOBAL u2*)gptr(gt + pl * q.gt_plane + (16 * i + e) * q.gt_stride) = x;
+            }
+            __builtin_amdgcn_sched_barrier(0);
+          }
         }
-        __builtin_amdgcn_sched_barrier(0);
       }
+    }
+    loaded = true;
   }
 }
 
@@ -399,81 +531,167 @@ __global__ __launch_bounds__(kRowsBlock) void k_loss_devices(Tokens a, const Gro
 struct Gradients {
   Matrix g, gt;                // [places][piece], [piece][places]
   Matrix wt, xt;               // [dim][vocabulary], [dim][places]
+  const uint32_t *w_top, *x_top;    // of half floats: the largest magnitudes of the columns
+  const float *share, *d_loss;
   uint32_t v0, v1, dim;
   uint32_t steps;              // of the piece
   uint32_t rows;               // tiles of dim
   uint32_t x_columns, w_columns;
   Pairs x_pairs, w_pairs;
-  float* sum;                  // [places][dim]: d_x of the pieces before
+  // The units of a split sum, of so many steps each. d_x: x_units of them for every tile.
+  // d_weight: units [w_first[d], w_first[d + 1]) for every tile of device d; where it has more
+  // than one, their sums go to w_sum.
+  uint32_t x_units, x_per, w_per;
+  uint32_t w_first[kMaxK + 1];
+  float* x_sum;                // [x_units][places][dim]: also of the pieces before
+  float* w_sum;                // [units][piece][dim]
+  uint64_t piece;
   void* d_x;
   uint64_t ld_d_x;
   void* d_weight[kMaxK];
   uint32_t first, last;        // whether the piece is
 };
 
-template <class X, class W>
+// What device d's sums are multiplied with.
+__device__ inline float factor_of(const Tokens& a, const Gradients& q, uint32_t d)
+{
+  return a.weight[d] * gptr(q.share)[d] * (q.d_loss ? gptr(q.d_loss)[0] : 1.0f);
+}
+
+// The power of two of column m's sums.
+template <class E>
+__device__ inline int column_scale(const uint32_t* top, uint32_t m)
+{
+  if constexpr (std::is_same<E, F16>::value) return scale_of(gptr(top)[m]) + kGBits;
+  return 0;
+}
+
+template <class E>
+__device__ inline f4 finished(f4 sum, const uint32_t* top, uint32_t m, uint32_t dim, float c)
+{
+#pragma unroll
+  for (uint32_t e = 0; e < 4; ++e) {
+    if constexpr (std::is_same<E, F16>::value) sum[e] = ldexpf(sum[e], -column_scale<E>(top, m + e < dim ? m + e : m));
+    sum[e] *= c;
+  }
+  return sum;
+}
+
+// E: of the operands; X, W: d_x's and d_weight's elements.
+template <class E, class X, class W>
 __global__ __launch_bounds__(kProductBlock, 2) void k_gradients(Tokens a, Gradients q)
 {
   __shared__ __attribute__((aligned(128))) char lds[kProductLds];
+  constexpr int kGroup = 4;
   const uint32_t x_tiles = q.rows * q.x_columns, w_tiles = q.rows * q.w_columns;
-  const bool of_x = blockIdx.x < x_tiles;
-  uint32_t tm, tn, d = 0, steps = q.steps;
+  const bool of_x = blockIdx.x < x_tiles * q.x_units;
+  uint32_t tm, tn, d = 0, unit, steps;
   uint64_t k0 = 0;
   if (of_x) {
-    tile_of(blockIdx.x, x_tiles, q.rows, q.x_columns, tm, tn);
+    unit = blockIdx.x / x_tiles;
+    tile_of(blockIdx.x - unit * x_tiles, x_tiles, q.rows, q.x_columns, tm, tn);
+    const uint32_t at = unit * q.x_per;
+    steps = at >= q.steps ? 0 : q.steps - at < q.x_per ? q.steps - at : q.x_per;   // a shorter last piece
+    k0 = (uint64_t)at * kStep;
   } else {
-    const uint32_t id = blockIdx.x - x_tiles;
-    d = id / w_tiles;
-    tile_of(id - d * w_tiles, w_tiles, q.rows, q.w_columns, tm, tn);
-    k0 = a.place[d];
-    steps = (a.place[d + 1] - a.place[d]) / kStep;
+    const uint32_t id = blockIdx.x - x_tiles * q.x_units;
+    unit = id / w_tiles;
+    tile_of(id - unit * w_tiles, w_tiles, q.rows, q.w_columns, tm, tn);
+    while (q.w_first[d + 1] <= unit) ++d;
+    const uint32_t all = (a.place[d + 1] - a.place[d]) / kStep, at = (unit - q.w_first[d]) * q.w_per;
+    steps = all - at < q.w_per ? all - at : q.w_per;
+    k0 = a.place[d] + (uint64_t)at * kStep;
   }
   const Matrix &A = of_x ? q.wt : q.xt, &B = of_x ? q.g : q.gt;
-  const uint32_t m0 = tm * kEdge, n0 = tn * kEdge, ends = of_x ? a.places : (q.v1 - q.v0);
+  const uint32_t m0 = tm * kEdge, n0 = tn * kEdge, ends = of_x ? a.places : q.v1 - q.v0;
   Side sa, sb;
-  sa.base = A.p + (uint64_t)m0 * A.ld + (of_x ? q.v0 : k0);
+  sa.base = A.p + (uint64_t)m0 * A.ld + (of_x ? q.v0 : 0) + k0;
   sa.plane = A.plane;
   sb.base = B.p + (uint64_t)n0 * B.ld + k0;
   sb.plane = B.plane;
 #pragma unroll
   for (int it = 0; it < 4; ++it) {
-    const uint32_t r = lane_row(it), last_m = q.dim - 1 - m0, last_n = ends - 1 - n0;
-    sa.off[it] = (uint32_t)((r < last_m ? r : last_m) * A.ld * 2) + lane_piece_a(it) * 16;
-    sb.off[it] = (uint32_t)((r < last_n ? r : last_n) * B.ld * 2) + lane_piece_b(it) * 16;
+    const uint32_t ra = lane_row_a<kGroup>(it), rb = lane_row_b(it), last_m = q.dim - 1 - m0, last_n = ends - 1 - n0;
+    sa.off[it] = (uint32_t)((ra < last_m ? ra : last_m) * A.ld * 2) + lane_piece(it) * 16;
+    sb.off[it] = (uint32_t)((rb < last_n ? rb : last_n) * B.ld * 2) + lane_piece(it) * 16;
   }
+  Pipe pipe(lds);
   f4 acc[8][4];
-  multiply(acc, sa, sb, steps, of_x ? q.x_pairs : q.w_pairs, lds);
-  const uint32_t m = m0 + lane_m(), n = n0 + lane_n();
-  if (m >= q.dim) return;
+  const Pairs pairs = of_x ? q.x_pairs : q.w_pairs;
+  pipe.begin(sa, sb, steps, pairs);
+  pipe.run<E>(acc, sa, sb, steps, pairs, false);
+  const uint32_t n = n0 + lane_n();
   if (of_x) {
     if (n >= a.places) return;
     const Where w = token_at(a, n);
+    const float c = q.x_units == 1 && q.last && w.t >= 0 ? factor_of(a, q, w.d) : 0.0f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       if (w.t < 0 || (uint64_t)w.t + j >= a.off[w.d + 1]) break;
       const bool on = target_of(a, w.t + j) != kNone;
-      float* sum = q.sum + (uint64_t)(n + j) * q.dim + m;
-      X* to = (X*)q.d_x + (uint64_t)(w.t + j) * q.ld_d_x + m;
+      float* sum = q.x_sum + ((uint64_t)unit * a.places + n + j) * q.dim;
+      X* to = (X*)q.d_x + (uint64_t)(w.t + j) * q.ld_d_x;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const uint32_t left = q.dim - m - 4 * i;
-        if (m + 4 * i >= q.dim) break;
+        const uint32_t m = m0 + lane_m<kGroup>(i), left = q.dim - m;
+        if (m >= q.dim) continue;
         f4 x = acc[i][j];
-        if (!q.first) x += load_f4(sum + 4 * i, left);
-        if (!q.last) store_f4(sum + 4 * i, x, left);
-        else store_f4(to + 4 * i, on ? x : f4{0, 0, 0, 0}, left);
+        if (!q.first) x += load_f4(sum + m, left);
+        if (q.x_units > 1 || !q.last) store_f4(sum + m, x, left);
+        else store_f4(to + m, on ? finished<E>(x, q.w_top, m, q.dim, c) : f4{0, 0, 0, 0}, left);
       }
     }
   } else {
+    const bool whole = q.w_first[d + 1] - q.w_first[d] == 1;
+    const float c = whole ? factor_of(a, q, d) : 0.0f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       if (n + j >= ends) break;
-      W* to = (W*)q.d_weight[d] + (uint64_t)(q.v0 + n + j) * q.dim + m;
+      W* to = (W*)q.d_weight[d] + (uint64_t)(q.v0 + n + j) * q.dim;
+      float* sum = q.w_sum + ((uint64_t)unit * q.piece + n + j) * q.dim;
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (m + 4 * i < q.dim) store_f4(to + 4 * i, acc[i][j], q.dim - m - 4 * i);
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t m = m0 + lane_m<kGroup>(i), left = q.dim - m;
+        if (m >= q.dim) continue;
+        if (whole) store_f4(to + m, finished<E>(acc[i][j], q.x_top, m, q.dim, c), left);
+        else store_f4(sum + m, acc[i][j], left);
+      }
     }
   }
+}
+
+// Adds the units of d_x: a lane has four elements of a token.
+template <class E, class X>
+__global__ __launch_bounds__(kBlock) void k_join_x(Tokens a, Gradients q, Share share)
+{
+  for_pieces(share, [&](uint32_t r, uint32_t g) {
+    const uint64_t p = (uint64_t)blockIdx.x * share.rows + r;
+    if (p >= a.places) return;
+    const Where w = token_at(a, (uint32_t)p);
+    if (w.t < 0) return;
+    const uint32_t m = g * 4, left = q.dim - m;
+    f4 x = {0, 0, 0, 0};
+    for (uint32_t u = 0; u < q.x_units; ++u) x += load_f4(q.x_sum + ((uint64_t)u * a.places + p) * q.dim + m, left);
+    const bool on = target_of(a, w.t) != kNone;
+    store_f4((X*)q.d_x + (uint64_t)w.t * q.ld_d_x + m, on ? finished<E>(x, q.w_top, m, q.dim, factor_of(a, q, w.d)) : f4{0, 0, 0, 0}, left);
+  });
+}
+
+// Adds the units of d_weight of the devices that have several.
+template <class E, class W>
+__global__ __launch_bounds__(kBlock) void k_join_weight(Tokens a, Gradients q, Share share)
+{
+  const uint32_t d = blockIdx.y, lo = q.w_first[d], hi = q.w_first[d + 1];
+  if (hi - lo == 1) return;
+  const float c = factor_of(a, q, d);
+  for_pieces(share, [&](uint32_t r, uint32_t g) {
+    const uint64_t v = (uint64_t)blockIdx.x * share.rows + r;
+    if (v >= q.v1 - q.v0) return;
+    const uint32_t m = g * 4, left = q.dim - m;
+    f4 x = {0, 0, 0, 0};
+    for (uint32_t u = lo; u < hi; ++u) x += load_f4(q.w_sum + ((uint64_t)u * q.piece + v) * q.dim + m, left);
+    store_f4((W*)q.d_weight[d] + (q.v0 + v) * q.dim + m, finished<E>(x, q.x_top, m, q.dim, c), left);
+  });
 }
 
 // ---- host -------------------------------------------------------------------------------------------
@@ -481,67 +699,8 @@ __global__ __launch_bounds__(kProductBlock, 2) void k_gradients(Tokens a, Gradie
 uint64_t size_of(int32_t type) { return type == SCADLES_BF16 ? 2 : 4; }
 uint64_t round_up(uint64_t x, uint64_t to) { return div_up(x, to) * to; }
 
-// The products of a matrix of one plane or three with one of `b` planes: all of one
-// plane's, or six of the nine of three parts each; the largest last.
-Pairs pairs_of(uint32_t a, uint32_t b)
-{
-  if (a == 3) return {6, 0x010210, 0x001012};
-  return b == 3 ? Pairs{3, 0, 0x012} : Pairs{1, 0, 0};
-}
-
-// What a call's arrays need in the workspace.
-struct Plan {
-  uint64_t x_width;            // elements of a row of x's and weight's planes
-  uint64_t vocab_width;        // of weight transposed
-  uint32_t planes;             // of x and weight
-  uint32_t g_planes;
-  uint32_t piece;              // vocabulary entries at a time
-  uint64_t places;
-  // addresses
-  uint16_t *x, *w, *xt, *wt, *g, *gt;
-  Part* part;
-  float *at_target, *sum;
-  Group* group;
-};
-
-uint64_t plan_call(const scadles_cross_entropy* ce, uint64_t tokens, uint64_t places, bool backward, bool own_x, bool own_w, char* ws, Plan& p)
-{
-  std::memset(&p, 0, sizeof(p));
-  uint64_t at = 0;
-  auto take = [&](uint64_t bytes) {
-    const uint64_t here = at;
-    at = round_up(at + bytes, 256);
-    return ws + here;
-  };
-  p.planes = ce->type == SCADLES_F32 ? 3 : 1;
-  p.g_planes = ce->type == SCADLES_F32 || ce->grad_type == SCADLES_F32 ? 3 : 1;
-  p.x_width = round_up(ce->dim, kStep);
-  p.vocab_width = round_up(ce->vocab, kStep);
-  p.places = places;
-  if (!own_x) p.x = (uint16_t*)take(tokens * p.x_width * 2 * p.planes);
-  if (!own_w) p.w = (uint16_t*)take(ce->vocab * p.x_width * 2 * p.planes);
-  if (!backward) {
-    p.part = (Part*)take(div_up(ce->vocab, kEdge) * places * sizeof(Part));
-    p.at_target = (float*)take(places * 4);
-    p.group = (Group*)take(places / 64 * sizeof(Group));
-    return at;
-  }
-  // G takes at most half of kPieceBytes, or kLeastPiece entries; the pieces are about equal
-  const uint64_t row = places * 2 * p.g_planes, all = round_up(ce->vocab, kEdge);
-  uint64_t piece = row ? kPieceBytes / 2 / row / kEdge * kEdge : all, bytes = kPieceBytes / 2;
-  if (piece < kLeastPiece) {
-    piece = kLeastPiece;
-    bytes = kLeastPiece * row;
-  }
-  if (bytes > all * row) bytes = all * row;
-  p.piece = (uint32_t)round_up(div_up(ce->vocab, div_up(ce->vocab, piece)), kEdge);
-  p.xt = (uint16_t*)take(ce->dim * places * 2 * p.planes);
-  p.wt = (uint16_t*)take(ce->dim * p.vocab_width * 2 * p.planes);
-  p.g = (uint16_t*)take(bytes);
-  p.gt = (uint16_t*)take(bytes);
-  if (piece < ce->vocab) p.sum = (float*)take(places * ce->dim * 4);
-  return at;
-}
+// Elements between rows of n, a multiple of 64: an odd number of 128-byte lines.
+uint64_t stride_of(uint64_t n) { return n / 64 % 2 ? n : n + 64; }
 
 scadles_status check_ce(const scadles_cross_entropy* ce)
 {
@@ -580,15 +739,105 @@ bool is_operand(const scadles_cross_entropy* ce, const void* p, uint64_t ld)
   return ce->type == SCADLES_BF16 && ce->dim % kStep == 0 && ld % 8 == 0 && is_aligned(p, 16) && ld <= 1u << 22;
 }
 
-template <class X>
-Matrix operand(const void* x, uint64_t ld, uint64_t rows, const scadles_cross_entropy* ce, const Plan& p, uint16_t* to, hipStream_t st)
+// How a call is done, and its arrays in the workspace.
+struct Plan {
+  bool half;                   // x and weight in half floats
+  bool half_g;                 // G, and the transposed ones
+  uint32_t planes;             // of x and weight: 2 of floats, else 1
+  uint64_t x_width, x_stride;  // of their rows
+  uint64_t vocab_width, wt_stride, xt_stride;
+  uint64_t piece, g_stride;    // vocabulary entries at a time
+  uint32_t x_units, x_per, w_per, w_units;
+  uint16_t *x, *w, *xt, *wt, *g, *gt;
+  int32_t *x_scale, *w_scale;
+  uint32_t *x_top, *w_top;
+  Part* part;
+  float *at_target, *x_sum, *w_sum;
+  Group* group;
+  uint64_t bytes;
+};
+
+// Vocabulary entries of a piece: as many rows of tiles as G's share of kPieceBytes holds, or a
+// few less where the tiles then come in whole rounds of the compute units.
+uint64_t piece_of(uint64_t vocab, uint64_t places, uint32_t planes)
 {
-  if (!to) return {(const uint16_t*)x, 0, ld};
-  const uint64_t plane = rows * p.x_width;
-  if (rows)
-    k_planes<X><<<(uint32_t)div_up(rows * (p.x_width / 8), kBlock), kBlock, 0, st>>>((const X*)x, ld, rows, ce->dim, (uint32_t)p.x_width, p.planes,
-                                                                                    to, plane);
-  return {to, plane, p.x_width};
+  const uint64_t row = places * 2 * planes * kEdge, columns = div_up(places, kEdge), all = div_up(vocab, kEdge);
+  uint64_t most = row ? kPieceBytes / 2 / row : all;
+  if (most < kLeastPiece / kEdge) most = kLeastPiece / kEdge;
+  if (most >= all) return all * kEdge;
+  uint64_t best = most;
+  double full = 0.0;
+  for (uint64_t r = most; 2 * r >= most && r; --r) {
+    const uint64_t tiles = r * columns;
+    const double f = (double)tiles / (double)round_up(tiles, kComputeUnits);
+    if (f > full * 1.02) {
+      full = f;
+      best = r;
+    }
+  }
+  return best * kEdge;
+}
+
+void plan_call(const scadles_cross_entropy* ce, const Tokens& a, bool backward, bool own_x, bool own_w, char* ws, Plan& p)
+{
+  std::memset(&p, 0, sizeof(p));
+  uint64_t at = 0;
+  auto take = [&](uint64_t bytes) {
+    const uint64_t here = at;
+    at = round_up(at + bytes, 256);
+    return ws + here;
+  };
+  const uint64_t tokens = a.off[a.K], places = a.places, V = ce->vocab;
+  p.half = ce->type == SCADLES_F32;
+  p.half_g = p.half || ce->grad_type == SCADLES_F32;
+  p.planes = p.half ? 2 : 1;
+  p.x_width = round_up(ce->dim, kStep);
+  p.x_stride = stride_of(p.x_width);
+  if (!own_x) p.x = (uint16_t*)take(tokens * p.x_stride * 2 * p.planes);
+  if (!own_w) p.w = (uint16_t*)take(V * p.x_stride * 2 * p.planes);
+  if (p.half) {
+    p.x_scale = (int32_t*)take(tokens * 4);
+    p.w_scale = (int32_t*)take(V * 4);
+  }
+  if (!backward) {
+    p.part = (Part*)take(div_up(V, kEdge) * places * sizeof(Part));
+    p.at_target = (float*)take(places * 4);
+    p.group = (Group*)take(places / 64 * sizeof(Group));
+    p.bytes = at;
+    return;
+  }
+  const uint32_t g_planes = p.half_g ? 2 : 1;
+  p.vocab_width = round_up(V, kStep);
+  p.wt_stride = stride_of(p.vocab_width);
+  p.xt_stride = stride_of(places);
+  p.piece = piece_of(V, places, g_planes);
+  p.g_stride = stride_of(p.piece);
+  p.xt = (uint16_t*)take(ce->dim * p.xt_stride * 2 * p.planes);
+  p.wt = (uint16_t*)take(ce->dim * p.wt_stride * 2 * p.planes);
+  p.g = (uint16_t*)take(places * p.g_stride * 2 * g_planes);
+  p.gt = (uint16_t*)take(p.piece * p.xt_stride * 2 * g_planes);
+  p.w_top = (uint32_t*)take(ce->dim * 4 * 2);
+  p.x_top = p.w_top + ce->dim;
+  // units: each about the 256th part of a piece's steps
+  const uint32_t x_pairs = p.planes == 2 ? 3 : 1, w_pairs = ce->grad_type == SCADLES_BF16 ? 1 : p.planes == 2 ? 3 : 2;
+  const uint64_t rows = div_up(ce->dim, kEdge), steps = (p.piece < V ? p.piece : p.vocab_width) / kStep;
+  const uint64_t x_all = rows * div_up(places, kEdge) * steps * x_pairs, w_tiles = rows * div_up(p.piece, kEdge);
+  const uint64_t w_all = w_tiles * (places / kStep) * w_pairs;
+  uint64_t per = div_up(x_all + w_all, kComputeUnits);
+  if (per < kLeastSteps) per = kLeastSteps;
+  p.x_units = (uint32_t)div_up(steps * x_pairs, per);
+  p.x_per = (uint32_t)div_up(steps, p.x_units);
+  p.x_units = (uint32_t)div_up(steps, p.x_per);
+  p.w_per = (uint32_t)div_up(per, w_pairs);
+  bool several = false;
+  for (uint32_t d = 0; d < a.K; ++d) {
+    const uint64_t n = div_up((a.place[d + 1] - a.place[d]) / kStep, p.w_per);
+    p.w_units += (uint32_t)(n ? n : 1);
+    several |= n > 1;
+  }
+  if (p.piece < V || p.x_units > 1) p.x_sum = (float*)take(p.x_units * places * ce->dim * 4);
+  if (several) p.w_sum = (float*)take(p.w_units * p.piece * ce->dim * 4);
+  p.bytes = at;
 }
 
 scadles_status check_arrays(const scadles_cross_entropy* ce, const scadles_batch* b, const float* weights, const void* x, uint64_t ld_x,
@@ -623,84 +872,149 @@ struct Range {
   uint64_t bytes;
 };
 
-template <class X>
+// An operand of the logits: where it is, or in planes.
+Matrix operand(const scadles_cross_entropy* ce, const Plan& p, const void* x, uint64_t ld, uint64_t rows, uint16_t* to, int32_t* scale, hipStream_t st)
+{
+  if (!to) return {(const uint16_t*)x, 0, ld};
+  const uint64_t plane = rows * p.x_stride;
+  if (rows) {
+    if (p.half)
+      k_planes<<<(uint32_t)div_up(rows, kWaves), kBlock, 0, st>>>((const float*)x, ld, (uint32_t)rows, ce->dim, (uint32_t)p.x_width, p.x_stride, to,
+                                                                  plane, scale);
+    else
+      k_align<<<(uint32_t)div_up(rows * (p.x_width / 8), kBlock), kBlock, 0, st>>>((const uint16_t*)x, ld, rows, ce->dim, (uint32_t)p.x_width,
+                                                                                  p.x_stride, to);
+  }
+  return {to, plane, p.x_stride};
+}
+
 void prepare(Logits& q, const scadles_cross_entropy* ce, const Tokens& a, const Plan& p, const void* x, uint64_t ld_x, const void* weight,
              uint64_t ld_w, hipStream_t st)
 {
   std::memset(&q, 0, sizeof(q));
-  q.x = operand<X>(x, ld_x, a.off[a.K], ce, p, p.x, st);
-  q.w = operand<X>(weight, ld_w, ce->vocab, ce, p, p.w, st);
+  q.x = operand(ce, p, x, ld_x, a.off[a.K], p.x, p.x_scale, st);
+  q.w = operand(ce, p, weight, ld_w, ce->vocab, p.w, p.w_scale, st);
+  q.x_scale = p.x_scale;
+  q.w_scale = p.w_scale;
   q.steps = (uint32_t)(p.x_width / kStep);
-  q.pairs = pairs_of(p.planes, p.planes);
+  q.pairs = p.half ? Pairs{3, 0x010, 0x001} : Pairs{1, 0, 0};
   q.columns = (uint32_t)div_up(a.places, kEdge);
 }
 
-template <class X>
+uint32_t blocks_for(const Logits& q)
+{
+  const uint32_t tiles = q.rows * q.columns;
+  return tiles < kComputeUnits ? tiles : kComputeUnits;
+}
+
 hipError_t forward(const scadles_cross_entropy* ce, const Tokens& a, const Plan& p, const void* x, uint64_t ld_x, const void* weight, uint64_t ld_w,
                    const scadles_cross_entropy_out* out, hipStream_t st)
 {
   if (a.places) {
     Logits q;
-    prepare<X>(q, ce, a, p, x, ld_x, weight, ld_w, st);
+    prepare(q, ce, a, p, x, ld_x, weight, ld_w, st);
     q.v1 = a.vocab;
     q.rows = (uint32_t)div_up(a.vocab, kEdge);
     q.part = p.part;
     q.at_target = p.at_target;
-    k_logits<false, sizeof(X) == 4><<<q.rows * q.columns, kProductBlock, 0, st>>>(a, q);
+    if (p.half) k_logits<false, F16, 1><<<blocks_for(q), kProductBlock, 0, st>>>(a, q);
+    else k_logits<false, BF16, 1><<<blocks_for(q), kProductBlock, 0, st>>>(a, q);
     k_loss_rows<<<a.places / 64, kRowsBlock, 0, st>>>(a, p.part, q.rows, p.at_target, out->nll, out->lse, p.group);
   }
   k_loss_devices<<<1, kRowsBlock, 0, st>>>(a, p.group, out->device_loss, out->share, out->loss);
   return hipGetLastError();
 }
 
-template <class X, class W>
+// The operands of the gradients' products, transposed.
+template <class X, class E, int kPlanes>
+void turn(const scadles_cross_entropy* ce, const Tokens& a, const Plan& p, const void* x, uint64_t ld_x, const void* weight, uint64_t ld_w,
+          bool tokens, hipStream_t st)
+{
+  const uint32_t dim = ce->dim, down = (uint32_t)div_up(dim, 64), V = (uint32_t)ce->vocab, T = (uint32_t)a.off[a.K];
+  if constexpr (std::is_same<E, F16>::value) {
+    k_clear<<<(uint32_t)div_up(2 * dim, kBlock), kBlock, 0, st>>>(p.w_top, 2 * dim);
+    const uint32_t across = (uint32_t)div_up(dim, 64 * Piece<X>::N);
+    k_column_top<X, false><<<dim3((uint32_t)div_up(V, 64), across), kBlock, 0, st>>>(a, (const X*)weight, ld_w, V, dim, p.w_top);
+    if (tokens) k_column_top<X, true><<<dim3(a.places / 64, across), kBlock, 0, st>>>(a, (const X*)x, ld_x, T, dim, p.x_top);
+  }
+  k_turn<X, false, E, kPlanes><<<dim3((uint32_t)(p.vocab_width / 64), down), kBlock, 0, st>>>(a, (const X*)weight, ld_w, V, dim, p.w_top, p.wt_stride,
+                                                                                             p.wt, dim * p.wt_stride);
+  if (tokens)
+    k_turn<X, true, E, kPlanes><<<dim3(a.places / 64, down), kBlock, 0, st>>>(a, (const X*)x, ld_x, T, dim, p.x_top, p.xt_stride, p.xt,
+                                                                             dim * p.xt_stride);
+}
+
+template <class E, class X, class W>
 hipError_t backward(const scadles_cross_entropy* ce, const Tokens& a, const Plan& p, const void* x, uint64_t ld_x, const void* weight, uint64_t ld_w,
                     const scadles_cross_entropy_out* out, const float* d_loss, void* d_x, uint64_t ld_d_x, void* const* d_weight, hipStream_t st)
 {
+  constexpr int kPlanes = sizeof(X) == 4 ? 2 : 1, kOut = std::is_same<E, F16>::value ? 2 : 1;
+  typedef typename std::conditional<sizeof(X) == 4, F16, BF16>::type In;
+  const uint32_t dim = ce->dim;
   Logits q;
-  prepare<X>(q, ce, a, p, x, ld_x, weight, ld_w, st);
+  std::memset(&q, 0, sizeof(q));
+  if (a.places) {
+    prepare(q, ce, a, p, x, ld_x, weight, ld_w, st);
+    turn<X, E, kPlanes>(ce, a, p, x, ld_x, weight, ld_w, d_weight != nullptr, st);
+  }
   q.lse = out->lse;
-  q.share = out->share;
-  q.d_loss = d_loss;
   q.g = p.g;
   q.gt = p.gt;
-  q.plane = p.places * p.piece;
-  q.piece = p.piece;
+  q.g_stride = p.g_stride;
+  q.gt_stride = p.xt_stride;
+  q.g_plane = a.places * p.g_stride;
+  q.gt_plane = p.piece * p.xt_stride;
   Gradients r;
   std::memset(&r, 0, sizeof(r));
-  const uint32_t dim = ce->dim, down = (uint32_t)div_up(dim, 64);
-  if (a.places) {
-    k_turn<X, false><<<dim3((uint32_t)(p.vocab_width / 64), down), kBlock, 0, st>>>(a, (const X*)weight, ld_w, ce->vocab, dim, p.vocab_width, p.planes,
-                                                                                   p.wt, dim * p.vocab_width);
-    if (d_weight)
-      k_turn<X, true><<<dim3((uint32_t)(p.places / 64), down), kBlock, 0, st>>>(a, (const X*)x, ld_x, a.off[a.K], dim, p.places, p.planes, p.xt,
-                                                                               dim * p.places);
-  }
-  r.g = {p.g, q.plane, p.piece};
-  r.gt = {p.gt, q.plane, p.places};
-  r.wt = {p.wt, dim * p.vocab_width, p.vocab_width};
-  r.xt = {p.xt, dim * p.places, p.places};
+  r.g = {p.g, q.g_plane, p.g_stride};
+  r.gt = {p.gt, q.gt_plane, p.xt_stride};
+  r.wt = {p.wt, dim * p.wt_stride, p.wt_stride};
+  r.xt = {p.xt, dim * p.xt_stride, p.xt_stride};
+  r.w_top = p.w_top;
+  r.x_top = p.x_top;
+  r.share = out->share;
+  r.d_loss = d_loss;
   r.dim = dim;
   r.rows = (uint32_t)div_up(dim, kEdge);
   r.x_columns = q.columns;
-  r.x_pairs = pairs_of(p.planes, sizeof(X) == 4 ? 3 : 1);
-  r.w_pairs = pairs_of(p.planes, sizeof(X) == 4 || sizeof(W) == 4 ? 3 : 1);
-  r.sum = p.sum;
+  // A is weight or x, B is G: of two parts each the largest products, the greatest last
+  r.x_pairs = kPlanes == 2 ? Pairs{3, 0x010, 0x001} : Pairs{1, 0, 0};
+  r.w_pairs = sizeof(W) == 2 ? Pairs{1, 0, 0} : kPlanes == 2 ? Pairs{3, 0x010, 0x001} : Pairs{2, 0, 0x01};
+  r.x_units = p.x_units;
+  r.x_per = p.x_per;
+  r.w_per = p.w_per;
+  for (uint32_t d = 0; d < a.K; ++d) {
+    const uint64_t n = div_up((a.place[d + 1] - a.place[d]) / kStep, p.w_per);
+    r.w_first[d + 1] = r.w_first[d] + (uint32_t)(n ? n : 1);
+    if (d_weight) r.d_weight[d] = d_weight[d];
+  }
+  r.x_sum = p.x_sum;
+  r.w_sum = p.w_sum;
+  r.piece = p.piece;
   r.d_x = d_x;
   r.ld_d_x = ld_d_x;
-  for (uint32_t d = 0; d < a.K && d_weight; ++d) r.d_weight[d] = d_weight[d];
-  for (uint32_t v0 = 0; v0 < a.vocab; v0 += p.piece) {
-    const uint32_t v1 = a.vocab - v0 < p.piece ? a.vocab : v0 + p.piece;
-    q.v0 = r.v0 = v0;
-    q.v1 = r.v1 = v1;
+  const uint32_t quads = (uint32_t)div_up(dim, 4);
+  for (uint64_t v0 = 0; v0 < a.vocab; v0 += p.piece) {
+    const uint64_t v1 = a.vocab - v0 < p.piece ? a.vocab : v0 + p.piece;
+    q.v0 = r.v0 = (uint32_t)v0;
+    q.v1 = r.v1 = (uint32_t)v1;
     q.rows = (uint32_t)div_up(v1 - v0, kEdge);
     r.steps = (uint32_t)div_up(v1 - v0, kStep);
+    // the last piece may be shorter: as many units as the others', some of them without steps
     r.w_columns = d_weight ? q.rows : 0;
     r.first = v0 == 0;
     r.last = v1 == a.vocab;
-    if (a.places) k_logits<true, sizeof(X) == 4 || sizeof(W) == 4><<<q.rows * q.columns, kProductBlock, 0, st>>>(a, q);
-    const uint64_t tiles = (uint64_t)r.rows * r.x_columns + (uint64_t)r.rows * r.w_columns * a.K;
-    if (tiles) k_gradients<X, W><<<(uint32_t)tiles, kProductBlock, 0, st>>>(a, r);
+    if (a.places) k_logits<true, In, kOut><<<blocks_for(q), kProductBlock, 0, st>>>(a, q);
+    const uint64_t units = (uint64_t)r.rows * r.x_columns * r.x_units + (uint64_t)r.rows * r.w_columns * r.w_first[a.K];
+    if (units) k_gradients<E, X, W><<<(uint32_t)units, kProductBlock, 0, st>>>(a, r);
+    if (d_weight && p.w_sum) {
+      const Share share = share_rows(v1 - v0, quads);
+      k_join_weight<E, W><<<dim3((uint32_t)div_up(v1 - v0, share.rows), a.K), kBlock, 0, st>>>(a, r, share);
+    }
+  }
+  if (r.x_units > 1 && a.places) {
+    const Share share = share_rows(a.places, quads);
+    k_join_x<E, X><<<(uint32_t)div_up(a.places, share.rows), kBlock, 0, st>>>(a, r, share);
   }
   return hipGetLastError();
 }
@@ -709,13 +1023,14 @@ hipError_t backward(const scadles_cross_entropy* ce, const Tokens& a, const Plan
 
 extern "C" {
 
-size_t scadles_cross_entropy_workspace_bytes(const scadles_cross_entropy* ce, uint64_t tokens, uint32_t devices, int backward)
+size_t scadles_cross_entropy_workspace_bytes(const scadles_cross_entropy* ce, const scadles_batch* batch, int backward)
 {
-  if (check_ce(ce) || tokens > kMost || !devices || devices > kMaxK) return 0;
+  if (check_ce(ce) || check_batch(batch) || batch->tokens > kMost) return 0;
+  Tokens a;
   Plan p;
-  const uint64_t places = round_up(tokens, 64) + (uint64_t)(devices - 1) * 64;
-  const uint64_t n = plan_call(ce, tokens, places, backward != 0, false, false, nullptr, p);
-  return (size_t)(n < 256 ? 256 : n);
+  make_tokens(ce, batch, nullptr, nullptr, a);
+  plan_call(ce, a, backward != 0, false, false, nullptr, p);
+  return (size_t)(p.bytes < 256 ? 256 : p.bytes);
 }
 
 scadles_status scadles_cross_entropy_forward(const scadles_cross_entropy* ce, const scadles_batch* batch, const float* weights, const void* x,
@@ -733,7 +1048,8 @@ scadles_status scadles_cross_entropy_forward(const scadles_cross_entropy* ce, co
   make_tokens(ce, batch, weights, target, a);
   Plan p;
   const uint64_t T = batch->tokens, K = batch->devices, es = size_of(ce->type);
-  const uint64_t need = plan_call(ce, T, a.places, false, is_operand(ce, x, ld_x), is_operand(ce, weight, ld_weight), (char*)ws, p);
+  plan_call(ce, a, false, is_operand(ce, x, ld_x), is_operand(ce, weight, ld_weight), (char*)ws, p);
+  const uint64_t need = p.bytes;
   if (scadles_status st = check_space(ws, ws_bytes, need)) return st;
   const Range at[9] = {{out->nll, T * 4}, {out->lse, T * 4}, {out->device_loss, K * 4}, {out->share, K * 4}, {out->loss, 4}, {ws, need},
                        {x, rows_bytes(T, ce->dim, ld_x, es)}, {weight, rows_bytes(ce->vocab, ce->dim, ld_weight, es)}, {target, T * ce->target_bytes}};
@@ -741,9 +1057,7 @@ scadles_status scadles_cross_entropy_forward(const scadles_cross_entropy* ce, co
     for (int j = i + 1; j < 9; ++j)
       if (bytes_overlap(at[i].p, at[i].bytes, at[j].p, at[j].bytes)) return fail(SCADLES_EINVAL, "an output overlaps an input, the workspace or another");
   hipStream_t st = static_cast<hipStream_t>(stream);
-  return launch_status(ce->type == SCADLES_BF16 ? forward<uint16_t>(ce, a, p, x, ld_x, weight, ld_weight, out, st)
-                                                : forward<float>(ce, a, p, x, ld_x, weight, ld_weight, out, st),
-                       "cross entropy forward");
+  return launch_status(forward(ce, a, p, x, ld_x, weight, ld_weight, out, st), "cross entropy forward");
 }
 
 scadles_status scadles_cross_entropy_backward(const scadles_cross_entropy* ce, const scadles_batch* batch, const float* weights, const void* x,
@@ -761,7 +1075,8 @@ scadles_status scadles_cross_entropy_backward(const scadles_cross_entropy* ce, c
   Tokens a;
   make_tokens(ce, batch, weights, target, a);
   Plan p;
-  const uint64_t need = plan_call(ce, T, a.places, true, is_operand(ce, x, ld_x), is_operand(ce, weight, ld_weight), (char*)ws, p);
+  plan_call(ce, a, true, is_operand(ce, x, ld_x), is_operand(ce, weight, ld_weight), (char*)ws, p);
+  const uint64_t need = p.bytes;
   if (scadles_status st = check_space(ws, ws_bytes, need)) return st;
   const Range in[6] = {{x, rows_bytes(T, ce->dim, ld_x, es)}, {weight, rows_bytes(ce->vocab, ce->dim, ld_weight, es)}, {target, T * ce->target_bytes},
                        {out->lse, T * 4}, {out->share, K * 4}, {d_loss, 4}};
@@ -784,8 +1099,8 @@ scadles_status scadles_cross_entropy_backward(const scadles_cross_entropy* ce, c
   hipStream_t st = static_cast<hipStream_t>(stream);
   const bool b = ce->type == SCADLES_BF16, gb = ce->grad_type == SCADLES_BF16;
   auto go = [&](auto f) { return f(ce, a, p, x, ld_x, weight, ld_weight, out, d_loss, d_x, ld_d_x, d_weight, st); };
-  return launch_status(b ? (gb ? go(backward<uint16_t, uint16_t>) : go(backward<uint16_t, float>))
-                         : (gb ? go(backward<float, uint16_t>) : go(backward<float, float>)),
+  return launch_status(b ? (gb ? go(backward<BF16, uint16_t, uint16_t>) : go(backward<F16, uint16_t, float>))
+                         : (gb ? go(backward<F16, float, uint16_t>) : go(backward<F16, float, float>)),
                        "cross entropy backward");
 }
 

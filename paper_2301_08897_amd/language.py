@@ -72,7 +72,7 @@ _layer_norm_backward = _sc._sig("scadles_layer_norm_backward", ctypes.c_int, cty
                                 ctypes.POINTER(Batch), _vp, _u64, _vp, _vp, _vp, _vp, _u64, _vp, _u64,
                                 ctypes.POINTER(_vp), ctypes.POINTER(_vp), _vp, ctypes.c_size_t, _vp)
 _cross_entropy_ws_bytes = _sc._sig("scadles_cross_entropy_workspace_bytes", ctypes.c_size_t,
-                                   ctypes.POINTER(CrossEntropyShape), _u64, _u32, ctypes.c_int)
+                                   ctypes.POINTER(CrossEntropyShape), ctypes.POINTER(Batch), ctypes.c_int)
 _cross_entropy_forward = _sc._sig("scadles_cross_entropy_forward", ctypes.c_int, ctypes.POINTER(CrossEntropyShape),
                                   ctypes.POINTER(Batch), ctypes.POINTER(ctypes.c_float), _vp, _u64, _vp, _u64, _vp,
                                   ctypes.POINTER(CrossEntropyOut), _vp, ctypes.c_size_t, _vp)
@@ -462,7 +462,7 @@ class LinearCrossEntropy:
         buf = _new((2 * T + 2 * K + 1,), f32, x, stream)
         q = buf.data_ptr()
         at = CrossEntropyOut(q, q + 4 * T, q + 8 * T, q + 8 * T + 4 * K, q + 8 * T + 8 * K)
-        ws = _scratch(_cross_entropy_ws_bytes(shape, T, K, 0), x, stream)
+        ws = _scratch(_cross_entropy_ws_bytes(shape, batch, 0), x, stream)
         _run(_cross_entropy_forward, shape, batch, self._weights(weights), *args, at, ws.data_ptr(), ws.numel(), like=x, stream=stream)
         return CrossEntropyOutputs(buf[:T], buf[T:2 * T], buf[2 * T:2 * T + K], buf[2 * T + K:2 * T + 2 * K], buf[2 * T + 2 * K:])
 
@@ -487,7 +487,7 @@ class LinearCrossEntropy:
         lse, share = _whole(out.lse, "lse", T, f32, like=x), _whole(out.share, "share", self.devices, f32, like=x)
         d = None if d_loss is None else _whole(d_loss, "d_loss", 1, f32, like=x)
         dx, q, ld_dx = _output(d_x, "d_x", T, self.dim, x.dtype, x, stream)
-        ws = _scratch(_cross_entropy_ws_bytes(shape, T, self.devices, 1), x, stream)
+        ws = _scratch(_cross_entropy_ws_bytes(shape, batch, 1), x, stream)
         _run(_cross_entropy_backward, shape, batch, None if weights is None else self._weights(weights), *args,
              CrossEntropyOut(None, lse, None, share, None), d, q, ld_dx, where, ws.data_ptr(), ws.numel(), like=x, stream=stream)
         _wrote(d_x, *each)

@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 
 from _gpu_common import torch_dev
-from _language import FILL, HALF, U, around, bounds, dtype, host, near, space, tensor
+from _language import FILL, U, around, bounds, dtype, host, near, space, tensor
 from oracle import language as ol
 
 pytestmark = pytest.mark.gpu
@@ -44,10 +44,13 @@ def run(sc, T, V, dim, K, kind, grad, *, pad=0, padding=True, wide=True, forward
     hw = host(w)
     z, nll, lse, each, share, loss = ol.cross_entropy(hx, hw, target, off, weights.astype(np.float64))
     # a product's terms go through one addition per instruction of 32 and those within it; the matrix cores'
-    # additions may be off by a step, not half of one. Parts of floats that are left out are below 2^-24
-    parts = 6 if kind == "f32" else 1
+    # additions may be off by a step, not half of one. Floats are two half floats, each rounding 2^-11: 2^-22 of
+    # them is left out, and the product of the second parts; below 2^-14 a half float's steps are 2^-24, where the
+    # largest of the row is 2^13 at least: half a step is 2^-38 of that
+    parts, floor = (3, 2.0**-38) if kind == "f32" else (1, 0.0)
     size = np.abs(hx) @ np.abs(hw).T
-    e_z = size * U * (2 * (parts * (dim // 32 + 1) + 40) + 2)
+    e_z = size * (U * (2 * (parts * (dim // 32 + 1) + 40) + 2) + (3 * 2.0**-22 if parts == 3 else 0.0))
+    e_z += floor * (np.abs(hx).max(axis=1)[:, None] * np.abs(hw).sum(axis=1) + np.abs(hx).sum(axis=1)[:, None] * np.abs(hw).max(axis=1))
     span = float(np.ptp(z[on])) if on.any() else 0.0
     # exponentials: their argument and 1.44 times it are rounded, and the result; 32 of a lane, the lanes, the tiles
     e_sum = U * (4 * span + 8 + 40 + V // 256 / 16 + 32 * 4)
@@ -70,17 +73,24 @@ def run(sc, T, V, dim, K, kind, grad, *, pad=0, padding=True, wide=True, forward
     # what is below 2^-126, the least normal float and bfloat16, may become zero: the exponential (times a factor
     # below 1), its product with the factor, and each of the three parts; so a term is off by up to 5 * 2^-126 |x|
     e_g += 5 * 2.0**-126 * on[:, None]
-    rounded = HALF["bf16"] if (kind, grad) == ("bf16", "bf16") else U
-    mine = HALF["bf16"] if kind == "bf16" else U                  # d_x goes by the first plane alone if it is bfloat16
-    pieces = 16
-    steps = lambda n: 2 * U * (parts * (n // 32 + 2) * (3 if parts == 1 else 1) + 40 + pieces)  # noqa: E731
-    near(dx, want_dx, (e_g + np.abs(g) * mine) @ np.abs(hw) + (np.abs(g) @ np.abs(hw)) * steps(V), kind, "d_x")
+    # G, and the other operand: one bfloat16 if everything is; else two half floats of 2^13 G (one suffices for bfloat16
+    # gradients), and bfloat16 x and weight are half floats but for what is below a column's largest by 2^-38
+    half = (kind, grad) != ("bf16", "bf16")
+    low = 2.0**-38 if half else 0.0
+    e_g += low * np.where(on[:, None], np.abs(np.repeat(c, np.diff(off)))[:, None], 0.0)
+    for_x = 2.0**-8 if not half else 2.0**-11 if kind == "bf16" else 3 * 2.0**-22
+    for_w = 2.0**-8 if not half else 2.0**-10 if (kind, grad) == ("f32", "bf16") else 3 * 2.0**-22
+    pieces = 32
+    steps = lambda n: 2 * U * (3 * (n // 32 + 2) + 40 + pieces)  # noqa: E731
+    room = (e_g + np.abs(g) * for_x) @ np.abs(hw) + (np.abs(g) @ np.abs(hw)) * steps(V)
+    near(dx, want_dx, room + low * np.abs(g).sum(axis=1)[:, None] * np.abs(hw).max(axis=0), kind, "d_x")
     dw = flat[:, 1:-3].reshape(K, V, dim)
+    top = np.abs(hx[on]).max(axis=0) if on.any() else np.zeros(dim)
     for k in range(K):
         s = slice(off[k], off[k + 1])
         xk = np.where(on[s, None], np.abs(hx[s]), 0.0)
-        room = (e_g[s] + np.abs(g[s]) * rounded).T @ xk + (np.abs(g[s]).T @ xk) * steps(T)
-        near(dw[k], want_dw[k], room, grad, "d_weight")
+        room = (e_g[s] + np.abs(g[s]) * for_w).T @ xk + (np.abs(g[s]).T @ xk) * steps(T)
+        near(dw[k], want_dw[k], room + low * np.abs(g[s]).sum(axis=0)[:, None] * top, grad, "d_weight")
     assert bool((flat[:, 0] == FILL).all()) and bool((flat[:, -3:] == FILL).all())
     assert not host(dx)[~on].any()
     if pad and T > 1:
