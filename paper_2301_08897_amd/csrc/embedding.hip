@@ -171,8 +171,7 @@ __device__ inline void write_grad(W* row, uint32_t left, typename Piece<X>::F su
 // each other in lanes of `lanes`; the rest write zeros, `per` ids of a device each.
 struct Sums {
   uint32_t n, sums, lanes, columns, chunks;      // chunks: groups of kRun sorted tokens
-  uint32_t per, device_groups;
-  Share fill;
+  uint32_t per, device_groups, magic;            // magic: x * magic >> 32 is x / dim for x < per * dim
 };
 
 template <class W>
@@ -181,15 +180,19 @@ __device__ inline void fill_rows(const Grads& g, const Sums& m, const uint32_t* 
   const uint32_t b = blockIdx.x - m.sums, d = b / m.device_groups, a = (b - d * m.device_groups) * m.per;
   const uint32_t ids = g.vocab - a < m.per ? g.vocab - a : m.per;
   if (threadIdx.x < m.per) hit[threadIdx.x] = 0;
-  if (threadIdx.x < 2) {                        // the sorted tokens of these ids
-    const uint32_t want = a + (threadIdx.x ? ids : 0);
-    uint32_t lo = 0, hi = m.n;
+  if (threadIdx.x < 128) {                      // the sorted tokens of these ids: a wave for each end
+    const uint32_t want = a + (threadIdx.x < 64 ? 0 : ids), lane = threadIdx.x & 63;
+    uint32_t lo = 0, hi = m.n;                  // 64 places of the range are looked at at once
     while (lo < hi) {
-      const uint32_t mid = (lo + hi) / 2, c = gptr(cell)[mid];
-      if (c != kNone && c % g.vocab < want) lo = mid + 1;
-      else hi = mid;
+      const uint32_t step = (hi - lo + 63) / 64, at = lo + lane * step;
+      const uint32_t c = at < hi ? gptr(cell)[at] : kNone;
+      const uint32_t below = (uint32_t)__popcll(__ballot(c != kNone && c % g.vocab < want));
+      if (below == 0) break;                    // lo itself is not below
+      const uint32_t last = lo + (below - 1) * step;
+      hi = last + step < hi ? last + step : hi;
+      lo = last + 1;
     }
-    range[threadIdx.x] = lo;
+    if (lane == 0) range[threadIdx.x >> 6] = lo;
   }
   __syncthreads();
   for (uint32_t i = range[0] + threadIdx.x; i < range[1]; i += kBlock) {
@@ -197,11 +200,24 @@ __device__ inline void fill_rows(const Grads& g, const Sums& m, const uint32_t* 
     if (c / g.vocab == d) hit[c % g.vocab - a] = 1;
   }
   __syncthreads();
+  // the rows follow each other: aligned words of 16 bytes where both their ends lie in rows
+  // without a token, single elements elsewhere
+  constexpr uint32_t N = 16 / sizeof(W);
   W* w = (W*)g.w[d] + (uint64_t)a * g.dim;
-  const f4 zero = {0, 0, 0, 0};
-  for_pieces(m.fill, [&](uint32_t r, uint32_t q) {
-    if (r < ids && !hit[r]) store_f4(w + (uint64_t)r * g.dim + q * 4, zero, g.dim - q * 4);
-  });
+  const uint32_t n = ids * g.dim, skip = (uint32_t)((16 - (uintptr_t)w % 16) % 16 / sizeof(W));
+  auto row = [&](uint32_t i) { return m.per == 1 ? 0u : g.dim == 1 ? i : __umulhi(i, m.magic); };
+  for (uint32_t i = threadIdx.x; i <= (n + N - 1) / N; i += kBlock) {
+    // word i begins N elements before the next; the first one may begin before the rows
+    const int32_t lo = (int32_t)(i * N) + (int32_t)skip - (int32_t)N;
+    if (lo >= 0 && lo + N <= n && !hit[row(lo)] && !hit[row(lo + N - 1)] && row(lo + N - 1) - row(lo) <= 1) {
+      *(GLOBAL u4*)gptr(w + lo) = u4{0, 0, 0, 0};
+      continue;
+    }
+    for (uint32_t e = 0; e < N; ++e) {
+      const int32_t at = lo + (int32_t)e;
+      if (at >= 0 && (uint32_t)at < n && !hit[row(at)]) gptr(w)[at] = 0;
+    }
+  }
 }
 
 template <class X, class W, bool kAdd>
@@ -409,13 +425,13 @@ hipError_t sums(const Grads& g, uint64_t n, const Space& s, const void* d_out, u
   uint64_t fills = 0;
   if (!accumulate) {
     // about 64 KiB of rows to a workgroup
-    const uint64_t row = (uint64_t)g.dim * sizeof(W), quads = div_up(g.dim, 4);
+    const uint64_t row = (uint64_t)g.dim * sizeof(W);
     uint64_t per = (64u << 10) / row;
     per = per < 1 ? 1 : per > kFillIds ? kFillIds : per;
     if (per > g.vocab) per = g.vocab;
     m.per = (uint32_t)per;
     m.device_groups = (uint32_t)div_up(g.vocab, per);
-    m.fill = {(uint32_t)quads, m.per, (uint32_t)(per == 1 || quads == 1 ? 0 : div_up(1ull << 32, quads))};
+    m.magic = (uint32_t)(g.dim == 1 ? 0 : div_up(1ull << 32, g.dim));
     fills = (uint64_t)m.device_groups * g.K;
   }
   const uint32_t width = width_of(g.dim);

@@ -20,8 +20,8 @@ using namespace scadles;
 
 namespace {
 
-constexpr uint32_t kBackBlocks = 1024;        // workgroups of a backward pass, about
-constexpr uint32_t kForwardBlocks = 2048;
+constexpr uint32_t kBackBlocks = 960;         // workgroups of a backward pass, about
+constexpr uint32_t kForwardBlocks = 768;
 constexpr uint32_t kJoinLanes = 64, kJoinSlices = 16;
 
 // The weights and the rows that workgroups take.
@@ -36,7 +36,6 @@ struct Split {
   uint64_t off[kMaxK + 1];    // device d's rows
   uint32_t first[kMaxK + 1];  // and workgroups
   uint32_t K;
-  uint64_t per;               // rows of a workgroup
 };
 
 struct Sums {
@@ -50,20 +49,68 @@ __device__ inline typename Piece<X>::F weights_at(const void* p, uint32_t wide, 
 {
   typename Piece<X>::F f;
 #pragma unroll
-  for (uint32_t q = 0; q < Piece<X>::N; ++q)
-    f[q] = q >= left ? 0.0f : wide ? gptr((const float*)p)[at + q] : __uint_as_float((uint32_t)gptr((const uint16_t*)p)[at + q] << 16);
+  for (uint32_t q = 0; q < Piece<X>::N; q += 4) {
+    f4 x = {0, 0, 0, 0};
+    if (q < left) x = wide ? load_f4((const float*)p + at + q, left - q) : load_f4((const uint16_t*)p + at + q, left - q);
+#pragma unroll
+    for (uint32_t e = 0; e < 4; ++e) f[q + e] = x[e];
+  }
   return f;
 }
 
-// The sum of x over a group of G lanes; groups of more than a wave go through `lds`,
-// one float for each wave, which may be used again after the next barrier.
+// One step of a sum over lanes: what `kCtrl` brings from another lane, in the rows of
+// 16 lanes that kRows names (0 elsewhere).
+template <int kCtrl, int kRows>
+__device__ inline float brought(float x)
+{
+  return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), kCtrl, kRows, 0xF, false));
+}
+
+// The sum of x over 16 lanes or a wave, the same in all of them.
+template <int G>
+__device__ inline float lanes_total(float x)
+{
+  x += brought<0xB1, 0xF>(x);      // lanes 1 apart
+  x += brought<0x4E, 0xF>(x);      // 2 apart
+  x += brought<0x141, 0xF>(x);     // the halves of 8
+  x += brought<0x140, 0xF>(x);     // of 16
+  if constexpr (G >= 64) {
+    x += brought<0x142, 0xA>(x);   // the row before, in every second row
+    x += brought<0x143, 0xC>(x);   // the lower half's last row, in the upper half
+    x = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), 63));
+  }
+  return x;
+}
+
+// The sums of a and b over a group of G lanes; groups of more than a wave go through `lds`,
+// which may be used again behind the next call with another one.
+typedef float Sums2[2][kWaves];
+template <int G>
+__device__ inline void group_totals(float& a, float& b, Sums2& lds)
+{
+  a = lanes_total<G>(a);
+  b = lanes_total<G>(b);
+  if constexpr (G > 64) {
+    if (threadIdx.x % 64 == 0) {
+      lds[0][threadIdx.x / 64] = a;
+      lds[1][threadIdx.x / 64] = b;
+    }
+    __syncthreads();
+    a = b = 0.0f;
+#pragma unroll
+    for (int q = 0; q < G / 64; ++q) {
+      a += lds[0][q];
+      b += lds[1][q];
+    }
+  }
+}
+
+// The sum of x alike.
 template <int G>
 __device__ inline float group_total(float x, float* lds)
 {
-#pragma unroll
-  for (int step = 1; step < (G < 64 ? G : 64); step *= 2) x += __shfl_xor(x, step, 64);
+  x = lanes_total<G>(x);
   if constexpr (G > 64) {
-    __syncthreads();
     if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = x;
     __syncthreads();
     x = 0.0f;
@@ -71,6 +118,12 @@ __device__ inline float group_total(float x, float* lds)
     for (int q = 0; q < G / 64; ++q) x += lds[q];
   }
   return x;
+}
+
+template <class F>
+__device__ inline F fused(F x, F y, F z)
+{
+  return __builtin_elementwise_fma(x, y, z);
 }
 
 template <class F>
@@ -97,15 +150,26 @@ __global__ __launch_bounds__(kBlock) void k_norm(Norm m, const X* x, uint64_t ld
     w[j] = weights_at<X>(m.weight, m.wide, at, left);
     b[j] = m.bias ? weights_at<X>(m.bias, m.wide, at, left) : F{};
   }
-  for (uint64_t t = (uint64_t)blockIdx.x * groups + threadIdx.x / G; t < m.tokens; t += (uint64_t)gridDim.x * groups) {
+  const uint64_t step = (uint64_t)gridDim.x * groups;
+  u4 next[P];
+  auto load = [&](uint64_t t) {
+#pragma unroll
+    for (int j = 0; j < P; ++j) {
+      const uint32_t at = (lane + j * G) * N;
+      next[j] = t < m.tokens && at < m.dim ? load_piece(x + t * ld_x + at, m.dim - at) : u4{0, 0, 0, 0};
+    }
+  };
+  uint64_t t = (uint64_t)blockIdx.x * groups + threadIdx.x / G;
+  load(t);
+  for (; t < m.tokens; t += step) {
     F v[P];
     float sum = 0.0f;
 #pragma unroll
     for (int j = 0; j < P; ++j) {
-      const uint32_t at = (lane + j * G) * N;
-      v[j] = at < m.dim ? unpack<X>(load_piece(x + t * ld_x + at, m.dim - at)) : F{};
+      v[j] = unpack<X>(next[j]);
       sum += sum_of(v[j], N);
     }
+    load(t + step);                // under this row's sums
     const float mean = group_total<G>(sum, lds[0]) * m.inverse;
     float square = 0.0f;
 #pragma unroll
@@ -122,7 +186,7 @@ __global__ __launch_bounds__(kBlock) void k_norm(Norm m, const X* x, uint64_t ld
 #pragma unroll
     for (int j = 0; j < P; ++j) {
       const uint32_t at = (lane + j * G) * N;
-      if (at < m.dim) store_piece(y + t * ld_y + at, pack<X>(v[j] * rstd * w[j] + b[j]), m.dim - at);
+      if (at < m.dim) store_piece(y + t * ld_y + at, pack<X>(fused(v[j] * rstd, w[j], b[j])), m.dim - at);
     }
     if (lane == 0) {
       gptr(mean_out)[t] = mean;
@@ -186,10 +250,13 @@ __global__ __launch_bounds__(kBlock) void k_norm_back(Norm m, Split s, Sums o, c
 {
   constexpr uint32_t N = Piece<X>::N, groups = kBlock / G;
   typedef typename Piece<X>::F F;
-  __shared__ float lds[4][kWaves];
+  __shared__ Sums2 lds[2];
+  uint32_t turn = 0;
   __shared__ F over[groups > 1 ? G * groups : 1];
   const uint32_t lane = threadIdx.x % G, group = threadIdx.x / G, d = device_of(s, blockIdx.x);
-  const uint64_t t0 = s.off[d] + (uint64_t)(blockIdx.x - s.first[d]) * s.per, t1 = t0 + s.per < s.off[d + 1] ? t0 + s.per : s.off[d + 1];
+  // the device's workgroups take its rows in turn
+  const uint64_t t0 = s.off[d] + (uint64_t)(blockIdx.x - s.first[d]) * groups + group, t1 = s.off[d + 1];
+  const uint64_t step = (uint64_t)(s.first[d + 1] - s.first[d]) * groups;
   F w[P], sw[P], sb[P];
 #pragma unroll
   for (int j = 0; j < P; ++j) {
@@ -198,32 +265,53 @@ __global__ __launch_bounds__(kBlock) void k_norm_back(Norm m, Split s, Sums o, c
     sw[j] = F{};
     sb[j] = F{};
   }
-  for (uint64_t t = t0 + group; t < t1; t += groups) {
-    const float mean = gptr(mean_in)[t], rstd = gptr(rstd_in)[t];
+  u4 next_x[P], next_g[P];
+  float next_mean = 0.0f, next_rstd = 0.0f;
+  auto load = [&](uint64_t t) {
+    const bool there = t < t1;
+#pragma unroll
+    for (int j = 0; j < P; ++j) {
+      const uint32_t at = (lane + j * G) * N;
+      const bool on = there && at < m.dim;
+      next_x[j] = on ? load_piece(x + t * ld_x + at, m.dim - at) : u4{0, 0, 0, 0};
+      next_g[j] = on ? load_piece(dy + t * ld_dy + at, m.dim - at) : u4{0, 0, 0, 0};
+    }
+    if (there) {
+      next_mean = gptr(mean_in)[t];
+      next_rstd = gptr(rstd_in)[t];
+    }
+  };
+  load(t0);
+  for (uint64_t t = t0; t < t1; t += step) {
+    const float mean = next_mean, rstd = next_rstd;
     F h[P], g[P];
     float a = 0.0f, b = 0.0f;
 #pragma unroll
     for (int j = 0; j < P; ++j) {
-      const uint32_t at = (lane + j * G) * N;
-      const bool on = at < m.dim;
-      h[j] = on ? unpack<X>(load_piece(x + t * ld_x + at, m.dim - at)) : F{};
-      g[j] = on ? unpack<X>(load_piece(dy + t * ld_dy + at, m.dim - at)) : F{};
+      h[j] = unpack<X>(next_x[j]);
+      g[j] = unpack<X>(next_g[j]);
     }
+    load(t + step);                // under this row's sums
 #pragma unroll
     for (int j = 0; j < P; ++j) {       // what lies behind the row has d_y = 0 and adds nothing
       h[j] = (h[j] - mean) * rstd;
-      sw[j] += g[j] * h[j];
+      sw[j] = fused(g[j], h[j], sw[j]);
       sb[j] += g[j];
       g[j] *= w[j];
-      a += sum_of(g[j], N);
-      b += sum_of(g[j] * h[j], N);
+#pragma unroll
+      for (uint32_t q = 0; q < N; ++q) {
+        a += g[j][q];
+        b = __builtin_fmaf(g[j][q], h[j][q], b);
+      }
     }
-    a = group_total<G>(a, lds[0]) * m.inverse;
-    b = group_total<G>(b, lds[1]) * m.inverse;
+    group_totals<G>(a, b, lds[turn]);
+    turn ^= 1;
+    a *= m.inverse;
+    b *= m.inverse;
 #pragma unroll
     for (int j = 0; j < P; ++j) {
       const uint32_t at = (lane + j * G) * N;
-      if (at < m.dim) store_piece(dx + t * ld_dx + at, pack<X>((g[j] - a - h[j] * b) * rstd), m.dim - at);
+      if (at < m.dim) store_piece(dx + t * ld_dx + at, pack<X>(fused(-h[j], F{} + b, g[j] - a) * rstd), m.dim - at);
     }
   }
   for (uint32_t which = 0; which < 2; ++which) {
@@ -285,10 +373,10 @@ __global__ __launch_bounds__(kBlock) void k_norm_columns(Norm m, Split s, Sums o
   const uint32_t at = (blockIdx.y * kBlock + threadIdx.x) * N;
   if (at >= m.dim) return;
   const uint32_t left = m.dim - at, d = device_of(s, blockIdx.x);
-  const uint64_t t0 = s.off[d] + (uint64_t)(blockIdx.x - s.first[d]) * s.per, t1 = t0 + s.per < s.off[d + 1] ? t0 + s.per : s.off[d + 1];
+  const uint64_t t0 = s.off[d] + (blockIdx.x - s.first[d]), step = s.first[d + 1] - s.first[d];
   F sw = {}, sb = {};
 #pragma unroll 4
-  for (uint64_t t = t0; t < t1; ++t) {
+  for (uint64_t t = t0; t < s.off[d + 1]; t += step) {
     const F g = unpack<X>(load_piece(dy + t * ld_dy + at, left));
     sw += g * ((unpack<X>(load_piece(x + t * ld_x + at, left)) - gptr(mean_in)[t]) * gptr(rstd_in)[t]);
     sb += g;
@@ -345,6 +433,7 @@ bool with_row(uint32_t dim, F f)
   SCADLES_ROW(64, 1);
   SCADLES_ROW(64, 2);
   SCADLES_ROW(64, 4);
+  SCADLES_ROW(256, 1);
   SCADLES_ROW(256, 2);
   SCADLES_ROW(256, 4);
   SCADLES_ROW(256, 8);
@@ -370,13 +459,13 @@ uint32_t split_rows(const scadles_batch* b, Split& s)
 {
   std::memset(&s, 0, sizeof(s));
   s.K = b->devices;
-  s.per = div_up(b->tokens, kBackBlocks);
-  if (s.per < 16) s.per = 16;
+  uint64_t per = div_up(b->tokens, kBackBlocks);
+  if (per < 16) per = 16;
   uint64_t w = 0;
   for (uint32_t d = 0; d < s.K; ++d) {
     s.off[d] = b->tok_off[d];
     s.first[d] = (uint32_t)w;
-    w += div_up(b->tok_off[d + 1] - b->tok_off[d], s.per);
+    w += div_up(b->tok_off[d + 1] - b->tok_off[d], per);
   }
   s.off[s.K] = b->tokens;
   s.first[s.K] = (uint32_t)w;
@@ -391,10 +480,12 @@ hipError_t backward(const Norm& m, const Split& s, const Sums& o, uint32_t W, co
 {
   const uint32_t width = width_of(m.dim);
   if (W) {
-    const bool done = with_row<X, 32>(m.dim, [&](auto g, auto p) {
+    // 16 floats of a row to a lane, so that several workgroups share a compute unit (131072 x 2048
+    // bfloat16: 340 us; 32 in a wave: 366), 32 for longer rows
+    auto launch = [&](auto g, auto p) {
       k_norm_back<X, g, p><<<W, kBlock, 0, st>>>(m, s, o, (const X*)x, ld_x, mean, rstd, (const X*)dy, ld_dy, (X*)dx, ld_dx, part, width);
-    });
-    if (!done) {
+    };
+    if (!with_row<X, 16>(m.dim, launch) && !with_row<X, 32>(m.dim, launch)) {
       k_norm_back_long<X><<<(uint32_t)m.tokens, kBlock, 0, st>>>(m, (const X*)x, ld_x, mean, rstd, (const X*)dy, ld_dy, (X*)dx, ld_dx);
       if (o.has_w || o.has_b)
         k_norm_columns<X><<<dim3(W, (uint32_t)div_up(div_up(m.dim, Piece<X>::N), kBlock)), kBlock, 0, st>>>(

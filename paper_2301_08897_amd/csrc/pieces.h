@@ -100,12 +100,12 @@ struct Share {
   uint32_t pieces, rows, magic;
 };
 
-inline Share share_rows(uint64_t rows, uint64_t pieces)
+inline Share share_rows(uint64_t rows, uint64_t pieces, uint64_t most = 1)
 {
-  // enough pieces for every lane of a workgroup, and several where there are far
-  // more than the GPU's lanes
+  // a piece for every lane of a workgroup, or up to `most` where there are far more than
+  // the GPU's lanes
   uint64_t each = rows * pieces / ((uint64_t)kBlock * 4096);
-  each = each < 1 ? 1 : each > 4 ? 4 : each;
+  each = each < 1 ? 1 : each > most ? most : each;
   uint64_t n = pieces > 1024 ? 1 : div_up(kBlock * each, pieces);
   if (n > rows) n = rows ? rows : 1;
   return {(uint32_t)pieces, (uint32_t)n, (uint32_t)(n == 1 ? 0 : div_up(1ull << 32, pieces))};
