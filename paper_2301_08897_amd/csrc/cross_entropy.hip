@@ -41,6 +41,9 @@ constexpr uint32_t kLeastPiece = 2048;            // vocabulary entries of a pie
 constexpr uint32_t kNone = ~0u;
 constexpr uint32_t kMost = 1u << 22;              // tokens and vocabulary entries: 32-bit offsets within a tile
 constexpr uint32_t kLeastSteps = 16;              // of a unit of a split sum, as long as its start and its store
+// rows that a workgroup looks for a column's largest in: fewer of tokens, of which there are few,
+// and which take two loads more to find
+constexpr uint32_t top_rows(bool tokens) { return tokens ? 32 : 256; }
 constexpr int kGBits = 13;                        // G in half floats is scaled by 2^13
 constexpr int kRowsBlock = 1024;
 constexpr uint32_t kRowSlices = kRowsBlock / 64;
@@ -179,26 +182,33 @@ __device__ inline int64_t row_at(const Tokens& a, uint32_t r, uint32_t rows)
   return t >= 0 && target_of(a, t) != kNone ? t : -1;
 }
 
-// The largest magnitude of every column, as bits, over 64 rows at a time (a maximum does
+// The largest magnitude of every column, as bits, over some rows at a time (a maximum does
 // not depend on the order).
 template <class X, bool kTokens>
 __global__ __launch_bounds__(kBlock) void k_column_top(Tokens a, const X* x, uint64_t ld, uint32_t rows, uint32_t dim, uint32_t* top)
 {
   constexpr uint32_t N = Piece<X>::N;
-  const uint32_t at = (blockIdx.y * 64 + threadIdx.x % 64) * N;
-  if (at >= dim) return;
+  __shared__ uint32_t each[kWaves][64 * N];
+  const uint32_t lane = threadIdx.x % 64, w = threadIdx.x / 64, at = (blockIdx.y * 64 + lane) * N;
   uint32_t most[N] = {};
-#pragma unroll 4
-  for (uint32_t r = 0; r < 16; ++r) {
-    const int64_t from = row_at<kTokens>(a, blockIdx.x * 64 + threadIdx.x / 64 * 16 + r, rows);
-    if (from < 0) continue;
-    const auto f = unpack<X>(load_piece(x + from * ld + at, dim - at));
+  if (at < dim) {
+#pragma unroll 8
+    for (uint32_t r = w; r < top_rows(kTokens); r += kWaves) {
+      const int64_t from = row_at<kTokens>(a, blockIdx.x * top_rows(kTokens) + r, rows);
+      const auto f = unpack<X>(load_piece(x + (from < 0 ? 0 : from) * ld + at, from < 0 ? 0 : dim - at));
 #pragma unroll
-    for (uint32_t e = 0; e < N; ++e) most[e] = max(most[e], finite_bits(f[e]));
+      for (uint32_t e = 0; e < N; ++e) most[e] = max(most[e], finite_bits(f[e]));
+    }
   }
 #pragma unroll
-  for (uint32_t e = 0; e < N; ++e)
-    if (at + e < dim && most[e]) atomicMax(top + at + e, most[e]);
+  for (uint32_t e = 0; e < N; ++e) each[w][lane * N + e] = most[e];
+  __syncthreads();
+  for (uint32_t c = threadIdx.x; c < 64 * N && blockIdx.y * 64 * N + c < dim; c += kBlock) {
+    uint32_t t = 0;
+#pragma unroll
+    for (int q = 0; q < kWaves; ++q) t = max(t, each[q][c]);
+    if (t) atomicMax(top + blockIdx.y * 64 * N + c, t);
+  }
 }
 
 // Rows of X transposed to planes [dim][stride], 64 x 64 at a time; half floats are scaled by
@@ -274,7 +284,13 @@ struct Logits {
 template <bool kExact>
 __device__ inline float exp_of(float x)
 {
-  if constexpr (kExact) return expf(x);
+  constexpr float log2e = 1.44269504088896340736f;
+  if constexpr (kExact) {
+    // 2^(x log2 e) with what the product's rounding and log2 e's leave: off by a step of the
+    // result's, in a third of expf's instructions
+    const float h = x * log2e, rest = __builtin_fmaf(x, log2e, -h) + x * 1.92596299e-8f, p = __builtin_amdgcn_exp2f(h);
+    return __builtin_fmaf(p, h > -200.0f ? rest * 0.693147180559945f : 0.0f, p);
+  }
   else return __builtin_amdgcn_exp2f(x * 1.44269504088896340736f);
 }
 
@@ -934,8 +950,8 @@ void turn(const scadles_cross_entropy* ce, const Tokens& a, const Plan& p, const
   if constexpr (std::is_same<E, F16>::value) {
     k_clear<<<(uint32_t)div_up(2 * dim, kBlock), kBlock, 0, st>>>(p.w_top, 2 * dim);
     const uint32_t across = (uint32_t)div_up(dim, 64 * Piece<X>::N);
-    k_column_top<X, false><<<dim3((uint32_t)div_up(V, 64), across), kBlock, 0, st>>>(a, (const X*)weight, ld_w, V, dim, p.w_top);
-    if (tokens) k_column_top<X, true><<<dim3(a.places / 64, across), kBlock, 0, st>>>(a, (const X*)x, ld_x, T, dim, p.x_top);
+    k_column_top<X, false><<<dim3((uint32_t)div_up(V, top_rows(false)), across), kBlock, 0, st>>>(a, (const X*)weight, ld_w, V, dim, p.w_top);
+    if (tokens) k_column_top<X, true><<<dim3((uint32_t)div_up(a.places, top_rows(true)), across), kBlock, 0, st>>>(a, (const X*)x, ld_x, T, dim, p.x_top);
   }
   k_turn<X, false, E, kPlanes><<<dim3((uint32_t)(p.vocab_width / 64), down), kBlock, 0, st>>>(a, (const X*)weight, ld_w, V, dim, p.w_top, p.wt_stride,
                                                                                              p.wt, dim * p.wt_stride);

@@ -11,9 +11,11 @@ history, and gradients are handed on with ``tensor.backward(gradient)``."""
 from __future__ import annotations
 
 import ctypes
+import math
 from dataclasses import dataclass
 
 import numpy as np
+import torch
 
 import paper_2301_08897_amd as _sc
 
@@ -84,82 +86,74 @@ _cross_entropy_backward = _sc._sig("scadles_cross_entropy_backward", ctypes.c_in
 
 # ---- arguments --------------------------------------------------------------------------------------
 
-def _gpu(t, name, *dtypes):
-    torch = _sc._torch()
+_F32, _I32 = (torch.float32,), (torch.int32,)
+_FLOATS, _INTEGERS = (torch.float32, torch.bfloat16), (torch.int32, torch.int64)
+
+
+def _gpu(t, name, kinds, like):
+    """Refuses what is not a GPU tensor of these types, on the GPU of ``like`` if given."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a GPU tensor")
-    if t.dtype not in dtypes:
-        raise TypeError(f"{name} must be {' or '.join(str(d).removeprefix('torch.') for d in dtypes)}, not {t.dtype}")
-    return t
-
-
-def _rows(t, name, rows, dim, *dtypes, like=None):
-    """(address, elements between rows) of a [rows, dim] tensor whose rows' elements
-    are adjacent; any number for None."""
-    _gpu(t, name, *dtypes)
+    if t.dtype not in kinds:
+        raise TypeError(f"{name} must be {' or '.join(str(d).removeprefix('torch.') for d in kinds)}, not {t.dtype}")
     if like is not None and t.device != like.device:
         raise ValueError(f"{name} must be on {like.device}")
-    if t.dim() != 2 or rows not in (None, t.shape[0]) or dim not in (None, t.shape[1]):
-        raise ValueError(f"{name} must be [{'rows' if rows is None else rows}, {'dim' if dim is None else dim}], not {list(t.shape)}")
-    dim = t.shape[1]
+
+
+def _rows(t, name, rows, dim, kinds, like=None):
+    """(address, elements between rows) of a [rows, dim] tensor whose rows' elements
+    are adjacent; any number for None."""
+    _gpu(t, name, kinds, like)
+    shape = t.shape
+    if len(shape) != 2 or (rows is not None and shape[0] != rows) or (dim is not None and shape[1] != dim):
+        raise ValueError(f"{name} must be [{'rows' if rows is None else rows}, {'dim' if dim is None else dim}], not {list(shape)}")
+    if t.is_contiguous():
+        return t.data_ptr(), shape[1]
     ld, step = t.stride()
-    if dim > 1 and step != 1:
+    if shape[1] > 1 and step != 1:
         raise ValueError(f"{name}: a row's elements must be adjacent")
-    if t.shape[0] < 2:
-        ld = dim
-    elif ld < dim:
+    if shape[0] < 2:
+        ld = shape[1]
+    elif ld < shape[1]:
         raise ValueError(f"{name}: rows overlap")
     return t.data_ptr(), ld
 
 
-def _whole(t, name, entries, *dtypes, like):
+def _whole(t, name, entries, kinds, like):
     """The address of a contiguous tensor of so many entries."""
-    _gpu(t, name, *dtypes)
-    if t.device != like.device:
-        raise ValueError(f"{name} must be on {like.device}")
+    _gpu(t, name, kinds, like)
     if t.numel() != entries or not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous and have {entries} entries")
     return t.data_ptr()
 
 
-def _types():
-    torch = _sc._torch()
-    return torch.float32, torch.bfloat16
-
-
 def _type_of(t):
-    return 1 if t.dtype == _sc._torch().bfloat16 else 0
+    return 1 if t.dtype == torch.bfloat16 else 0
 
 
 def _batch(tokens, tok_off, devices):
     """scadles_batch of the rows; None: all of them the first device's."""
-    off = (_u64 * (devices + 1))()
     if tok_off is None:
         if devices != 1:
             raise ValueError(f"tok_off is needed for {devices} devices")
-        off[1] = tokens
-    else:
-        if len(tok_off) != devices + 1:
-            raise ValueError(f"tok_off must have {devices + 1} entries")
-        for i, x in enumerate(tok_off):
-            if x < 0:
-                raise ValueError("tok_off must not be negative")
-            off[i] = int(x)
-    return Batch(tokens, off, devices)
-
-
-def _stream_of(gpu, stream):
-    if stream is None:
-        return _sc._torch()._C._cuda_getCurrentRawStream(gpu)
-    if stream.device_index != gpu:
-        raise ValueError(f"the stream must be one of cuda:{gpu}")
-    return stream.cuda_stream
+        return Batch(tokens, (_u64 * 2)(0, tokens), 1)
+    if len(tok_off) != devices + 1:
+        raise ValueError(f"tok_off must have {devices + 1} entries")
+    off = [int(x) for x in tok_off]
+    if min(off) < 0:
+        raise ValueError("tok_off must not be negative")
+    return Batch(tokens, (_u64 * (devices + 1))(*off), devices)
 
 
 def _run(call, *args, like, stream):
     """A library call on the tensor's GPU, with the stream's address as its last argument."""
-    torch, gpu = _sc._torch(), like.device.index
-    p = _stream_of(gpu, stream)
+    gpu = like.get_device()
+    if stream is None:
+        p = torch._C._cuda_getCurrentRawStream(gpu)
+    elif stream.device_index != gpu:
+        raise ValueError(f"the stream must be one of cuda:{gpu}")
+    else:
+        p = stream.cuda_stream
     if torch.cuda.current_device() == gpu:
         return _sc._check(call(*args, p))
     with torch.cuda.device(gpu):
@@ -167,43 +161,54 @@ def _run(call, *args, like, stream):
 
 
 def _new(shape, dtype, like, stream):
-    return _sc._empty(shape, dtype, like.device, stream)
+    """Uninitialised memory that belongs to the stream (the current one for None)."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    if stream.device_index != like.get_device():
+        raise ValueError(f"the stream must be one of {like.device}")
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=like.device)
 
 
 def _scratch(size, like, stream):
     """A workspace of the call's: memory of its stream, which the allocator gives to
     others only behind the call there."""
-    return _sc._empty((max(int(size), 256),), _sc._torch().uint8, like.device, stream)
+    return _new((max(size, 256),), torch.uint8, like, stream)
 
 
-def _output(t, name, rows, dim, dtype, like, stream):
+def _output(t, name, rows, dim, kind, like, stream):
     """The tensor that a result goes to, new for None: (tensor, address, elements between rows)."""
     if t is None:
-        t = _new((rows, dim), dtype, like, stream)
+        t = _new((rows, dim), kind, like, stream)
         return t, t.data_ptr(), dim
-    return (t,) + _rows(t, name, rows, dim, dtype, like=like)
+    return (t,) + _rows(t, name, rows, dim, (kind,), like)
 
 
-def _each(tensors, name, devices, shape, *dtypes, like):
-    """(the tensors, their addresses): one contiguous tensor of the shape for each device,
-    as a list or as a tensor [devices, ...]."""
-    torch, n = _sc._torch(), int(np.prod(shape, dtype=np.int64))
-    each = list(tensors) if not isinstance(tensors, torch.Tensor) else [tensors] if tuple(tensors.shape) == shape and devices == 1 \
-        else list(tensors.unbind(0)) if tensors.dim() == len(shape) + 1 else []
+def _each(tensors, name, devices, shape, kinds, like):
+    """(the tensors, their type, their addresses): one contiguous tensor of the shape for each
+    device, as a list or as a tensor [devices, ...] (without that for one device)."""
+    n = math.prod(shape)
+    if isinstance(tensors, torch.Tensor):
+        given = tuple(tensors.shape)
+        if given == (devices,) + shape or (devices == 1 and given == shape):
+            p, size = _whole(tensors, name, devices * n, kinds, like), n * tensors.element_size()
+            return (tensors,), tensors.dtype, (_vp * devices)(*range(p, p + devices * size, size))
+        each = list(tensors.unbind(0)) if tensors.dim() else []
+    else:
+        each = list(tensors)
     if len(each) != devices:
         raise ValueError(f"{name} must be a tensor of {list(shape)} for each of {devices} devices")
-    for i, t in enumerate(each):
-        _whole(t, f"{name}[{i}]", n, *dtypes, like=like)
-        if t.dtype != each[0].dtype:
-            raise TypeError(f"{name} must be of one type")
-    return each, (_vp * devices)(*[t.data_ptr() for t in each])
+    at = [_whole(t, f"{name}[{i}]", n, kinds, like) for i, t in enumerate(each)]
+    if any(t.dtype != each[0].dtype for t in each):
+        raise TypeError(f"{name} must be of one type")
+    return tuple(each), each[0].dtype, (_vp * devices)(*at)
 
 
 def _wrote(*tensors):
     """Tells autograd that the caller's tensors have been written."""
-    given = [t for t in tensors if t is not None and not t.is_inference()]
+    given = tuple(t for t in tensors if t is not None and not t.is_inference())
     if given:
-        _sc._written(tuple(given))
+        _sc._written(given)
 
 
 # ---- tokens sorted by expert ----------------------------------------------------------------------------
@@ -233,32 +238,31 @@ class ExpertOrder:
         """``idx`` int32 [T, k] as ``Router.forward`` gives it (an index outside the
         experts is a missing choice); rows ``tok_off[d]`` to ``tok_off[d + 1]`` are those
         of device d."""
-        i32 = _sc._torch().int32
-        _gpu(idx, "idx", i32)
+        _gpu(idx, "idx", _I32, None)
         if idx.dim() != 2 or idx.shape[1] != self.k or not idx.is_contiguous():
             raise ValueError(f"idx must be contiguous [tokens, {self.k}]")
         T, n, cells = idx.shape[0], idx.numel(), self.experts * self.devices + 1
         batch = _batch(T, tok_off, self.devices)
-        need = int(_order_ws_bytes(T, self.experts, self.k))
-        buf = _new((2 * n + cells,), i32, idx, stream)
-        pos, src, bounds = buf[:n].view(T, self.k), buf[n:2 * n], buf[2 * n:]
-        ws = _scratch(need, idx, stream)
+        need = _order_ws_bytes(T, self.experts, self.k)
+        space = -(-need // 256) * 64               # the workspace before the results, in their memory
+        buf = _new((space + 2 * n + cells,), torch.int32, idx, stream)
+        _, pos, src, bounds = buf.split((space, n, n, cells))
         p = buf.data_ptr()
-        _run(_order_sort, batch, idx.data_ptr(), self.experts, self.k, p, p + 4 * n, p + 8 * n, ws.data_ptr(), ws.numel(),
-             like=idx, stream=stream)
-        return ExpertRows(pos, src, bounds)
+        q = p + 4 * space
+        _run(_order_sort, batch, idx.data_ptr(), self.experts, self.k, q, q + 4 * n, q + 8 * n, p, need, like=idx, stream=stream)
+        return ExpertRows(pos.view(T, self.k), src, bounds)
 
     def _shape(self, order, x, T):
         pos = order.pos
         if pos.device != x.device:
             raise ValueError(f"the order must be on {x.device}")
-        if pos.dtype != _sc._torch().int32 or tuple(pos.shape) != (T, self.k) or not pos.is_contiguous():
+        if pos.dtype != torch.int32 or pos.shape != (T, self.k) or not pos.is_contiguous():
             raise ValueError(f"the order is not one of {T} tokens with {self.k} choices")
         return OrderShape(T, pos.data_ptr(), self.k, x.shape[1], _type_of(x))
 
     def dispatch(self, x, order: ExpertRows, *, out=None, stream=None):
         """The experts' input rows [T * k, dim]: row ``pos[t, c]`` is ``x[t]``."""
-        p, ld = _rows(x, "x", None, None, *_types())
+        p, ld = _rows(x, "x", None, None, _FLOATS)
         T, dim = x.shape
         rows, q, ld_rows = _output(out, "out", T * self.k, dim, x.dtype, x, stream)
         _run(_dispatch, self._shape(order, x, T), p, ld, q, ld_rows, like=x, stream=stream)
@@ -272,12 +276,12 @@ class ExpertOrder:
     def combine(self, rows, gate, order: ExpertRows, *, out=None, stream=None):
         """The tokens' sums [T, dim] of their experts' outputs ``rows`` [T * k, dim] times
         the gates, float32 [T, k]. Gates and rows of missing choices are not read."""
-        _whole(gate, "gate", order.pos.numel(), _types()[0], like=rows)
+        _whole(gate, "gate", order.pos.numel(), _F32, rows)
         return self._combine(rows, "rows", gate.data_ptr(), order, out, "out", stream)
 
     def _combine(self, rows, name, gate, order, out, out_name, stream):
         T = order.pos.shape[0]
-        p, ld = _rows(rows, name, T * self.k, None, *_types())
+        p, ld = _rows(rows, name, T * self.k, None, _FLOATS)
         sums, q, ld_out = _output(out, out_name, T, rows.shape[1], rows.dtype, rows, stream)
         _run(_combine, self._shape(order, rows, T), p, ld, gate, q, ld_out, like=rows, stream=stream)
         _wrote(out)
@@ -286,12 +290,12 @@ class ExpertOrder:
     def combine_backward(self, d_out, rows, gate, order: ExpertRows, *, d_rows=None, stream=None):
         """Gradients of ``rows`` [T * k, dim] (in ``d_rows`` if given, which may be ``rows``
         itself) and of the gates, float32 [T, k], 0 where a choice is missing."""
-        T, f32 = order.pos.shape[0], _types()[0]
-        p, ld = _rows(rows, "rows", T * self.k, None, *_types())
-        up, ld_up = _rows(d_out, "d_out", T, rows.shape[1], rows.dtype, like=rows)
-        g = _whole(gate, "gate", T * self.k, f32, like=rows)
+        T = order.pos.shape[0]
+        p, ld = _rows(rows, "rows", T * self.k, None, _FLOATS)
+        up, ld_up = _rows(d_out, "d_out", T, rows.shape[1], (rows.dtype,), rows)
+        g = _whole(gate, "gate", T * self.k, _F32, rows)
         to, q, ld_to = _output(d_rows, "d_rows", T * self.k, rows.shape[1], rows.dtype, rows, stream)
-        d_gate = _new((T, self.k), f32, rows, stream)
+        d_gate = _new((T, self.k), torch.float32, rows, stream)
         _run(_combine_backward, self._shape(order, rows, T), up, ld_up, p, ld, g, q, ld_to, d_gate.data_ptr(), like=rows, stream=stream)
         _wrote(d_rows)
         return to, d_gate
@@ -311,8 +315,8 @@ class Embedding:
             raise _sc.ScadlesError(1, f"invalid vocab={vocab}, dim={dim}, scale={scale} or devices={devices}")
 
     def _tokens(self, tokens, like):
-        torch = _sc._torch()
-        return _whole(tokens, "tokens", tokens.numel(), torch.int32, torch.int64, like=like)
+        _gpu(tokens, "tokens", _INTEGERS, like)
+        return _whole(tokens, "tokens", tokens.numel(), _INTEGERS, like)
 
     def _shape(self, tokens, x, grad=0):
         return EmbeddingShape(self.vocab, self.dim, _type_of(x), grad, tokens.element_size(), self.scale)
@@ -320,7 +324,7 @@ class Embedding:
     def forward(self, tokens, weight, *, out=None, stream=None):
         """``tokens`` int32 or int64, contiguous, of any shape; ``weight`` [vocab, dim]
         float32 or bfloat16. Returns [tokens, dim] of the weight's type."""
-        p, ld = _rows(weight, "weight", self.vocab, self.dim, *_types())
+        p, ld = _rows(weight, "weight", self.vocab, self.dim, _FLOATS)
         ids, T = self._tokens(tokens, weight), tokens.numel()
         rows, q, ld_out = _output(out, "out", T, self.dim, weight.dtype, weight, stream)
         _run(_embedding_forward, self._shape(tokens, weight), T, ids, p, ld, q, ld_out, like=weight, stream=stream)
@@ -333,15 +337,15 @@ class Embedding:
         part of its flat gradient will do, at any offset), or one tensor [devices, vocab,
         dim]. ``accumulate`` adds to what is there (a table that the logits use too). Tokens
         ``tok_off[d]`` to ``tok_off[d + 1]`` are device d's. Returns ``d_weight``."""
-        p, ld = _rows(d_out, "d_out", None, self.dim, *_types())
+        p, ld = _rows(d_out, "d_out", None, self.dim, _FLOATS)
         T = d_out.shape[0]
         ids = self._tokens(tokens, d_out)
         if tokens.numel() != T:
             raise ValueError(f"tokens must have {T} entries")
         batch = _batch(T, tok_off, self.devices)
-        each, at = _each(d_weight, "d_weight", self.devices, (self.vocab, self.dim), *_types(), like=d_out)
+        each, kind, at = _each(d_weight, "d_weight", self.devices, (self.vocab, self.dim), _FLOATS, d_out)
         ws = _scratch(_embedding_ws_bytes(T, self.vocab, self.dim), d_out, stream)
-        _run(_embedding_backward, self._shape(tokens, d_out, _type_of(each[0])), batch, ids, p, ld, at, int(bool(accumulate)),
+        _run(_embedding_backward, self._shape(tokens, d_out, 1 if kind == torch.bfloat16 else 0), batch, ids, p, ld, at, int(bool(accumulate)),
              ws.data_ptr(), ws.numel(), like=d_out, stream=stream)
         _wrote(*each)
         return d_weight
@@ -372,17 +376,16 @@ class LayerNorm:
 
     def forward(self, x, weight, bias=None, *, out=None, stream=None) -> LayerNormOutputs:
         """``x`` [T, dim]; ``y`` is of its type."""
-        f32 = _types()[0]
-        p, ld = _rows(x, "x", None, self.dim, *_types())
-        w = _whole(weight, "weight", self.dim, *_types(), like=x)
-        b = None if bias is None else _whole(bias, "bias", self.dim, weight.dtype, like=x)
+        p, ld = _rows(x, "x", None, self.dim, _FLOATS)
+        w = _whole(weight, "weight", self.dim, _FLOATS, x)
+        b = None if bias is None else _whole(bias, "bias", self.dim, (weight.dtype,), x)
         T = x.shape[0]
         y, q, ld_y = _output(out, "out", T, self.dim, x.dtype, x, stream)
-        both = _new((2, T), f32, x, stream)
+        both = _new((2, T), torch.float32, x, stream)
         m = both.data_ptr()
         _run(_layer_norm_forward, self._shape(x, weight), T, p, ld, w, b, q, ld_y, m, m + 4 * T, like=x, stream=stream)
         _wrote(out)
-        return LayerNormOutputs(y, both[0], both[1])
+        return LayerNormOutputs(y, *both.unbind(0))
 
     def backward(self, x, weight, out: LayerNormOutputs, d_y, d_weight=None, d_bias=None, *, tok_off=None, d_x=None, stream=None):
         """The gradient of ``x`` [T, dim] (in ``d_x`` if given) under ``d_y``, and those of
@@ -390,26 +393,25 @@ class LayerNorm:
         dim elements for each device (a part of its flat gradient will do), or one tensor
         [devices, dim]; None where they are not wanted. ``out`` is the forward pass's
         (its mean and rstd are read); rows ``tok_off[d]`` to ``tok_off[d + 1]`` are device d's."""
-        f32 = _types()[0]
-        p, ld = _rows(x, "x", None, self.dim, *_types())
+        p, ld = _rows(x, "x", None, self.dim, _FLOATS)
         T = x.shape[0]
-        w = _whole(weight, "weight", self.dim, *_types(), like=x)
-        g, ld_g = _rows(d_y, "d_y", T, self.dim, x.dtype, like=x)
-        mean, rstd = _whole(out.mean, "mean", T, f32, like=x), _whole(out.rstd, "rstd", T, f32, like=x)
+        w = _whole(weight, "weight", self.dim, _FLOATS, x)
+        g, ld_g = _rows(d_y, "d_y", T, self.dim, (x.dtype,), x)
+        mean, rstd = _whole(out.mean, "mean", T, _F32, x), _whole(out.rstd, "rstd", T, _F32, x)
         if tok_off is None and d_weight is None and d_bias is None:
             batch = _batch(T, None, 1)
         else:
             batch = _batch(T, tok_off, self.devices)
-        given, at = [], []
+        given, at = (d_x,), []
         for t, name in ((d_weight, "d_weight"), (d_bias, "d_bias")):
-            each, where = ([], None) if t is None else _each(t, name, self.devices, (self.dim,), f32, like=x)
+            each, _, where = ((), None, None) if t is None else _each(t, name, self.devices, (self.dim,), _F32, x)
             given += each
             at.append(where)
         dx, q, ld_dx = _output(d_x, "d_x", T, self.dim, x.dtype, x, stream)
         ws = _scratch(_layer_norm_ws_bytes(T, self.dim), x, stream)
         _run(_layer_norm_backward, self._shape(x, weight), batch, p, ld, w, mean, rstd, g, ld_g, q, ld_dx, at[0], at[1],
              ws.data_ptr(), ws.numel(), like=x, stream=stream)
-        _wrote(d_x, *given)
+        _wrote(*given)
         return dx
 
 
@@ -438,11 +440,10 @@ class LinearCrossEntropy:
             raise _sc.ScadlesError(1, f"invalid vocab={vocab}, dim={dim} or devices={devices}")
 
     def _arguments(self, x, weight, target, tok_off, grad):
-        torch = _sc._torch()
-        p, ld = _rows(x, "x", None, self.dim, *_types())
-        w, ld_w = _rows(weight, "weight", self.vocab, self.dim, x.dtype, like=x)
+        p, ld = _rows(x, "x", None, self.dim, _FLOATS)
+        w, ld_w = _rows(weight, "weight", self.vocab, self.dim, (x.dtype,), x)
         T = x.shape[0]
-        ids = _whole(target, "target", T, torch.int32, torch.int64, like=x)
+        ids = _whole(target, "target", T, _INTEGERS, x)
         batch = _batch(T, tok_off, self.devices)
         return T, CrossEntropyShape(self.vocab, self.dim, _type_of(x), grad, target.element_size()), batch, (p, ld, w, ld_w, ids)
 
@@ -454,17 +455,16 @@ class LinearCrossEntropy:
     def forward(self, x, weight, target, *, tok_off=None, weights=None, stream=None) -> CrossEntropyOutputs:
         """Rows ``tok_off[d]`` to ``tok_off[d + 1]`` are device d's. ``weights``: Eqn 4a, by
         default the devices' shares of the rows."""
-        f32 = _types()[0]
         T, shape, batch, args = self._arguments(x, weight, target, tok_off, 0)
         if weights is None:
             weights = [(batch.tok_off[d + 1] - batch.tok_off[d]) / T if T else 1.0 / self.devices for d in range(self.devices)]
         K = self.devices
-        buf = _new((2 * T + 2 * K + 1,), f32, x, stream)
+        buf = _new((2 * T + 2 * K + 1,), torch.float32, x, stream)
         q = buf.data_ptr()
         at = CrossEntropyOut(q, q + 4 * T, q + 8 * T, q + 8 * T + 4 * K, q + 8 * T + 8 * K)
         ws = _scratch(_cross_entropy_ws_bytes(shape, batch, 0), x, stream)
         _run(_cross_entropy_forward, shape, batch, self._weights(weights), *args, at, ws.data_ptr(), ws.numel(), like=x, stream=stream)
-        return CrossEntropyOutputs(buf[:T], buf[T:2 * T], buf[2 * T:2 * T + K], buf[2 * T + K:2 * T + 2 * K], buf[2 * T + 2 * K:])
+        return CrossEntropyOutputs(*buf.split((T, T, K, K, 1)))
 
     def backward(self, x, weight, target, out: CrossEntropyOutputs, d_weight=None, *, tok_off=None, weights=None, d_loss=None, d_x=None,
                  stream=None):
@@ -476,16 +476,13 @@ class LinearCrossEntropy:
         device has the gradient of its own loss, before the aggregation weights it; the
         forward pass's give the gradient of its ``loss``. All of it times ``d_loss``, one
         float32 on the GPU, if given."""
-        f32 = _types()[0]
-        each, where, grad = [], None, 0
+        _gpu(x, "x", _FLOATS, None)
+        each, kind, where = (), x.dtype, None
         if d_weight is not None:
-            each, where = _each(d_weight, "d_weight", self.devices, (self.vocab, self.dim), *_types(), like=x)
-            grad = _type_of(each[0])
-        elif isinstance(x, _sc._torch().Tensor):
-            grad = _type_of(x)
-        T, shape, batch, args = self._arguments(x, weight, target, tok_off, grad)
-        lse, share = _whole(out.lse, "lse", T, f32, like=x), _whole(out.share, "share", self.devices, f32, like=x)
-        d = None if d_loss is None else _whole(d_loss, "d_loss", 1, f32, like=x)
+            each, kind, where = _each(d_weight, "d_weight", self.devices, (self.vocab, self.dim), _FLOATS, x)
+        T, shape, batch, args = self._arguments(x, weight, target, tok_off, 1 if kind == torch.bfloat16 else 0)
+        lse, share = _whole(out.lse, "lse", T, _F32, x), _whole(out.share, "share", self.devices, _F32, x)
+        d = None if d_loss is None else _whole(d_loss, "d_loss", 1, _F32, x)
         dx, q, ld_dx = _output(d_x, "d_x", T, self.dim, x.dtype, x, stream)
         ws = _scratch(_cross_entropy_ws_bytes(shape, batch, 1), x, stream)
         _run(_cross_entropy_backward, shape, batch, None if weights is None else self._weights(weights), *args,
