@@ -264,8 +264,9 @@ class ExpertOrder:
         """The experts' input rows [T * k, dim]: row ``pos[t, c]`` is ``x[t]``."""
         p, ld = _rows(x, "x", None, None, _FLOATS)
         T, dim = x.shape
+        shape = self._shape(order, x, T)
         rows, q, ld_rows = _output(out, "out", T * self.k, dim, x.dtype, x, stream)
-        _run(_dispatch, self._shape(order, x, T), p, ld, q, ld_rows, like=x, stream=stream)
+        _run(_dispatch, shape, p, ld, q, ld_rows, like=x, stream=stream)
         _wrote(out)
         return rows
 
@@ -282,8 +283,9 @@ class ExpertOrder:
     def _combine(self, rows, name, gate, order, out, out_name, stream):
         T = order.pos.shape[0]
         p, ld = _rows(rows, name, T * self.k, None, _FLOATS)
+        shape = self._shape(order, rows, T)
         sums, q, ld_out = _output(out, out_name, T, rows.shape[1], rows.dtype, rows, stream)
-        _run(_combine, self._shape(order, rows, T), p, ld, gate, q, ld_out, like=rows, stream=stream)
+        _run(_combine, shape, p, ld, gate, q, ld_out, like=rows, stream=stream)
         _wrote(out)
         return sums
 
@@ -294,9 +296,10 @@ class ExpertOrder:
         p, ld = _rows(rows, "rows", T * self.k, None, _FLOATS)
         up, ld_up = _rows(d_out, "d_out", T, rows.shape[1], (rows.dtype,), rows)
         g = _whole(gate, "gate", T * self.k, _F32, rows)
+        shape = self._shape(order, rows, T)
         to, q, ld_to = _output(d_rows, "d_rows", T * self.k, rows.shape[1], rows.dtype, rows, stream)
         d_gate = _new((T, self.k), torch.float32, rows, stream)
-        _run(_combine_backward, self._shape(order, rows, T), up, ld_up, p, ld, g, q, ld_to, d_gate.data_ptr(), like=rows, stream=stream)
+        _run(_combine_backward, shape, up, ld_up, p, ld, g, q, ld_to, d_gate.data_ptr(), like=rows, stream=stream)
         _wrote(d_rows)
         return to, d_gate
 
@@ -458,12 +461,12 @@ class LinearCrossEntropy:
         T, shape, batch, args = self._arguments(x, weight, target, tok_off, 0)
         if weights is None:
             weights = [(batch.tok_off[d + 1] - batch.tok_off[d]) / T if T else 1.0 / self.devices for d in range(self.devices)]
-        K = self.devices
+        weights, K = self._weights(weights), self.devices
         buf = _new((2 * T + 2 * K + 1,), torch.float32, x, stream)
         q = buf.data_ptr()
         at = CrossEntropyOut(q, q + 4 * T, q + 8 * T, q + 8 * T + 4 * K, q + 8 * T + 8 * K)
         ws = _scratch(_cross_entropy_ws_bytes(shape, batch, 0), x, stream)
-        _run(_cross_entropy_forward, shape, batch, self._weights(weights), *args, at, ws.data_ptr(), ws.numel(), like=x, stream=stream)
+        _run(_cross_entropy_forward, shape, batch, weights, *args, at, ws.data_ptr(), ws.numel(), like=x, stream=stream)
         return CrossEntropyOutputs(*buf.split((T, T, K, K, 1)))
 
     def backward(self, x, weight, target, out: CrossEntropyOutputs, d_weight=None, *, tok_off=None, weights=None, d_loss=None, d_x=None,
@@ -483,9 +486,10 @@ class LinearCrossEntropy:
         T, shape, batch, args = self._arguments(x, weight, target, tok_off, 1 if kind == torch.bfloat16 else 0)
         lse, share = _whole(out.lse, "lse", T, _F32, x), _whole(out.share, "share", self.devices, _F32, x)
         d = None if d_loss is None else _whole(d_loss, "d_loss", 1, _F32, x)
+        weights = None if weights is None else self._weights(weights)
         dx, q, ld_dx = _output(d_x, "d_x", T, self.dim, x.dtype, x, stream)
         ws = _scratch(_cross_entropy_ws_bytes(shape, batch, 1), x, stream)
-        _run(_cross_entropy_backward, shape, batch, None if weights is None else self._weights(weights), *args,
+        _run(_cross_entropy_backward, shape, batch, weights, *args,
              CrossEntropyOut(None, lse, None, share, None), d, q, ld_dx, where, ws.data_ptr(), ws.numel(), like=x, stream=stream)
         _wrote(d_x, *each)
         return dx
