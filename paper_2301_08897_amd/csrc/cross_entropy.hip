@@ -160,10 +160,11 @@ __global__ __launch_bounds__(kBlock) void k_align(const uint16_t* x, uint64_t ld
                                                   uint16_t* out)
 {
   const uint32_t per = width / 8;
-  const uint64_t i = (uint64_t)blockIdx.x * kBlock + threadIdx.x, r = i / per;
-  const uint32_t at = (uint32_t)(i - r * per) * 8;
-  if (r >= rows) return;
-  *(GLOBAL u4*)gptr(out + r * stride + at) = load_piece(x + r * ld + at, at < dim ? dim - at : 0);
+  for (uint64_t i = (uint64_t)blockIdx.x * kBlock + threadIdx.x; i < rows * per; i += (uint64_t)gridDim.x * kBlock) {
+    const uint64_t r = i / per;
+    const uint32_t at = (uint32_t)(i - r * per) * 8;
+    *(GLOBAL u4*)gptr(out + r * stride + at) = load_piece(x + r * ld + at, at < dim ? dim - at : 0);
+  }
 }
 
 __global__ void k_clear(uint32_t* p, uint32_t n)
@@ -680,9 +681,7 @@ __global__ __launch_bounds__(kProductBlock, 2) void k_gradients(Tokens a, Gradie
 template <class E, class X>
 __global__ __launch_bounds__(kBlock) void k_join_x(Tokens a, Gradients q, Share share)
 {
-  for_pieces(share, [&](uint32_t r, uint32_t g) {
-    const uint64_t p = (uint64_t)blockIdx.x * share.rows + r;
-    if (p >= a.places) return;
+  for_all_pieces(share, a.places, [&](uint64_t p, uint32_t g) {
     const Where w = token_at(a, (uint32_t)p);
     if (w.t < 0) return;
     const uint32_t m = g * 4, left = q.dim - m;
@@ -700,9 +699,7 @@ __global__ __launch_bounds__(kBlock) void k_join_weight(Tokens a, Gradients q, S
   const uint32_t d = blockIdx.y, lo = q.w_first[d], hi = q.w_first[d + 1];
   if (hi - lo == 1) return;
   const float c = factor_of(a, q, d);
-  for_pieces(share, [&](uint32_t r, uint32_t g) {
-    const uint64_t v = (uint64_t)blockIdx.x * share.rows + r;
-    if (v >= q.v1 - q.v0) return;
+  for_all_pieces(share, q.v1 - q.v0, [&](uint64_t v, uint32_t g) {
     const uint32_t m = g * 4, left = q.dim - m;
     f4 x = {0, 0, 0, 0};
     for (uint32_t u = lo; u < hi; ++u) x += load_f4(q.w_sum + ((uint64_t)u * q.piece + v) * q.dim + m, left);
@@ -898,7 +895,7 @@ Matrix operand(const scadles_cross_entropy* ce, const Plan& p, const void* x, ui
       k_planes<<<(uint32_t)div_up(rows, kWaves), kBlock, 0, st>>>((const float*)x, ld, (uint32_t)rows, ce->dim, (uint32_t)p.x_width, p.x_stride, to,
                                                                   plane, scale);
     else
-      k_align<<<(uint32_t)div_up(rows * (p.x_width / 8), kBlock), kBlock, 0, st>>>((const uint16_t*)x, ld, rows, ce->dim, (uint32_t)p.x_width,
+      k_align<<<grid_of(div_up(rows * (p.x_width / 8), kBlock)), kBlock, 0, st>>>((const uint16_t*)x, ld, rows, ce->dim, (uint32_t)p.x_width,
                                                                                   p.x_stride, to);
   }
   return {to, plane, p.x_stride};
@@ -1025,12 +1022,12 @@ hipError_t backward(const scadles_cross_entropy* ce, const Tokens& a, const Plan
     if (units) k_gradients<E, X, W><<<(uint32_t)units, kProductBlock, 0, st>>>(a, r);
     if (d_weight && p.w_sum) {
       const Share share = share_rows(v1 - v0, quads);
-      k_join_weight<E, W><<<dim3((uint32_t)div_up(v1 - v0, share.rows), a.K), kBlock, 0, st>>>(a, r, share);
+      k_join_weight<E, W><<<dim3(grid_of(div_up(v1 - v0, share.rows)), a.K), kBlock, 0, st>>>(a, r, share);
     }
   }
   if (r.x_units > 1 && a.places) {
     const Share share = share_rows(a.places, quads);
-    k_join_x<E, X><<<(uint32_t)div_up(a.places, share.rows), kBlock, 0, st>>>(a, r, share);
+    k_join_x<E, X><<<grid_of(div_up(a.places, share.rows)), kBlock, 0, st>>>(a, r, share);
   }
   return hipGetLastError();
 }

@@ -13,6 +13,7 @@
 // The rows without a token are set to zero by further workgroups of the same
 // launch, which search the sorted tokens for their ids. So every element of a
 // gradient is written once, and nothing depends on the order of workgroups.
+#include <algorithm>
 #include <cstring>
 
 #include "pieces.h"
@@ -68,10 +69,7 @@ template <class X>
 __global__ __launch_bounds__(kBlock) void k_embed(Ids a, uint64_t tokens, Share share, uint32_t dim, float scale, const X* weight,
                                                   uint64_t ld_w, X* out, uint64_t ld_out)
 {
-  const uint64_t t0 = (uint64_t)blockIdx.x * share.rows;
-  for_pieces(share, [&](uint32_t r, uint32_t g) {
-    const uint64_t t = t0 + r;
-    if (t >= tokens) return;
+  for_all_pieces(share, tokens, [&](uint64_t t, uint32_t g) {
     const uint32_t at = g * Piece<X>::N, left = dim - at, id = token_id(a, t);
     u4 v = {0, 0, 0, 0};
     if (id < a.vocab) v = pack<X>(unpack<X>(load_piece(weight + (uint64_t)id * ld_w + at, left)) * scale);
@@ -175,9 +173,9 @@ struct Sums {
 };
 
 template <class W>
-__device__ inline void fill_rows(const Grads& g, const Sums& m, const uint32_t* cell, uint8_t* hit, uint32_t* range)
+__device__ inline void fill_rows(const Grads& g, const Sums& m, uint32_t b, const uint32_t* cell, uint8_t* hit, uint32_t* range)
 {
-  const uint32_t b = blockIdx.x - m.sums, d = b / m.device_groups, a = (b - d * m.device_groups) * m.per;
+  const uint32_t d = b / m.device_groups, a = (b - d * m.device_groups) * m.per;
   const uint32_t ids = g.vocab - a < m.per ? g.vocab - a : m.per;
   if (threadIdx.x < m.per) hit[threadIdx.x] = 0;
   if (threadIdx.x < 128) {                      // the sorted tokens of these ids: a wave for each end
@@ -228,7 +226,13 @@ __global__ __launch_bounds__(kBlock) void k_embed_sum(Grads g, Sums m, const uin
   if constexpr (!kAdd) {
     __shared__ uint8_t hit[kFillIds];
     __shared__ uint32_t range[2];
-    if (blockIdx.x >= m.sums) return fill_rows<W>(g, m, cell, hit, range);
+    if (blockIdx.x >= m.sums) {
+      for (uint32_t b = blockIdx.x - m.sums; b < m.device_groups * g.K; b += gridDim.x - m.sums) {
+        fill_rows<W>(g, m, b, cell, hit, range);
+        __syncthreads();
+      }
+      return;
+    }
   }
   const uint32_t column = blockIdx.x % m.columns, chunk = blockIdx.x / m.columns * (kBlock / m.lanes) + threadIdx.x / m.lanes;
   const uint32_t at = (column * m.lanes + threadIdx.x % m.lanes) * Piece<X>::N;
@@ -274,11 +278,11 @@ __global__ __launch_bounds__(kBlock) void k_embed_sum(Grads g, Sums m, const uin
 // The cells that begin in a chunk of sorted tokens and go on behind it. The workgroup's
 // lanes share the columns, and the chunks of a long cell in slices.
 template <class X, class W, bool kAdd>
-__global__ __launch_bounds__(kJoinBlock) void k_embed_join(Grads g, Sums m, const uint32_t* cell, const float* part, uint32_t width)
+__device__ inline void join_cell(const Grads& g, const Sums& m, uint32_t block, const uint32_t* cell, const float* part, uint32_t width,
+                                 typename Piece<X>::F* slice)
 {
   typedef typename Piece<X>::F F;
-  __shared__ F slice[kJoinBlock];
-  const uint32_t column = blockIdx.x % m.columns, chunk = blockIdx.x / m.columns;
+  const uint32_t column = block % m.columns, chunk = block / m.columns;
   const uint32_t first = (chunk + 1) * kRun;             // of the next chunk; the last chunk has no workgroup here
   const uint32_t now = gptr(cell)[first];
   if (now == kNone || gptr(cell)[first - 1] != now) return;
@@ -310,6 +314,16 @@ __global__ __launch_bounds__(kJoinBlock) void k_embed_join(Grads g, Sums m, cons
   for (uint32_t q = 1; q < slices; ++q) sum += slice[q * m.lanes + lane];
   const uint32_t d = now / g.vocab;
   write_grad<X>((W*)g.w[d] + (uint64_t)(now - d * g.vocab) * g.dim + at, g.dim - at, sum * g.scale, kAdd);
+}
+
+template <class X, class W, bool kAdd>
+__global__ __launch_bounds__(kJoinBlock) void k_embed_join(Grads g, Sums m, const uint32_t* cell, const float* part, uint32_t width)
+{
+  __shared__ typename Piece<X>::F slice[kJoinBlock];
+  for (uint32_t b = blockIdx.x; b < (m.chunks - 1) * m.columns; b += gridDim.x) {
+    join_cell<X, W, kAdd>(g, m, b, cell, part, width, slice);
+    __syncthreads();
+  }
 }
 
 // ---- host -------------------------------------------------------------------------------------------------
@@ -376,7 +390,7 @@ hipError_t forward(const scadles_embedding* e, uint64_t tokens, const void* ids,
 {
   const Ids a = {ids, nullptr, nullptr, e->token_bytes == 8, (uint32_t)e->vocab};
   const Share share = share_rows(tokens, div_up(e->dim, Piece<X>::N));
-  k_embed<X><<<(uint32_t)div_up(tokens, share.rows), kBlock, 0, st>>>(a, tokens, share, e->dim, e->scale, (const X*)weight, ld_w, (X*)out,
+  k_embed<X><<<grid_of(div_up(tokens, share.rows)), kBlock, 0, st>>>(a, tokens, share, e->dim, e->scale, (const X*)weight, ld_w, (X*)out,
                                                                       ld_out);
   return hipGetLastError();
 }
@@ -432,17 +446,17 @@ hipError_t sums(const Grads& g, uint64_t n, const Space& s, const void* d_out, u
     m.per = (uint32_t)per;
     m.device_groups = (uint32_t)div_up(g.vocab, per);
     m.magic = (uint32_t)(g.dim == 1 ? 0 : div_up(1ull << 32, g.dim));
-    fills = (uint64_t)m.device_groups * g.K;
+    fills = grid_of((uint64_t)m.device_groups * g.K);
   }
   const uint32_t width = width_of(g.dim);
-  if (m.sums + fills > 0x7FFFFFFFull) return hipErrorInvalidValue;
+  if (m.sums > kMostBlocks) return hipErrorInvalidValue;      // more than 2^19 MB of rows
   if (m.sums + fills) {
     const uint32_t blocks = (uint32_t)(m.sums + fills);
     if (accumulate) k_embed_sum<X, W, true><<<blocks, kBlock, 0, st>>>(g, m, s.cell, s.src, (const X*)d_out, ld, s.part, width);
     else k_embed_sum<X, W, false><<<blocks, kBlock, 0, st>>>(g, m, s.cell, s.src, (const X*)d_out, ld, s.part, width);
   }
   if (m.chunks > 1) {
-    const uint32_t blocks = (m.chunks - 1) * m.columns;
+    const uint32_t blocks = (uint32_t)std::min<uint64_t>((uint64_t)(m.chunks - 1) * m.columns, kMostBlocks / 2);
     if (accumulate) k_embed_join<X, W, true><<<blocks, kJoinBlock, 0, st>>>(g, m, s.cell, s.part, width);
     else k_embed_join<X, W, false><<<blocks, kJoinBlock, 0, st>>>(g, m, s.cell, s.part, width);
   }

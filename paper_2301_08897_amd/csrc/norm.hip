@@ -201,7 +201,7 @@ __global__ __launch_bounds__(kBlock) void k_norm_long(Norm m, const X* x, uint64
 {
   constexpr uint32_t N = Piece<X>::N;
   __shared__ float lds[2][kWaves];
-  const uint64_t t = blockIdx.x;
+  const uint64_t t = blockIdx.x;     // fewer than 2^24 rows this long fit in memory
   const X* row = x + t * ld_x;
   float sum = 0.0f, square = 0.0f;
   for (uint32_t at = threadIdx.x * N; at < m.dim; at += kBlock * N) sum += sum_of(unpack<X>(load_piece(row + at, m.dim - at)), N);

@@ -145,10 +145,7 @@ __device__ inline bool row_of(const Move& m, uint64_t i, uint32_t& p)
 template <class X>
 __global__ __launch_bounds__(kBlock) void k_dispatch(Move m, uint32_t k, const X* x, uint64_t ld_x, X* rows, uint64_t ld_rows)
 {
-  const uint64_t t0 = (uint64_t)blockIdx.x * m.share.rows;
-  for_pieces(m.share, [&](uint32_t r, uint32_t g) {
-    const uint64_t t = t0 + r;
-    if (t >= m.tokens) return;
+  for_all_pieces(m.share, m.tokens, [&](uint64_t t, uint32_t g) {
     const uint32_t at = g * Piece<X>::N, left = m.dim - at;
     const u4 v = load_piece(x + t * ld_x + at, left);
     for (uint32_t c = 0; c < k; ++c) {
@@ -163,10 +160,7 @@ template <class X, int C, bool kGate>
 __global__ __launch_bounds__(kBlock) void k_combine(Move m, uint32_t k, const X* rows, uint64_t ld_rows, const float* gate, X* out,
                                                     uint64_t ld_out)
 {
-  const uint64_t t0 = (uint64_t)blockIdx.x * m.share.rows;
-  for_pieces(m.share, [&](uint32_t r, uint32_t g) {
-    const uint64_t t = t0 + r;
-    if (t >= m.tokens) return;
+  for_all_pieces(m.share, m.tokens, [&](uint64_t t, uint32_t g) {
     const uint32_t at = g * Piece<X>::N, left = m.dim - at;
     typename Piece<X>::F sum = {};
     for (uint32_t c0 = 0; c0 < k; c0 += C) {
@@ -197,50 +191,50 @@ template <class X, int C, int G>
 __global__ __launch_bounds__(kBlock) void k_combine_back(Move m, uint32_t k, const X* d_out, uint64_t ld_d_out, const X* rows,
                                                          uint64_t ld_rows, const float* gate, X* d_rows, uint64_t ld_d_rows, float* d_gate)
 {
-  const uint64_t t = (uint64_t)blockIdx.x * (kBlock / G) + threadIdx.x / G;
   const uint32_t lane = threadIdx.x % G;
-  if (t >= m.tokens) return;
-  for (uint32_t c0 = 0; c0 < k; c0 += C) {
-    uint32_t p[C];
-    bool on[C];
-    float w[C], sum[C];
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-      on[c] = c0 + c < k && row_of(m, t * k + c0 + c, p[c]);
-      w[c] = on[c] ? gptr(gate)[t * k + c0 + c] : 0.0f;
-      sum[c] = 0.0f;
-    }
-    for (uint32_t at = lane * Piece<X>::N; at < m.dim; at += G * Piece<X>::N) {
-      const uint32_t left = m.dim - at;
-      const auto g = unpack<X>(load_piece(d_out + t * ld_d_out + at, left));
-      u4 v[C];
-      if (d_gate) {
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-          if (on[c]) v[c] = load_piece(rows + (uint64_t)p[c] * ld_rows + at, left);
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-          if (on[c]) {
-            const auto y = unpack<X>(v[c]);
-#pragma unroll
-            for (uint32_t q = 0; q < Piece<X>::N; ++q) sum[c] = __builtin_fmaf(g[q], y[q], sum[c]);
-          }
-      }
-      if (d_rows) {
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-          if (on[c]) store_piece_once(d_rows + (uint64_t)p[c] * ld_d_rows + at, pack<X>(g * w[c]), left);
-      }
-    }
-    if (d_gate) {
+  const uint64_t stride = (uint64_t)gridDim.x * (kBlock / G);
+  for (uint64_t t = (uint64_t)blockIdx.x * (kBlock / G) + threadIdx.x / G; t < m.tokens; t += stride)
+    for (uint32_t c0 = 0; c0 < k; c0 += C) {
+      uint32_t p[C];
+      bool on[C];
+      float w[C], sum[C];
 #pragma unroll
       for (int c = 0; c < C; ++c) {
+        on[c] = c0 + c < k && row_of(m, t * k + c0 + c, p[c]);
+        w[c] = on[c] ? gptr(gate)[t * k + c0 + c] : 0.0f;
+        sum[c] = 0.0f;
+      }
+      for (uint32_t at = lane * Piece<X>::N; at < m.dim; at += G * Piece<X>::N) {
+        const uint32_t left = m.dim - at;
+        const auto g = unpack<X>(load_piece(d_out + t * ld_d_out + at, left));
+        u4 v[C];
+        if (d_gate) {
 #pragma unroll
-        for (int step = 1; step < G; step *= 2) sum[c] += __shfl_xor(sum[c], step, 64);
-        if (lane == 0 && c0 + c < k) gptr(d_gate)[t * k + c0 + c] = on[c] ? sum[c] : 0.0f;
+          for (int c = 0; c < C; ++c)
+            if (on[c]) v[c] = load_piece(rows + (uint64_t)p[c] * ld_rows + at, left);
+#pragma unroll
+          for (int c = 0; c < C; ++c)
+            if (on[c]) {
+              const auto y = unpack<X>(v[c]);
+#pragma unroll
+              for (uint32_t q = 0; q < Piece<X>::N; ++q) sum[c] = __builtin_fmaf(g[q], y[q], sum[c]);
+            }
+        }
+        if (d_rows) {
+#pragma unroll
+          for (int c = 0; c < C; ++c)
+            if (on[c]) store_piece_once(d_rows + (uint64_t)p[c] * ld_d_rows + at, pack<X>(g * w[c]), left);
+        }
+      }
+      if (d_gate) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+#pragma unroll
+          for (int step = 1; step < G; step *= 2) sum[c] += __shfl_xor(sum[c], step, 64);
+          if (lane == 0 && c0 + c < k) gptr(d_gate)[t * k + c0 + c] = on[c] ? sum[c] : 0.0f;
+        }
       }
     }
-  }
 }
 
 // ---- host -------------------------------------------------------------------------------------------
@@ -326,14 +320,14 @@ template <class X>
 void dispatch(const scadles_order* o, const void* x, uint64_t ld_x, void* rows, uint64_t ld_rows, hipStream_t st)
 {
   const Move m = make_move(o, Piece<X>::N, 1);
-  k_dispatch<X><<<(uint32_t)div_up(o->tokens, m.share.rows), kBlock, 0, st>>>(m, o->k, (const X*)x, ld_x, (X*)rows, ld_rows);
+  k_dispatch<X><<<grid_of(div_up(o->tokens, m.share.rows)), kBlock, 0, st>>>(m, o->k, (const X*)x, ld_x, (X*)rows, ld_rows);
 }
 
 template <class X, int C>
 void combine_of(const scadles_order* o, const void* rows, uint64_t ld_rows, const float* gate, void* out, uint64_t ld_out, hipStream_t st)
 {
   const Move m = make_move(o, Piece<X>::N, 4);
-  const uint32_t W = (uint32_t)div_up(o->tokens, m.share.rows);
+  const uint32_t W = grid_of(div_up(o->tokens, m.share.rows));
   if (gate) k_combine<X, C, true><<<W, kBlock, 0, st>>>(m, o->k, (const X*)rows, ld_rows, gate, (X*)out, ld_out);
   else k_combine<X, C, false><<<W, kBlock, 0, st>>>(m, o->k, (const X*)rows, ld_rows, gate, (X*)out, ld_out);
 }
@@ -353,7 +347,7 @@ void combine_back_of(const scadles_order* o, const void* d_out, uint64_t ld_d_ou
 {
   const Move m = make_move(o, Piece<X>::N, 4);
   auto go = [&](auto kernel, uint32_t G) {
-    kernel<<<(uint32_t)div_up(o->tokens, kBlock / G), kBlock, 0, st>>>(m, o->k, (const X*)d_out, ld_d_out, (const X*)rows, ld_rows, gate,
+    kernel<<<grid_of(div_up(o->tokens, kBlock / G)), kBlock, 0, st>>>(m, o->k, (const X*)d_out, ld_d_out, (const X*)rows, ld_rows, gate,
                                                                        (X*)d_rows, ld_d_rows, d_gate);
   };
   if (m.share.pieces <= 8) go(k_combine_back<X, C, 8>, 8);

@@ -111,6 +111,10 @@ inline Share share_rows(uint64_t rows, uint64_t pieces, uint64_t most = 1)
   return {(uint32_t)pieces, (uint32_t)n, (uint32_t)(n == 1 ? 0 : div_up(1ull << 32, pieces))};
 }
 
+// A launch has fewer than 2^32 lanes: workgroups beyond these take their turn.
+constexpr uint64_t kMostBlocks = 1u << 22;
+inline uint32_t grid_of(uint64_t blocks) { return (uint32_t)(blocks < kMostBlocks ? blocks : kMostBlocks); }
+
 // Calls f(row of the workgroup, piece) for every place of this lane.
 template <class F>
 __device__ inline void for_pieces(const Share& s, F f)
@@ -119,6 +123,16 @@ __device__ inline void for_pieces(const Share& s, F f)
     const uint32_t r = s.rows == 1 ? 0u : s.pieces == 1 ? i : __umulhi(i, s.magic);
     f(r, i - r * s.pieces);
   }
+}
+
+// The same for all `rows` rows, f(row, piece): workgroup after workgroup of them.
+template <class F>
+__device__ inline void for_all_pieces(const Share& s, uint64_t rows, F f)
+{
+  for (uint64_t r0 = (uint64_t)blockIdx.x * s.rows; r0 < rows; r0 += (uint64_t)gridDim.x * s.rows)
+    for_pieces(s, [&](uint32_t r, uint32_t g) {
+      if (r0 + r < rows) f(r0 + r, g);
+    });
 }
 
 // Bytes from the first to the last element of `rows` rows.
