@@ -13,7 +13,6 @@
 // The rows without a token are set to zero by further workgroups of the same
 // launch, which search the sorted tokens for their ids. So every element of a
 // gradient is written once, and nothing depends on the order of workgroups.
-#include <algorithm>
 #include <cstring>
 
 #include "pieces.h"
@@ -29,6 +28,7 @@ constexpr uint32_t kSortOne = 4 * kSortBlock; // tokens of a sort in one launch
 constexpr uint32_t kFillIds = 256;            // ids of a workgroup that writes zeros, at most
 constexpr uint32_t kNone = ~0u;
 constexpr int kJoinBlock = 1024;
+constexpr uint32_t kJoins = 1u << 21;         // workgroups of a launch that joins
 
 // Where ids come from: the caller's tokens, or an earlier pass.
 struct Ids {
@@ -278,10 +278,11 @@ __global__ __launch_bounds__(kBlock) void k_embed_sum(Grads g, Sums m, const uin
 // The cells that begin in a chunk of sorted tokens and go on behind it. The workgroup's
 // lanes share the columns, and the chunks of a long cell in slices.
 template <class X, class W, bool kAdd>
-__device__ inline void join_cell(const Grads& g, const Sums& m, uint32_t block, const uint32_t* cell, const float* part, uint32_t width,
-                                 typename Piece<X>::F* slice)
+__global__ __launch_bounds__(kJoinBlock) void k_embed_join(Grads g, Sums m, uint32_t block, const uint32_t* cell, const float* part, uint32_t width)
 {
   typedef typename Piece<X>::F F;
+  __shared__ F slice[kJoinBlock];
+  block += blockIdx.x;
   const uint32_t column = block % m.columns, chunk = block / m.columns;
   const uint32_t first = (chunk + 1) * kRun;             // of the next chunk; the last chunk has no workgroup here
   const uint32_t now = gptr(cell)[first];
@@ -314,16 +315,6 @@ __device__ inline void join_cell(const Grads& g, const Sums& m, uint32_t block, 
   for (uint32_t q = 1; q < slices; ++q) sum += slice[q * m.lanes + lane];
   const uint32_t d = now / g.vocab;
   write_grad<X>((W*)g.w[d] + (uint64_t)(now - d * g.vocab) * g.dim + at, g.dim - at, sum * g.scale, kAdd);
-}
-
-template <class X, class W, bool kAdd>
-__global__ __launch_bounds__(kJoinBlock) void k_embed_join(Grads g, Sums m, const uint32_t* cell, const float* part, uint32_t width)
-{
-  __shared__ typename Piece<X>::F slice[kJoinBlock];
-  for (uint32_t b = blockIdx.x; b < (m.chunks - 1) * m.columns; b += gridDim.x) {
-    join_cell<X, W, kAdd>(g, m, b, cell, part, width, slice);
-    __syncthreads();
-  }
 }
 
 // ---- host -------------------------------------------------------------------------------------------------
@@ -455,10 +446,11 @@ hipError_t sums(const Grads& g, uint64_t n, const Space& s, const void* d_out, u
     if (accumulate) k_embed_sum<X, W, true><<<blocks, kBlock, 0, st>>>(g, m, s.cell, s.src, (const X*)d_out, ld, s.part, width);
     else k_embed_sum<X, W, false><<<blocks, kBlock, 0, st>>>(g, m, s.cell, s.src, (const X*)d_out, ld, s.part, width);
   }
-  if (m.chunks > 1) {
-    const uint32_t blocks = (uint32_t)std::min<uint64_t>((uint64_t)(m.chunks - 1) * m.columns, kMostBlocks / 2);
-    if (accumulate) k_embed_join<X, W, true><<<blocks, kJoinBlock, 0, st>>>(g, m, s.cell, s.part, width);
-    else k_embed_join<X, W, false><<<blocks, kJoinBlock, 0, st>>>(g, m, s.cell, s.part, width);
+  const uint64_t joins = (uint64_t)(m.chunks ? m.chunks - 1 : 0) * m.columns;
+  for (uint64_t at = 0; at < joins; at += kJoins) {
+    const uint32_t blocks = (uint32_t)(joins - at < kJoins ? joins - at : kJoins), b = (uint32_t)at;
+    if (accumulate) k_embed_join<X, W, true><<<blocks, kJoinBlock, 0, st>>>(g, m, b, s.cell, s.part, width);
+    else k_embed_join<X, W, false><<<blocks, kJoinBlock, 0, st>>>(g, m, b, s.cell, s.part, width);
   }
   return hipGetLastError();
 }
