@@ -163,7 +163,7 @@ __global__ __launch_bounds__(kBlock) void k_align(const uint16_t* x, uint64_t ld
   for (uint64_t i = (uint64_t)blockIdx.x * kBlock + threadIdx.x; i < rows * per; i += (uint64_t)gridDim.x * kBlock) {
     const uint64_t r = i / per;
     const uint32_t at = (uint32_t)(i - r * per) * 8;
-    *(GLOBAL u4*)gptr(out + r * stride + at) = load_piece(x + r * ld + at, at < dim ? dim - at : 0);
+    *(GLOBAL u4*)gptr(out + r * stride + at) = at < dim ? load_piece(x + r * ld, at, dim) : u4{0, 0, 0, 0};
   }
 }
 
@@ -196,7 +196,8 @@ __global__ __launch_bounds__(kBlock) void k_column_top(Tokens a, const X* x, uin
 #pragma unroll 8
     for (uint32_t r = w; r < top_rows(kTokens); r += kWaves) {
       const int64_t from = row_at<kTokens>(a, blockIdx.x * top_rows(kTokens) + r, rows);
-      const auto f = unpack<X>(load_piece(x + (from < 0 ? 0 : from) * ld + at, from < 0 ? 0 : dim - at));
+      const u4 v = load_piece(x + (from < 0 ? 0 : from) * ld, at, dim);
+      const auto f = unpack<X>(from < 0 ? u4{0, 0, 0, 0} : v);
 #pragma unroll
       for (uint32_t e = 0; e < N; ++e) most[e] = max(most[e], finite_bits(f[e]));
     }
@@ -225,8 +226,9 @@ __global__ __launch_bounds__(kBlock) void k_turn(Tokens a, const X* x, uint64_t 
     const int64_t from = row_at<kTokens>(a, r0 + r, rows);
 #pragma unroll
     for (uint32_t q = 0; q < 16; q += Piece<X>::N) {
-      const uint32_t at = c0 + c + q, k = from >= 0 && at < dim ? dim - at : 0;
-      const auto f = unpack<X>(load_piece(x + (from >= 0 ? from : 0) * ld + at, k));
+      const uint32_t at = c0 + c + q;
+      const u4 v = load_raw(x + (from >= 0 ? from : 0) * ld, at, dim);
+      const auto f = unpack<X>(from >= 0 && at < dim ? settled<X>(v, at, dim) : u4{0, 0, 0, 0});
 #pragma unroll
       for (uint32_t e = 0; e < Piece<X>::N; ++e) tile[r][c + q + e] = f[e];
     }

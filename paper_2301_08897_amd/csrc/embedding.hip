@@ -65,15 +65,19 @@ __device__ inline uint32_t cell_of(const Grads& g, uint32_t id, uint32_t t)
 
 // ---- forward ------------------------------------------------------------------------------------
 
-template <class X>
+// kWhole: rows are whole pieces, and nothing is decided for the last one (131072 x 1024 bfloat16: 88
+// us, else 96).
+template <class X, bool kWhole>
 __global__ __launch_bounds__(kBlock) void k_embed(Ids a, uint64_t tokens, Share share, uint32_t dim, float scale, const X* weight,
                                                   uint64_t ld_w, X* out, uint64_t ld_out)
 {
   for_all_pieces(share, tokens, [&](uint64_t t, uint32_t g) {
-    const uint32_t at = g * Piece<X>::N, left = dim - at, id = token_id(a, t);
+    constexpr uint32_t N = Piece<X>::N;
+    const uint32_t at = g * N, id = token_id(a, t);
+    const X* row = weight + (uint64_t)id * ld_w;
     u4 v = {0, 0, 0, 0};
-    if (id < a.vocab) v = pack<X>(unpack<X>(load_piece(weight + (uint64_t)id * ld_w + at, left)) * scale);
-    store_piece(out + t * ld_out + at, v, left);
+    if (id < a.vocab) v = pack<X>(unpack<X>(kWhole ? load_piece(row + at, 0, N) : load_piece(row, at, dim)) * scale);
+    store_piece(out + t * ld_out + at, v, kWhole ? N : dim - at);
   });
 }
 
@@ -258,7 +262,8 @@ __global__ __launch_bounds__(kBlock) void k_embed_sum(Grads g, Sums m, const uin
 #pragma unroll
     for (uint32_t q = 0; q < 8; ++q) {
       c[q] = i + q < i1 ? gptr(cell)[i + q] : kNone;
-      if (c[q] != kNone) v[q] = load_piece(d_out + (uint64_t)gptr(src)[i + q] * ld + at, left);
+      // padding's rows are read too, so that no load waits for another's branch
+      v[q] = load_raw(d_out + (uint64_t)(i + q < i1 ? gptr(src)[i + q] : 0) * ld, at, g.dim);
     }
 #pragma unroll
     for (uint32_t q = 0; q < 8; ++q) {
@@ -269,7 +274,7 @@ __global__ __launch_bounds__(kBlock) void k_embed_sum(Grads g, Sums m, const uin
         before = false;
         sum = F{};
       }
-      if (c[q] != kNone) sum += unpack<X>(v[q]);
+      if (c[q] != kNone) sum += unpack<X>(settled<X>(v[q], at, g.dim));
     }
   }
   done(i1 < m.n && gptr(cell)[i1] == now);
@@ -381,8 +386,11 @@ hipError_t forward(const scadles_embedding* e, uint64_t tokens, const void* ids,
 {
   const Ids a = {ids, nullptr, nullptr, e->token_bytes == 8, (uint32_t)e->vocab};
   const Share share = share_rows(tokens, div_up(e->dim, Piece<X>::N));
-  k_embed<X><<<grid_of(div_up(tokens, share.rows)), kBlock, 0, st>>>(a, tokens, share, e->dim, e->scale, (const X*)weight, ld_w, (X*)out,
-                                                                      ld_out);
+  auto go = [&](auto kernel) {
+    kernel<<<grid_of(div_up(tokens, share.rows)), kBlock, 0, st>>>(a, tokens, share, e->dim, e->scale, (const X*)weight, ld_w, (X*)out, ld_out);
+  };
+  if (e->dim % Piece<X>::N) go(k_embed<X, false>);
+  else go(k_embed<X, true>);
   return hipGetLastError();
 }
 
@@ -429,9 +437,11 @@ hipError_t sums(const Grads& g, uint64_t n, const Space& s, const void* d_out, u
   m.sums = (uint32_t)div_up(m.chunks, kBlock / m.lanes) * m.columns;
   uint64_t fills = 0;
   if (!accumulate) {
-    // about 64 KiB of rows to a workgroup
+    // 64 KiB of rows to a workgroup, and 8 KiB for a few tokens, whose search is short: those under
+    // way then write next to each other (65536 x 1024 floats, 100 tokens: 61 us a call; 64 KiB: 76. Four
+    // tables of 50001 x 515 floats, 8190 tokens: 91 us, 16 KiB: 99, 8 KiB: 148)
     const uint64_t row = (uint64_t)g.dim * sizeof(W);
-    uint64_t per = (64u << 10) / row;
+    uint64_t per = (n <= 4096 ? 8u << 10 : 64u << 10) / row;
     per = per < 1 ? 1 : per > kFillIds ? kFillIds : per;
     if (per > g.vocab) per = g.vocab;
     m.per = (uint32_t)per;

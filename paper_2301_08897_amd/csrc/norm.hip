@@ -156,8 +156,12 @@ __global__ __launch_bounds__(kBlock) void k_norm(Norm m, const X* x, uint64_t ld
 #pragma unroll
     for (int j = 0; j < P; ++j) {
       const uint32_t at = (lane + j * G) * N;
-      next[j] = t < m.tokens && at < m.dim ? load_piece(x + t * ld_x + at, m.dim - at) : u4{0, 0, 0, 0};
+      next[j] = t < m.tokens && at < m.dim ? load_raw(x + t * ld_x, at, m.dim) : u4{0, 0, 0, 0};
     }
+  };
+  auto row_piece = [&](u4 v, int j) {
+    const uint32_t at = (lane + j * G) * N;
+    return at < m.dim ? settled<X>(v, at, m.dim) : v;
   };
   uint64_t t = (uint64_t)blockIdx.x * groups + threadIdx.x / G;
   load(t);
@@ -166,7 +170,7 @@ __global__ __launch_bounds__(kBlock) void k_norm(Norm m, const X* x, uint64_t ld
     float sum = 0.0f;
 #pragma unroll
     for (int j = 0; j < P; ++j) {
-      v[j] = unpack<X>(next[j]);
+      v[j] = unpack<X>(row_piece(next[j], j));
       sum += sum_of(v[j], N);
     }
     load(t + step);                // under this row's sums
@@ -204,10 +208,10 @@ __global__ __launch_bounds__(kBlock) void k_norm_long(Norm m, const X* x, uint64
   const uint64_t t = blockIdx.x;     // fewer than 2^24 rows this long fit in memory
   const X* row = x + t * ld_x;
   float sum = 0.0f, square = 0.0f;
-  for (uint32_t at = threadIdx.x * N; at < m.dim; at += kBlock * N) sum += sum_of(unpack<X>(load_piece(row + at, m.dim - at)), N);
+  for (uint32_t at = threadIdx.x * N; at < m.dim; at += kBlock * N) sum += sum_of(unpack<X>(load_piece(row, at, m.dim)), N);
   const float mean = group_total<kBlock>(sum, lds[0]) * m.inverse;
   for (uint32_t at = threadIdx.x * N; at < m.dim; at += kBlock * N) {
-    const auto v = unpack<X>(load_piece(row + at, m.dim - at));
+    const auto v = unpack<X>(load_piece(row, at, m.dim));
 #pragma unroll
     for (uint32_t q = 0; q < N; ++q) {
       const float c = v[q] - mean;
@@ -217,7 +221,7 @@ __global__ __launch_bounds__(kBlock) void k_norm_long(Norm m, const X* x, uint64
   const float rstd = 1.0f / __builtin_sqrtf(group_total<kBlock>(square, lds[1]) * m.inverse + m.eps);
   for (uint32_t at = threadIdx.x * N; at < m.dim; at += kBlock * N) {
     const uint32_t left = m.dim - at;
-    auto v = (unpack<X>(load_piece(row + at, left)) - mean) * rstd * weights_at<X>(m.weight, m.wide, at, left);
+    auto v = (unpack<X>(load_piece(row, at, m.dim)) - mean) * rstd * weights_at<X>(m.weight, m.wide, at, left);
     if (m.bias) v += weights_at<X>(m.bias, m.wide, at, left);
     store_piece(y + t * ld_y + at, pack<X>(v), left);
   }
@@ -273,13 +277,17 @@ __global__ __launch_bounds__(kBlock) void k_norm_back(Norm m, Split s, Sums o, c
     for (int j = 0; j < P; ++j) {
       const uint32_t at = (lane + j * G) * N;
       const bool on = there && at < m.dim;
-      next_x[j] = on ? load_piece(x + t * ld_x + at, m.dim - at) : u4{0, 0, 0, 0};
-      next_g[j] = on ? load_piece(dy + t * ld_dy + at, m.dim - at) : u4{0, 0, 0, 0};
+      next_x[j] = on ? load_raw(x + t * ld_x, at, m.dim) : u4{0, 0, 0, 0};
+      next_g[j] = on ? load_raw(dy + t * ld_dy, at, m.dim) : u4{0, 0, 0, 0};
     }
     if (there) {
       next_mean = gptr(mean_in)[t];
       next_rstd = gptr(rstd_in)[t];
     }
+  };
+  auto row_piece = [&](u4 v, int j) {
+    const uint32_t at = (lane + j * G) * N;
+    return at < m.dim ? settled<X>(v, at, m.dim) : v;
   };
   load(t0);
   for (uint64_t t = t0; t < t1; t += step) {
@@ -288,8 +296,8 @@ __global__ __launch_bounds__(kBlock) void k_norm_back(Norm m, Split s, Sums o, c
     float a = 0.0f, b = 0.0f;
 #pragma unroll
     for (int j = 0; j < P; ++j) {
-      h[j] = unpack<X>(next_x[j]);
-      g[j] = unpack<X>(next_g[j]);
+      h[j] = unpack<X>(row_piece(next_x[j], j));
+      g[j] = unpack<X>(row_piece(next_g[j], j));
     }
     load(t + step);                // under this row's sums
 #pragma unroll
@@ -346,8 +354,8 @@ __global__ __launch_bounds__(kBlock) void k_norm_back_long(Norm m, const X* x, u
   float a = 0.0f, b = 0.0f;
   auto both = [&](uint32_t at, auto& h, auto& g) {
     const uint32_t left = m.dim - at;
-    h = (unpack<X>(load_piece(x + t * ld_x + at, left)) - mean) * rstd;
-    g = unpack<X>(load_piece(dy + t * ld_dy + at, left)) * weights_at<X>(m.weight, m.wide, at, left);
+    h = (unpack<X>(load_piece(x + t * ld_x, at, m.dim)) - mean) * rstd;
+    g = unpack<X>(load_piece(dy + t * ld_dy, at, m.dim)) * weights_at<X>(m.weight, m.wide, at, left);
   };
   typename Piece<X>::F h, g;
   for (uint32_t at = threadIdx.x * N; at < m.dim; at += kBlock * N) {
@@ -377,8 +385,8 @@ __global__ __launch_bounds__(kBlock) void k_norm_columns(Norm m, Split s, Sums o
   F sw = {}, sb = {};
 #pragma unroll 4
   for (uint64_t t = t0; t < s.off[d + 1]; t += step) {
-    const F g = unpack<X>(load_piece(dy + t * ld_dy + at, left));
-    sw += g * ((unpack<X>(load_piece(x + t * ld_x + at, left)) - gptr(mean_in)[t]) * gptr(rstd_in)[t]);
+    const F g = unpack<X>(load_piece(dy + t * ld_dy, at, m.dim));
+    sw += g * ((unpack<X>(load_piece(x + t * ld_x, at, m.dim)) - gptr(mean_in)[t]) * gptr(rstd_in)[t]);
     sb += g;
   }
   for (uint32_t which = 0; which < 2; ++which) {

@@ -30,34 +30,61 @@ struct Piece<uint16_t> {     // bfloat16
   typedef u4at2 Any;
 };
 
-// The first k elements (all of them if there are N or more) at p; the rest read as zero.
+// 16 bytes of a row of dim elements from element `at` on, as `settled` makes them: the row's last,
+// incomplete piece is read as the 16 bytes that end with the row, which is one load for all
+// lanes and no wait (single elements are waited for one row at a time). `at` may lie behind the row.
 template <class X>
-__device__ inline u4 load_piece(const X* p, uint32_t k)
+__device__ inline u4 load_raw(const X* row, uint32_t at, uint32_t dim)
 {
-  if (k >= Piece<X>::N) return *(const GLOBAL typename Piece<X>::Any*)gptr(p);
+  constexpr uint32_t N = Piece<X>::N;
+  if (dim >= N) return *(const GLOBAL typename Piece<X>::Any*)gptr(row + (at < dim - N ? at : dim - N));
   u4 x = {0, 0, 0, 0};
 #pragma unroll
-  for (uint32_t q = 0; q < Piece<X>::N - 1; ++q)
-    if (q < k) {
-      if constexpr (sizeof(X) == 4) x[q] = __float_as_uint(gptr(p)[q]);
-      else x[q / 2] |= (uint32_t)gptr(p)[q] << (q % 2 * 16);
+  for (uint32_t q = 0; q < N - 1; ++q)
+    if (q < dim) {
+      if constexpr (sizeof(X) == 4) x[q] = __float_as_uint(gptr(row)[q]);
+      else x[q / 2] |= (uint32_t)gptr(row)[q] << (q % 2 * 16);
     }
   return x;
 }
 
+// The elements from `at` < dim on; those behind the row are zero.
+template <class X>
+__device__ inline u4 settled(u4 x, uint32_t at, uint32_t dim)
+{
+  constexpr uint32_t N = Piece<X>::N;
+  if (dim % N == 0 || dim < N) return x;
+  const uint32_t extra = at + N > dim ? (at + N - dim) * (uint32_t)sizeof(X) * 8 : 0;      // bits in front
+  const uint64_t lo = x[0] | (uint64_t)x[1] << 32, hi = x[2] | (uint64_t)x[3] << 32;
+  const uint64_t low = extra == 0 ? lo : extra < 64 ? lo >> extra | hi << (64 - extra) : hi >> (extra & 63), high = extra < 64 ? hi >> extra : 0;
+  return u4{(uint32_t)low, (uint32_t)(low >> 32), (uint32_t)high, (uint32_t)(high >> 32)};
+}
+
+template <class X>
+__device__ inline u4 load_piece(const X* row, uint32_t at, uint32_t dim)
+{
+  return settled<X>(load_raw(row, at, dim), at, dim);
+}
+
+// The first k elements (all of them if there are N or more) to p.
 template <class X>
 __device__ inline void store_piece(X* p, u4 x, uint32_t k)
 {
+  typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+  typedef u2 u2any __attribute__((aligned(2)));
+  typedef uint32_t u1any __attribute__((aligned(2)));
   if (k >= Piece<X>::N) {
     *(GLOBAL typename Piece<X>::Any*)gptr(p) = x;
     return;
   }
-#pragma unroll
-  for (uint32_t q = 0; q < Piece<X>::N - 1; ++q)
-    if (q < k) {
-      if constexpr (sizeof(X) == 4) gptr(p)[q] = __uint_as_float(x[q]);
-      else gptr(p)[q] = (uint16_t)(x[q / 2] >> (q % 2 * 16));
-    }
+  uint32_t at = k & (8 / sizeof(X));             // the elements stored so far
+  if (at) *(GLOBAL u2any*)gptr(p) = u2{x[0], x[1]};
+  const uint32_t a = at ? x[2] : x[0], b = at ? x[3] : x[1];
+  const bool one = k & (4 / sizeof(X));
+  if (one) *(GLOBAL u1any*)gptr(p + at) = a;
+  if constexpr (sizeof(X) == 2) {
+    if (k & 1) gptr(p)[k - 1] = (uint16_t)(one ? b : a);
+  }
 }
 
 // The same for data that is not read again soon.
@@ -100,13 +127,10 @@ struct Share {
   uint32_t pieces, rows, magic;
 };
 
-inline Share share_rows(uint64_t rows, uint64_t pieces, uint64_t most = 1)
+// A piece for every lane of a workgroup.
+inline Share share_rows(uint64_t rows, uint64_t pieces)
 {
-  // a piece for every lane of a workgroup, or up to `most` where there are far more than
-  // the GPU's lanes
-  uint64_t each = rows * pieces / ((uint64_t)kBlock * 4096);
-  each = each < 1 ? 1 : each > most ? most : each;
-  uint64_t n = pieces > 1024 ? 1 : div_up(kBlock * each, pieces);
+  uint64_t n = pieces > 1024 ? 1 : div_up(kBlock, pieces);
   if (n > rows) n = rows ? rows : 1;
   return {(uint32_t)pieces, (uint32_t)n, (uint32_t)(n == 1 ? 0 : div_up(1ull << 32, pieces))};
 }
