@@ -198,7 +198,8 @@ __global__ __launch_bounds__(kBlock) void k_combine(Move m, uint32_t k, const X*
 
 // A group of G lanes has a token: its pieces of d_out are multiplied with the same of
 // every choice's row and scaled into d_rows; the products are added over the lanes
-// at the end. d_rows may be the rows: a piece is read before it is written, by the same lane.
+// at the end. d_rows may be the rows: a piece is read before it is written, by the same lane
+// (what the load of a row's last piece sees of the one before is dropped).
 template <class X, int C, int G>
 __global__ __launch_bounds__(kBlock) void k_combine_back(Move m, uint32_t k, const X* d_out, uint64_t ld_d_out, const X* rows,
                                                          uint64_t ld_rows, const float* gate, X* d_rows, uint64_t ld_d_rows, float* d_gate)
