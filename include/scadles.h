@@ -696,12 +696,15 @@ scadles_status scadles_layer_norm_backward(const scadles_norm* norm, const scadl
  * computes the logits again, a piece of the vocabulary at a time:
  *   G = weights[d] * share[d] * d_loss * (softmax(z) - onehot(target)),
  *   d_x = G weight, d_weight[d] = G^T x over device d's rows.
- * Products are those of the matrix cores, with sums in float. bfloat16 x and
- * weight are multiplied as they are, and G is rounded to bfloat16 where all gradients
- * are bfloat16. Else numbers are taken as sums of two half floats (22 bits), after
- * a power of two has brought the largest of their row (for the logits) or column
- * (for the gradients) to 2^13 .. 2^14, so that they are off by 2^-22 of their size or
- * 2^-38 of that largest one; G alike, by 2^-22 of its size or 2^-38. Elements that are
+ * Products are those of the matrix cores, with sums in float. Logits: bfloat16 x and
+ * weight are multiplied as they are; floats are taken as sums of two half floats (22
+ * bits), after a power of two has brought the largest of their row to 2^13 .. 2^14, so
+ * that they are off by 2^-22 of their size or 2^-38 of that largest one. Gradients: a
+ * product of G with an element of x or weight is off by 2^-21 of its own size, at any
+ * magnitude above 2^-126, if it goes into a float, by 2^-14 if it goes into a bfloat16;
+ * G is rounded to bfloat16 (2^-8) where x, weight and all gradients are, so that float
+ * gradients are what asks for more. No row or device has a part in the precision of
+ * another's, and an entry masked with finite values is like none. Elements that are
  * not finite make what they go into NaN (infinities of bfloat16 x and weight as
  * in exact arithmetic in the forward pass).
  *   vocab         1 <= vocab <= 2^22; tokens <= 2^22.

@@ -13,12 +13,15 @@
 // index adjacent, so that k_turn writes both transposed once per call.
 //
 // Types. bfloat16 x and weight are multiplied where they lie; G is rounded to bfloat16 for
-// bfloat16 gradients. For the rest, numbers are sums of two half floats (22 bits), scaled by
-// powers of two: x and weight by row for the logits, by column for the gradients,
-// where the largest of a row or column comes to 2^13 .. 2^14; G by 2^13. Three
-// products of such parts, the fourth being below 2^-22 of the first, have the precision of
-// sums in float: six products of three bfloat16 parts have it too, and took twice
-// as long.
+// bfloat16 gradients. The logits of floats: x and weight are sums of two half floats (22
+// bits), scaled by powers of two by row, where the largest of a row comes to 2^13 .. 2^14.
+// Three products of such parts, the fourth being below 2^-22 of the first, have the precision of
+// sums in float, and what a row lacks is small beside its own largest.
+// The gradients' products contract over rows, so that a scale would have to be common to rows that
+// have nothing to do with each other: a masked entry's and the others', one device's tokens and
+// another's. Their operands, and G, are three bfloat16 parts instead: all 24 bits of a float, at
+// any magnitude (a probability of 1e-30 has as many as one of 1e-1), and six products, twice the three
+// of half floats. The products are as many as the result's type asks for (x_pairs, w_pairs).
 //
 // Tokens are counted with every device's first one at a multiple of 64 (Tokens::place), so
 // that a step of the product over tokens belongs to one device. A token that is
@@ -46,10 +49,7 @@ constexpr uint32_t kLeastPiece = 2048;            // vocabulary entries of a pie
 constexpr uint32_t kNone = ~0u;
 constexpr uint32_t kMost = 1u << 22;              // tokens and vocabulary entries: 32-bit offsets within a tile
 constexpr uint32_t kLeastSteps = 16;              // of a unit of a split sum, as long as its start and its store
-// rows that a workgroup looks for a column's largest in: fewer of tokens, of which there are few,
-// and which take two loads more to find
-constexpr uint32_t top_rows(bool tokens) { return tokens ? 32 : 256; }
-constexpr int kGBits = 13;                        // G in half floats is scaled by 2^13
+constexpr int kParts = 3;                         // bfloat16 parts of a float
 constexpr int kRowsBlock = 1024;
 constexpr uint32_t kRowSlices = kRowsBlock / 64;
 
@@ -126,6 +126,18 @@ __device__ inline uint16_t half_part(float& x)
   return bits_of(h);
 }
 
+// The first part of x in bfloat16, which becomes the rest. A float beyond the largest bfloat16
+// is not rounded to infinity; what is not finite has no rest.
+__device__ inline uint16_t bf16_part(float& x)
+{
+  const uint32_t b = __float_as_uint(x);
+  const bool beyond = (b & 0x7FFFFFFFu) - 0x7F7F8000u < 0x8000u;
+  const __bf16 h = (__bf16)__uint_as_float(beyond ? b & 0xFFFF0000u : b);
+  const float rest = x - (float)h;
+  x = rest - rest == 0.0f ? rest : 0.0f;
+  return bits_of(h);
+}
+
 // Rows of floats to rows of two planes, zeros behind dim, and the rows' powers of two: a wave
 // has a row.
 __global__ __launch_bounds__(kBlock) void k_planes(const float* x, uint64_t ld, uint32_t rows, uint32_t dim, uint32_t width, uint64_t stride,
@@ -172,12 +184,6 @@ __global__ __launch_bounds__(kBlock) void k_align(const uint16_t* x, uint64_t ld
   }
 }
 
-__global__ void k_clear(uint32_t* p, uint32_t n)
-{
-  const uint32_t i = blockIdx.x * blockDim.x + threadIdx.x;
-  if (i < n) gptr(p)[i] = 0;
-}
-
 // The row of x that is row r of the transposed operand: a table's own row, or the token in
 // a place if it is counted; -1 for zeros.
 template <bool kTokens>
@@ -188,42 +194,12 @@ __device__ inline int64_t row_at(const Tokens& a, uint32_t r, uint32_t rows)
   return t >= 0 && target_of(a, t) != kNone ? t : -1;
 }
 
-// The largest magnitude of every column, as bits, over some rows at a time (a maximum does
-// not depend on the order).
+// Rows of X transposed to planes of bfloat16 [dim][stride], 64 x 64 at a time: kParts of floats.
 template <class X, bool kTokens>
-__global__ __launch_bounds__(kBlock) void k_column_top(Tokens a, const X* x, uint64_t ld, uint32_t rows, uint32_t dim, uint32_t* top)
+__global__ __launch_bounds__(kBlock) void k_turn(Tokens a, const X* x, uint64_t ld, uint32_t rows, uint32_t dim, uint64_t stride, uint16_t* out,
+                                                 uint64_t plane)
 {
-  constexpr uint32_t N = Piece<X>::N;
-  __shared__ uint32_t each[kWaves][64 * N];
-  const uint32_t lane = threadIdx.x % 64, w = threadIdx.x / 64, at = (blockIdx.y * 64 + lane) * N;
-  uint32_t most[N] = {};
-  if (at < dim) {
-#pragma unroll 8
-    for (uint32_t r = w; r < top_rows(kTokens); r += kWaves) {
-      const int64_t from = row_at<kTokens>(a, blockIdx.x * top_rows(kTokens) + r, rows);
-      const u4 v = load_piece(x + (from < 0 ? 0 : from) * ld, at, dim);
-      const auto f = unpack<X>(from < 0 ? u4{0, 0, 0, 0} : v);
-#pragma unroll
-      for (uint32_t e = 0; e < N; ++e) most[e] = max(most[e], finite_bits(f[e]));
-    }
-  }
-#pragma unroll
-  for (uint32_t e = 0; e < N; ++e) each[w][lane * N + e] = most[e];
-  __syncthreads();
-  for (uint32_t c = threadIdx.x; c < 64 * N && blockIdx.y * 64 * N + c < dim; c += kBlock) {
-    uint32_t t = 0;
-#pragma unroll
-    for (int q = 0; q < kWaves; ++q) t = max(t, each[q][c]);
-    if (t) atomicMax(top + blockIdx.y * 64 * N + c, t);
-  }
-}
-
-// Rows of X transposed to planes [dim][stride], 64 x 64 at a time; half floats are scaled by
-// the columns' largest magnitudes.
-template <class X, bool kTokens, class E, int kPlanes>
-__global__ __launch_bounds__(kBlock) void k_turn(Tokens a, const X* x, uint64_t ld, uint32_t rows, uint32_t dim, const uint32_t* top, uint64_t stride,
-                                                 uint16_t* out, uint64_t plane)
-{
+  constexpr int kPlanes = sizeof(X) == 4 ? kParts : 1;
   __shared__ float tile[64][65];
   const uint32_t r0 = blockIdx.x * 64, c0 = blockIdx.y * 64;
   {
@@ -242,17 +218,14 @@ __global__ __launch_bounds__(kBlock) void k_turn(Tokens a, const X* x, uint64_t 
   const uint32_t c = threadIdx.x / 4, r = threadIdx.x % 4 * 16;
   if (c0 + c >= dim) return;
   uint32_t w[kPlanes][8];
-  const int s = std::is_same<E, F16>::value ? scale_of(gptr(top)[c0 + c]) : 0;
 #pragma unroll
   for (int q = 0; q < 8; ++q) {
     float lo = tile[r + 2 * q][c], hi = tile[r + 2 * q + 1][c];
-    if constexpr (std::is_same<E, F16>::value) {
-      lo = ldexpf(lo, s);
-      hi = ldexpf(hi, s);
+    if constexpr (kPlanes > 1) {
 #pragma unroll
       for (int n = 0; n < kPlanes; ++n) {
-        const uint32_t first = half_part(lo);
-        w[n][q] = first | (uint32_t)half_part(hi) << 16;
+        const uint32_t first = bf16_part(lo);
+        w[n][q] = first | (uint32_t)bf16_part(hi) << 16;
       }
     } else {
       w[0][q] = bits_of((__bf16)lo) | (uint32_t)bits_of((__bf16)hi) << 16;
@@ -302,11 +275,11 @@ __device__ inline float exp_of(float x)
   else return __builtin_amdgcn_exp2f(x * 1.44269504088896340736f);
 }
 
-// E: of x and weight. kOut: planes of G, one of bfloat16 or two of half floats.
+// E: of x and weight. kOut: planes of G, one bfloat16 or its kParts.
 template <bool kBack, class E, int kOut>
 __global__ __launch_bounds__(kProductBlock, 2) void k_logits(Tokens a, Logits q)
 {
-  constexpr bool kHalf = std::is_same<E, F16>::value, kExact = kHalf || kOut == 2;
+  constexpr bool kHalf = std::is_same<E, F16>::value, kExact = kHalf || kOut > 1;
   __shared__ __attribute__((aligned(128))) char lds[kProductLds];
   Pipe pipe(lds);
   const uint32_t tiles = q.rows * q.columns;
@@ -441,12 +414,6 @@ __global__ __launch_bounds__(kProductBlock, 2) void k_logits(Tokens a, Logits q)
         uint16_t* gt = q.gt + (uint64_t)(m - q.v0) * q.gt_stride + n;
 #pragma unroll
         for (int i = 0; i < 8; i += 2) {
-          if constexpr (kOut == 2) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-              for (int e = 0; e < 8; ++e) acc[i + e / 4][j][e % 4] *= (float)(1 << kGBits);
-          }
 #pragma unroll
           for (int pl = 0; pl < kOut; ++pl) {
             uint16_t h[4][8];
@@ -455,9 +422,9 @@ __global__ __launch_bounds__(kProductBlock, 2) void k_logits(Tokens a, Logits q)
               u4 x;
 #pragma unroll
               for (int e = 0; e < 8; ++e) {
-                float rest = acc[i + e / 4][j][e % 4];
-                h[j][e] = kOut == 2 ? half_part(rest) : bits_of((__bf16)rest);
-                acc[i + e / 4][j][e % 4] = rest;
+                const __bf16 part = (__bf16)acc[i + e / 4][j][e % 4];
+                h[j][e] = bits_of(part);
+                if (kOut > 1) acc[i + e / 4][j][e % 4] -= (float)part;
               }
 #pragma unroll
               for (int e = 0; e < 4; ++e) x[e] = h[j][2 * e] | (uint32_t)h[j][2 * e + 1] << 16;
@@ -555,7 +522,6 @@ __global__ __launch_bounds__(kRowsBlock) void k_loss_devices(Tokens a, const Gro
 struct Gradients {
   Matrix g, gt;                // [places][piece], [piece][places]
   Matrix wt, xt;               // [dim][vocabulary], [dim][places]
-  const uint32_t *w_top, *x_top;    // of half floats: the largest magnitudes of the columns
   const float *share, *d_loss;
   uint32_t v0, v1, dim;
   uint32_t steps;              // of the piece
@@ -582,27 +548,8 @@ __device__ inline float factor_of(const Tokens& a, const Gradients& q, uint32_t 
   return a.weight[d] * gptr(q.share)[d] * (q.d_loss ? gptr(q.d_loss)[0] : 1.0f);
 }
 
-// The power of two of column m's sums.
-template <class E>
-__device__ inline int column_scale(const uint32_t* top, uint32_t m)
-{
-  if constexpr (std::is_same<E, F16>::value) return scale_of(gptr(top)[m]) + kGBits;
-  return 0;
-}
-
-template <class E>
-__device__ inline f4 finished(f4 sum, const uint32_t* top, uint32_t m, uint32_t dim, float c)
-{
-#pragma unroll
-  for (uint32_t e = 0; e < 4; ++e) {
-    if constexpr (std::is_same<E, F16>::value) sum[e] = ldexpf(sum[e], -column_scale<E>(top, m + e < dim ? m + e : m));
-    sum[e] *= c;
-  }
-  return sum;
-}
-
-// E: of the operands; X, W: d_x's and d_weight's elements.
-template <class E, class X, class W>
+// X, W: d_x's and d_weight's elements.
+template <class X, class W>
 __global__ __launch_bounds__(kProductBlock, 2) void k_gradients(Tokens a, Gradients q)
 {
   __shared__ __attribute__((aligned(128))) char lds[kProductLds];
@@ -643,7 +590,7 @@ __global__ __launch_bounds__(kProductBlock, 2) void k_gradients(Tokens a, Gradie
   f4 acc[8][4];
   const Pairs pairs = of_x ? q.x_pairs : q.w_pairs;
   pipe.begin(sa, sb, steps, pairs);
-  pipe.run<E>(acc, sa, sb, steps, pairs, false);
+  pipe.run<BF16>(acc, sa, sb, steps, pairs, false);
   const uint32_t n = n0 + lane_n();
   if (of_x) {
     if (n >= a.places) return;
@@ -662,7 +609,7 @@ __global__ __launch_bounds__(kProductBlock, 2) void k_gradients(Tokens a, Gradie
         f4 x = acc[i][j];
         if (!q.first) x += load_f4(sum + m, left);
         if (q.x_units > 1 || !q.last) store_f4(sum + m, x, left);
-        else store_f4(to + m, on ? finished<E>(x, q.w_top, m, q.dim, c) : f4{0, 0, 0, 0}, left);
+        else store_f4(to + m, on ? x * c : f4{0, 0, 0, 0}, left);
       }
     }
   } else {
@@ -677,7 +624,7 @@ __global__ __launch_bounds__(kProductBlock, 2) void k_gradients(Tokens a, Gradie
       for (int i = 0; i < 8; ++i) {
         const uint32_t m = m0 + lane_m<kGroup>(i), left = q.dim - m;
         if (m >= q.dim) continue;
-        if (whole) store_f4(to + m, finished<E>(acc[i][j], q.x_top, m, q.dim, c), left);
+        if (whole) store_f4(to + m, acc[i][j] * c, left);
         else store_f4(sum + m, acc[i][j], left);
       }
     }
@@ -685,7 +632,7 @@ __global__ __launch_bounds__(kProductBlock, 2) void k_gradients(Tokens a, Gradie
 }
 
 // Adds the units of d_x: a lane has four elements of a token.
-template <class E, class X>
+template <class X>
 __global__ __launch_bounds__(kBlock) void k_join_x(Tokens a, Gradients q, Share share)
 {
   for_all_pieces(share, a.places, [&](uint64_t p, uint32_t g) {
@@ -695,12 +642,12 @@ __global__ __launch_bounds__(kBlock) void k_join_x(Tokens a, Gradients q, Share 
     f4 x = {0, 0, 0, 0};
     for (uint32_t u = 0; u < q.x_units; ++u) x += load_f4(q.x_sum + ((uint64_t)u * a.places + p) * q.dim + m, left);
     const bool on = target_of(a, w.t) != kNone;
-    store_f4((X*)q.d_x + (uint64_t)w.t * q.ld_d_x + m, on ? finished<E>(x, q.w_top, m, q.dim, factor_of(a, q, w.d)) : f4{0, 0, 0, 0}, left);
+    store_f4((X*)q.d_x + (uint64_t)w.t * q.ld_d_x + m, on ? x * factor_of(a, q, w.d) : f4{0, 0, 0, 0}, left);
   });
 }
 
 // Adds the units of d_weight of the devices that have several.
-template <class E, class W>
+template <class W>
 __global__ __launch_bounds__(kBlock) void k_join_weight(Tokens a, Gradients q, Share share)
 {
   const uint32_t d = blockIdx.y, lo = q.w_first[d], hi = q.w_first[d + 1];
@@ -710,7 +657,7 @@ __global__ __launch_bounds__(kBlock) void k_join_weight(Tokens a, Gradients q, S
     const uint32_t m = g * 4, left = q.dim - m;
     f4 x = {0, 0, 0, 0};
     for (uint32_t u = lo; u < hi; ++u) x += load_f4(q.w_sum + ((uint64_t)u * q.piece + v) * q.dim + m, left);
-    store_f4((W*)q.d_weight[d] + (q.v0 + v) * q.dim + m, finished<E>(x, q.x_top, m, q.dim, c), left);
+    store_f4((W*)q.d_weight[d] + (q.v0 + v) * q.dim + m, x * c, left);
   });
 }
 
@@ -759,18 +706,28 @@ bool is_operand(const scadles_cross_entropy* ce, const void* p, uint64_t ld)
   return ce->type == SCADLES_BF16 && ce->dim % kStep == 0 && ld % 8 == 0 && is_aligned(p, 16) && ld <= 1u << 22;
 }
 
+// The products of parts that a gradient of a type has, of x or weight (A) and G (B), the greatest last.
+// Float gradients: all but those of 2^-24 of the first and less, six, or three of bfloat16 x and weight.
+// bfloat16 gradients, whose own rounding is 2^-8: those down to 2^-8, which leave 2^-16; of bfloat16 x and
+// weight, two, or one if all gradients are bfloat16 and G is rounded like them.
+Pairs pairs_of(const scadles_cross_entropy* ce, int32_t type)
+{
+  if (ce->type == SCADLES_F32) return type == SCADLES_F32 ? Pairs{6, 0x001102, 0x010120} : Pairs{3, 0x001, 0x010};
+  if (type == SCADLES_F32) return {3, 0, 0x012};
+  return ce->grad_type == SCADLES_F32 ? Pairs{2, 0, 0x01} : Pairs{1, 0, 0};
+}
+
 // How a call is done, and its arrays in the workspace.
 struct Plan {
-  bool half;                   // x and weight in half floats
-  bool half_g;                 // G, and the transposed ones
-  uint32_t planes;             // of x and weight: 2 of floats, else 1
+  bool half;                   // x and weight in half floats for the logits
+  uint32_t planes;             // 2 of these, else 1
+  uint32_t t_planes, g_planes; // of x and weight transposed and of G: kParts of floats, else 1
   uint64_t x_width, x_stride;  // of their rows
   uint64_t vocab_width, wt_stride, xt_stride;
   uint64_t piece, g_stride;    // vocabulary entries at a time
   uint32_t x_units, x_per, w_per, w_units;
   uint16_t *x, *w, *xt, *wt, *g, *gt;
   int32_t *x_scale, *w_scale;
-  uint32_t *x_top, *w_top;
   Part* part;
   float *at_target, *x_sum, *w_sum;
   Group* group;
@@ -809,7 +766,6 @@ void plan_call(const scadles_cross_entropy* ce, const Tokens& a, bool backward, 
   };
   const uint64_t tokens = a.off[a.K], places = a.places, V = ce->vocab;
   p.half = ce->type == SCADLES_F32;
-  p.half_g = p.half || ce->grad_type == SCADLES_F32;
   p.planes = p.half ? 2 : 1;
   p.x_width = round_up(ce->dim, kStep);
   p.x_stride = stride_of(p.x_width);
@@ -826,20 +782,19 @@ void plan_call(const scadles_cross_entropy* ce, const Tokens& a, bool backward, 
     p.bytes = at;
     return;
   }
-  const uint32_t g_planes = p.half_g ? 2 : 1;
+  p.t_planes = p.half ? kParts : 1;
+  p.g_planes = p.half || ce->grad_type == SCADLES_F32 ? kParts : 1;
   p.vocab_width = round_up(V, kStep);
   p.wt_stride = stride_of(p.vocab_width);
   p.xt_stride = stride_of(places);
-  p.piece = piece_of(V, places, g_planes);
+  p.piece = piece_of(V, places, p.g_planes);
   p.g_stride = stride_of(p.piece);
-  p.xt = (uint16_t*)take(ce->dim * p.xt_stride * 2 * p.planes);
-  p.wt = (uint16_t*)take(ce->dim * p.wt_stride * 2 * p.planes);
-  p.g = (uint16_t*)take(places * p.g_stride * 2 * g_planes);
-  p.gt = (uint16_t*)take(p.piece * p.xt_stride * 2 * g_planes);
-  p.w_top = (uint32_t*)take(ce->dim * 4 * 2);
-  p.x_top = p.w_top + ce->dim;
+  p.xt = (uint16_t*)take(ce->dim * p.xt_stride * 2 * p.t_planes);
+  p.wt = (uint16_t*)take(ce->dim * p.wt_stride * 2 * p.t_planes);
+  p.g = (uint16_t*)take(places * p.g_stride * 2 * p.g_planes);
+  p.gt = (uint16_t*)take(p.piece * p.xt_stride * 2 * p.g_planes);
   // units: each about the 256th part of a piece's steps
-  const uint32_t x_pairs = p.planes == 2 ? 3 : 1, w_pairs = ce->grad_type == SCADLES_BF16 ? 1 : p.planes == 2 ? 3 : 2;
+  const uint32_t x_pairs = pairs_of(ce, ce->type).n, w_pairs = pairs_of(ce, ce->grad_type).n;
   const uint64_t rows = div_up(ce->dim, kEdge), steps = (p.piece < V ? p.piece : p.vocab_width) / kStep;
   const uint64_t x_all = rows * div_up(places, kEdge) * steps * x_pairs, w_tiles = rows * div_up(p.piece, kEdge);
   const uint64_t w_all = w_tiles * (places / kStep) * w_pairs;
@@ -946,36 +901,27 @@ hipError_t forward(const scadles_cross_entropy* ce, const Tokens& a, const Plan&
 }
 
 // The operands of the gradients' products, transposed.
-template <class X, class E, int kPlanes>
+template <class X>
 void turn(const scadles_cross_entropy* ce, const Tokens& a, const Plan& p, const void* x, uint64_t ld_x, const void* weight, uint64_t ld_w,
           bool tokens, hipStream_t st)
 {
   const uint32_t dim = ce->dim, down = (uint32_t)div_up(dim, 64), V = (uint32_t)ce->vocab, T = (uint32_t)a.off[a.K];
-  if constexpr (std::is_same<E, F16>::value) {
-    k_clear<<<(uint32_t)div_up(2 * dim, kBlock), kBlock, 0, st>>>(p.w_top, 2 * dim);
-    const uint32_t across = (uint32_t)div_up(dim, 64 * Piece<X>::N);
-    k_column_top<X, false><<<dim3((uint32_t)div_up(V, top_rows(false)), across), kBlock, 0, st>>>(a, (const X*)weight, ld_w, V, dim, p.w_top);
-    if (tokens) k_column_top<X, true><<<dim3((uint32_t)div_up(a.places, top_rows(true)), across), kBlock, 0, st>>>(a, (const X*)x, ld_x, T, dim, p.x_top);
-  }
-  k_turn<X, false, E, kPlanes><<<dim3((uint32_t)(p.vocab_width / 64), down), kBlock, 0, st>>>(a, (const X*)weight, ld_w, V, dim, p.w_top, p.wt_stride,
-                                                                                             p.wt, dim * p.wt_stride);
-  if (tokens)
-    k_turn<X, true, E, kPlanes><<<dim3(a.places / 64, down), kBlock, 0, st>>>(a, (const X*)x, ld_x, T, dim, p.x_top, p.xt_stride, p.xt,
-                                                                             dim * p.xt_stride);
+  k_turn<X, false><<<dim3((uint32_t)(p.vocab_width / 64), down), kBlock, 0, st>>>(a, (const X*)weight, ld_w, V, dim, p.wt_stride, p.wt, dim * p.wt_stride);
+  if (tokens) k_turn<X, true><<<dim3(a.places / 64, down), kBlock, 0, st>>>(a, (const X*)x, ld_x, T, dim, p.xt_stride, p.xt, dim * p.xt_stride);
 }
 
-template <class E, class X, class W>
+template <class X, class W>
 hipError_t backward(const scadles_cross_entropy* ce, const Tokens& a, const Plan& p, const void* x, uint64_t ld_x, const void* weight, uint64_t ld_w,
                     const scadles_cross_entropy_out* out, const float* d_loss, void* d_x, uint64_t ld_d_x, void* const* d_weight, hipStream_t st)
 {
-  constexpr int kPlanes = sizeof(X) == 4 ? 2 : 1, kOut = std::is_same<E, F16>::value ? 2 : 1;
+  constexpr int kOut = sizeof(X) == 4 || sizeof(W) == 4 ? kParts : 1;
   typedef typename std::conditional<sizeof(X) == 4, F16, BF16>::type In;
   const uint32_t dim = ce->dim;
   Logits q;
   std::memset(&q, 0, sizeof(q));
   if (a.places) {
     prepare(q, ce, a, p, x, ld_x, weight, ld_w, st);
-    turn<X, E, kPlanes>(ce, a, p, x, ld_x, weight, ld_w, d_weight != nullptr, st);
+    turn<X>(ce, a, p, x, ld_x, weight, ld_w, d_weight != nullptr, st);
   }
   q.lse = out->lse;
   q.g = p.g;
@@ -990,16 +936,13 @@ hipError_t backward(const scadles_cross_entropy* ce, const Tokens& a, const Plan
   r.gt = {p.gt, q.gt_plane, p.xt_stride};
   r.wt = {p.wt, dim * p.wt_stride, p.wt_stride};
   r.xt = {p.xt, dim * p.xt_stride, p.xt_stride};
-  r.w_top = p.w_top;
-  r.x_top = p.x_top;
   r.share = out->share;
   r.d_loss = d_loss;
   r.dim = dim;
   r.rows = (uint32_t)div_up(dim, kEdge);
   r.x_columns = q.columns;
-  // A is weight or x, B is G: of two parts each the largest products, the greatest last
-  r.x_pairs = kPlanes == 2 ? Pairs{3, 0x010, 0x001} : Pairs{1, 0, 0};
-  r.w_pairs = sizeof(W) == 2 ? Pairs{1, 0, 0} : kPlanes == 2 ? Pairs{3, 0x010, 0x001} : Pairs{2, 0, 0x01};
+  r.x_pairs = pairs_of(ce, ce->type);
+  r.w_pairs = pairs_of(ce, ce->grad_type);
   r.x_units = p.x_units;
   r.x_per = p.x_per;
   r.w_per = p.w_per;
@@ -1026,15 +969,15 @@ hipError_t backward(const scadles_cross_entropy* ce, const Tokens& a, const Plan
     r.last = v1 == a.vocab;
     if (a.places) k_logits<true, In, kOut><<<blocks_for(q), kProductBlock, 0, st>>>(a, q);
     const uint64_t units = (uint64_t)r.rows * r.x_columns * r.x_units + (uint64_t)r.rows * r.w_columns * r.w_first[a.K];
-    if (units) k_gradients<E, X, W><<<(uint32_t)units, kProductBlock, 0, st>>>(a, r);
+    if (units) k_gradients<X, W><<<(uint32_t)units, kProductBlock, 0, st>>>(a, r);
     if (d_weight && p.w_sum) {
       const Share share = share_rows(v1 - v0, quads);
-      k_join_weight<E, W><<<dim3(grid_of(div_up(v1 - v0, share.rows)), a.K), kBlock, 0, st>>>(a, r, share);
+      k_join_weight<W><<<dim3(grid_of(div_up(v1 - v0, share.rows)), a.K), kBlock, 0, st>>>(a, r, share);
     }
   }
   if (r.x_units > 1 && a.places) {
     const Share share = share_rows(a.places, quads);
-    k_join_x<E, X><<<grid_of(div_up(a.places, share.rows)), kBlock, 0, st>>>(a, r, share);
+    k_join_x<X><<<grid_of(div_up(a.places, share.rows)), kBlock, 0, st>>>(a, r, share);
   }
   return hipGetLastError();
 }
@@ -1119,8 +1062,8 @@ scadles_status scadles_cross_entropy_backward(const scadles_cross_entropy* ce, c
   hipStream_t st = static_cast<hipStream_t>(stream);
   const bool b = ce->type == SCADLES_BF16, gb = ce->grad_type == SCADLES_BF16;
   auto go = [&](auto f) { return f(ce, a, p, x, ld_x, weight, ld_weight, out, d_loss, d_x, ld_d_x, d_weight, st); };
-  return launch_status(b ? (gb ? go(backward<BF16, uint16_t, uint16_t>) : go(backward<F16, uint16_t, float>))
-                         : (gb ? go(backward<F16, float, uint16_t>) : go(backward<F16, float, float>)),
+  return launch_status(b ? (gb ? go(backward<uint16_t, uint16_t>) : go(backward<uint16_t, float>))
+                         : (gb ? go(backward<float, uint16_t>) : go(backward<float, float>)),
                        "cross entropy backward");
 }
 
