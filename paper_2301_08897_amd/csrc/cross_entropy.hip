@@ -246,6 +246,10 @@ struct Part {
   float top, sum;
 };
 
+// What the logarithms that a largest one is taken from are counted from: it, or 0 if it is
+// infinite, so that a logit of infinity gives an infinite sum and those of -infinity none.
+__device__ inline float base_of(float top) { return __builtin_fabsf(top) == INFINITY ? 0.0f : top; }
+
 struct Logits {
   Matrix w, x;                 // vocabulary and tokens
   const int32_t *w_scale, *x_scale;   // of half floats: the rows' powers of two
@@ -268,9 +272,10 @@ __device__ inline float exp_of(float x)
   constexpr float log2e = 1.44269504088896340736f;
   if constexpr (kExact) {
     // 2^(x log2 e) with what the product's rounding and log2 e's leave: off by a step of the
-    // result's, in a third of expf's instructions
+    // result's, in a third of expf's instructions. Beyond 2^200, zero and infinity as they are.
     const float h = x * log2e, rest = __builtin_fmaf(x, log2e, -h) + x * 1.92596299e-8f, p = __builtin_amdgcn_exp2f(h);
-    return __builtin_fmaf(p, h > -200.0f ? rest * 0.693147180559945f : 0.0f, p);
+    const float q = __builtin_fmaf(p, rest * 0.693147180559945f, p);
+    return __builtin_fabsf(h) < 200.0f ? q : p;
   }
   else return __builtin_amdgcn_exp2f(x * 1.44269504088896340736f);
 }
@@ -365,7 +370,7 @@ __global__ __launch_bounds__(kProductBlock, 2) void k_logits(Tokens a, Logits q)
         for (int i = 0; i < 8; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e) top = __builtin_fmaxf(top, acc[i][j][e]);
-        const float from = top == -INFINITY ? 0.0f : top;
+        const float from = base_of(top);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
 #pragma unroll
@@ -373,7 +378,7 @@ __global__ __launch_bounds__(kProductBlock, 2) void k_logits(Tokens a, Logits q)
 #pragma unroll
         for (int step = 16; step < 64; step *= 2) {
           const float t = __shfl_xor(top, step, 64), s = __shfl_xor(sum, step, 64);
-          const float most = __builtin_fmaxf(top, t), base = most == -INFINITY ? 0.0f : most;
+          const float most = __builtin_fmaxf(top, t), base = base_of(most);
           sum = sum * exp_of<kExact>(top - base) + s * exp_of<kExact>(t - base);
           top = most;
         }
@@ -384,7 +389,7 @@ __global__ __launch_bounds__(kProductBlock, 2) void k_logits(Tokens a, Logits q)
       asm volatile("" ::: "memory");
       if (threadIdx.x < kEdge && tokens + threadIdx.x < a.places) {
         const Part u = both[threadIdx.x], v = both[kEdge + threadIdx.x];
-        const float most = __builtin_fmaxf(u.top, v.top), base = most == -INFINITY ? 0.0f : most;
+        const float most = __builtin_fmaxf(u.top, v.top), base = base_of(most);
         q.part[(uint64_t)tile * a.places + tokens + threadIdx.x] = {most, u.sum * exp_of<kExact>(u.top - base) + v.sum * exp_of<kExact>(v.top - base)};
       }
     } else {
@@ -461,7 +466,7 @@ __global__ __launch_bounds__(kRowsBlock) void k_loss_rows(Tokens a, const Part* 
   const uint32_t lane = threadIdx.x & 63, s = threadIdx.x >> 6, p = blockIdx.x * 64 + lane;
   float top = -INFINITY, sum = 0.0f;
   auto add = [&](Part x) {
-    const float most = __builtin_fmaxf(top, x.top), base = most == -INFINITY ? 0.0f : most;
+    const float most = __builtin_fmaxf(top, x.top), base = base_of(most);
     sum = sum * expf(top - base) + x.sum * expf(x.top - base);
     top = most;
   };

@@ -172,3 +172,45 @@ def test_the_second_part_of_x_for_bfloat16_gradients(sc):
     want = 0.25 * 2.0**-13 * np.array([[1.0], [-1.0]])
     # G is off by its exponential and logarithm, 8 U each, and both products are rounded
     near(dw[0], want, np.full((2, 1), 0.5 * 20 * U), "bf16")
+
+
+@pytest.mark.parametrize("V,hit", [(300, 299), (300, 7), (9000, 8000), (9000, 0)])
+def test_logits_at_infinity(sc, V, hit):
+    """The log-sum of a row with one is infinite, and so is the loss of any other target; rows that have it at -infinity,
+    and other devices, are as without it."""
+    torch, dev = torch_dev()
+    T, dim, off = 70, 64, [0, 40, 70]
+    x = torch.rand(T, dim, device=dev).add_(0.5).to(torch.bfloat16)
+    x[40:] *= -1
+    x[3] *= -1
+    w = torch.randn(V, dim, device=dev).to(torch.bfloat16)
+    ids = torch.randint(0, V - 2, (T,), device=dev)
+    ids = torch.where(ids >= hit, ids + 1, ids)
+    ids[5] = hit
+    h = sc.LinearCrossEntropy(V, dim, devices=2)
+    w[hit] = float("inf")
+    f = h.forward(x, w, ids, tok_off=off, weights=[1.0, 1.0])
+    rows = [t for t in range(40) if t != 3]
+    assert bool((f.lse[rows] == float("inf")).all())
+    assert bool((f.nll[[t for t in rows if t != 5]] == float("inf")).all()) and bool(f.nll[5].isnan())     # inf - inf
+    keep = [3] + list(range(40, T))
+    want = h.forward(-x.abs(), w, ids, tok_off=off, weights=[1.0, 1.0])       # the entry is at -infinity for every row
+    assert torch.equal(f.lse[keep], want.lse[keep]) and torch.equal(f.nll[keep], want.nll[keep])
+    assert bool(f.lse[keep].isfinite().all()) and bool(f.device_loss[1].isfinite())
+    ids[5] = ids[6]
+    f = h.forward(x, w, ids, tok_off=off, weights=[1.0, 1.0])
+    assert f.device_loss[0] == float("inf") and f.loss[0] == float("inf") and torch.equal(f.device_loss[1], want.device_loss[1])
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_logits_beyond_the_largest_float(sc, kind):
+    torch, dev = torch_dev()
+    V, dim, T = 600, 32, 9
+    t = dtype(torch, kind)
+    x, w = (torch.rand(T, dim, device=dev) + 0.5).to(t), torch.randn(V, dim, device=dev).to(t)
+    x[4] = 0
+    w[500] = torch.finfo(t).max
+    f = sc.LinearCrossEntropy(V, dim).forward(x, w, torch.arange(T, device=dev))
+    rest = [i for i in range(T) if i != 4]
+    assert bool((f.lse[rest] == float("inf")).all()) and bool((f.nll[rest] == float("inf")).all())
+    assert abs(float(f.lse[4]) - float(np.log(V))) <= 8 * U * np.log(V) + 24 * U
