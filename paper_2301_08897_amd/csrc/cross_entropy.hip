@@ -547,10 +547,11 @@ struct Gradients {
   uint32_t first, last;        // whether the piece is
 };
 
-// What device d's sums are multiplied with.
+// What device d's sums are multiplied with; 0 where no rows are counted, whatever d_loss is.
 __device__ inline float factor_of(const Tokens& a, const Gradients& q, uint32_t d)
 {
-  return a.weight[d] * gptr(q.share)[d] * (q.d_loss ? gptr(q.d_loss)[0] : 1.0f);
+  const float share = gptr(q.share)[d];
+  return share == 0.0f ? 0.0f : a.weight[d] * share * (q.d_loss ? gptr(q.d_loss)[0] : 1.0f);
 }
 
 // X, W: d_x's and d_weight's elements.

@@ -214,3 +214,19 @@ def test_logits_beyond_the_largest_float(sc, kind):
     rest = [i for i in range(T) if i != 4]
     assert bool((f.lse[rest] == float("inf")).all()) and bool((f.nll[rest] == float("inf")).all())
     assert abs(float(f.lse[4]) - float(np.log(V))) <= 8 * U * np.log(V) + 24 * U
+
+
+@pytest.mark.parametrize("kind,grad", TYPES)
+def test_devices_without_counted_rows_under_an_infinite_gradient(sc, kind, grad):
+    """The sum over no rows is 0, whatever it is multiplied with."""
+    torch, dev = torch_dev()
+    T, V, dim, off = 400, 70, 24, [0, 100, 100, 400]
+    t = dtype(torch, kind)
+    x, w = torch.randn(T, dim, device=dev).to(t), torch.randn(V, dim, device=dev).to(t)
+    ids = torch.randint(0, V, (T,), device=dev)
+    ids[100:] = -1
+    h = sc.LinearCrossEntropy(V, dim, devices=3)
+    f = h.forward(x, w, ids, tok_off=off)
+    dw = torch.ones(3, V, dim, dtype=dtype(torch, grad), device=dev)
+    dx = h.backward(x, w, ids, f, dw, tok_off=off, d_loss=torch.tensor([float("inf")], device=dev))
+    assert not dw[1:].any() and not dx[100:].any() and not dw[0].isfinite().any()
