@@ -44,7 +44,10 @@ using namespace scadles;
 
 namespace {
 
-constexpr uint64_t kPieceBytes = 256ull << 20;    // of G and its transpose, about
+// Of one plane of G and its transpose, about: three planes have pieces of the same length, since shorter ones
+// cost the products more than G's memory does (8192 x 65536 x 1024 bfloat16 with float gradients: 8.05 ms; 256
+// MiB for the three: 10.5. 2039 x 20011 x 500 floats: 1094 us, 1162; 14285 x 24630 x 64 floats: 4.68 ms, 4.52).
+constexpr uint64_t kPieceBytes = 256ull << 20;
 constexpr uint32_t kLeastPiece = 2048;            // vocabulary entries of a piece, at least
 constexpr uint32_t kNone = ~0u;
 constexpr uint32_t kMost = 1u << 22;              // tokens and vocabulary entries: 32-bit offsets within a tile
@@ -740,11 +743,11 @@ struct Plan {
   uint64_t bytes;
 };
 
-// Vocabulary entries of a piece: as many rows of tiles as G's share of kPieceBytes holds, or a
-// few less where the tiles then come in whole rounds of the compute units.
-uint64_t piece_of(uint64_t vocab, uint64_t places, uint32_t planes)
+// Vocabulary entries of a piece: as many rows of tiles as a plane of G's share of kPieceBytes
+// holds, or a few less where the tiles then come in whole rounds of the compute units.
+uint64_t piece_of(uint64_t vocab, uint64_t places)
 {
-  const uint64_t row = places * 2 * planes * kEdge, columns = div_up(places, kEdge), all = div_up(vocab, kEdge);
+  const uint64_t row = places * 2 * kEdge, columns = div_up(places, kEdge), all = div_up(vocab, kEdge);
   uint64_t most = row ? kPieceBytes / 2 / row : all;
   if (most < kLeastPiece / kEdge) most = kLeastPiece / kEdge;
   if (most >= all) return all * kEdge;
@@ -793,7 +796,7 @@ void plan_call(const scadles_cross_entropy* ce, const Tokens& a, bool backward, 
   p.vocab_width = round_up(V, kStep);
   p.wt_stride = stride_of(p.vocab_width);
   p.xt_stride = stride_of(places);
-  p.piece = piece_of(V, places, p.g_planes);
+  p.piece = piece_of(V, places);
   p.g_stride = stride_of(p.piece);
   p.xt = (uint16_t*)take(ce->dim * p.xt_stride * 2 * p.t_planes);
   p.wt = (uint16_t*)take(ce->dim * p.wt_stride * 2 * p.t_planes);
