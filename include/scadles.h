@@ -700,13 +700,13 @@ scadles_status scadles_layer_norm_backward(const scadles_norm* norm, const scadl
  * weight are multiplied as they are; floats are taken as sums of two half floats (22
  * bits), after a power of two has brought the largest of their row to 2^13 .. 2^14, so
  * that they are off by 2^-22 of their size or 2^-38 of that largest one. Gradients: a
- * product of G with an element of x or weight is off by 2^-21 of its own size, at any
- * magnitude above 2^-126, if it goes into a float, by 2^-14 if it goes into a bfloat16;
- * G is rounded to bfloat16 (2^-8) where x, weight and all gradients are, so that float
- * gradients are what asks for more. No row or device has a part in the precision of
- * another's, and an entry masked with finite values is like none. Elements that are
- * not finite make what they go into NaN (infinities of bfloat16 x and weight as
- * in exact arithmetic in the forward pass).
+ * product of G with an element of x or weight is off by 2^-21 of its own size if it goes
+ * into a float and by 2^-14 if it goes into a bfloat16, or by 2^-125 of one of its two
+ * factors; G is rounded to bfloat16 (2^-8) where x, weight and all gradients are, so
+ * that float gradients are what asks for more. No row or device has a part in the
+ * precision of another's, and an entry masked with finite values is like none.
+ * Elements that are not finite make what they go into NaN or what exact arithmetic
+ * makes of it (always the latter in the forward pass of bfloat16).
  *   vocab         1 <= vocab <= 2^22; tokens <= 2^22.
  *   dim           1 <= dim <= 65536.
  *   type          of x, weight and d_x: SCADLES_F32 or SCADLES_BF16.

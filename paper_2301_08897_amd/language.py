@@ -479,7 +479,8 @@ class LinearCrossEntropy:
         pass's (its lse and share are read). ``weights``: by default ones, so that every
         device has the gradient of its own loss, before the aggregation weights it; the
         forward pass's give the gradient of its ``loss``. All of it times ``d_loss``, one
-        float32 on the GPU, if given."""
+        float32 on the GPU, if given. With bfloat16 ``x`` and ``d_weight`` the softmax's part is
+        rounded to bfloat16 before it is multiplied; float32 gradients keep it whole."""
         _gpu(x, "x", _FLOATS, None)
         each, kind, where = (), x.dtype, None
         if d_weight is not None:
